@@ -9,6 +9,8 @@ the library sources (``csrc/``), its build script and a thin ctypes binding.
 
 from .tokenizer import (CL100K, DEEPSEEK, GPT2, O200K, PATTERNS, Session, Tokenizer, splice_plan,  # noqa: F401
                         status_string, sync_boundaries)
+from .model import (head_scores, head_scores_grad, head_scores_grad_workspace, head_scores_workspace,  # noqa: F401
+                    step_plan, token_scores, token_scores_grad, token_scores_workspace)
 from ._lib import TokTierError  # noqa: F401
 
 

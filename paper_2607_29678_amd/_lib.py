@@ -1,4 +1,4 @@
-"""ctypes declarations of the C ABI in ``include/toktier.h``.
+"""ctypes declarations of the C ABI in ``include/toktier.h`` and ``include/toktier_model.h``.
 
 Loading fails loudly when ``libtoktier.so`` has not been built: there is no
 fallback implementation in this package.
@@ -60,6 +60,30 @@ SIGNATURES = {
     "tt_stage_times": (ctypes.c_int, [_P, _P, _P, _I32, ctypes.POINTER(_I32)]),
 }
 
+# the same for include/toktier_model.h
+_F = ctypes.c_float
+MODEL_SIGNATURES = {
+    "tt_step_plan": (ctypes.c_int, [_P, _P]),
+    "tt_token_scores_workspace": (_I64, [_I64, _I64, _I32]),
+    "tt_token_scores": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _I32, _P, _P, _P, _I64, _P]),
+    "tt_token_scores_grad": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "tt_head_scores_workspace": (_I64, [_I64, _I64, _I64]),
+    "tt_head_scores": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _I64, _P]),
+    "tt_head_scores_grad_workspace": (_I64, [_I64, _I64, _I64, _I32]),
+    "tt_head_scores_grad": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _P, _I64,
+                                           _P, _I64, _P, _I64, _P]),
+}
+TT_F32, TT_BF16, TT_F16 = 0, 1, 2
+TT_MAX_ALTERNATIVES = 64
+
+
+class Step(ctypes.Structure):
+    """``tt_step``: one step of a server with a paged cache."""
+
+    _fields_ = [("n_requests", _I32), ("page_size", _I32), ("table_width", _I32), ("table_stride", _I64),
+                ("max_tokens", _I64), ("n_free", _I64), ("cached", _P), ("fresh", _P), ("held", _P), ("ids", _P),
+                ("free_pages", _P), ("free_count", _P), ("tables", _P), ("offsets", _P), ("lengths", _P), ("pages", _P),
+                ("slots", _P), ("positions", _P), ("requests", _P), ("targets", _P), ("result", _P)]
 
 
 class Options(ctypes.Structure):
@@ -95,7 +119,7 @@ def load():
             raise ImportError("libtoktier.so is not built: run __graft_entry__.build() "
                               "or python -m paper_2607_29678_amd._build")
         lib = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in {**SIGNATURES, **MODEL_SIGNATURES}.items():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args

@@ -1,0 +1,117 @@
+// What the scores of stored logits and of the head share: element types, the
+// running statistics of a softmax and how two of them join.
+#pragma once
+
+#include <type_traits>
+
+#include "../../include/toktier_model.h"
+#include "tt_internal.h"
+
+namespace tt {
+
+using bf16_t = __bf16;
+using f16_t = _Float16;
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr float NEG_INF = -__builtin_inff();
+
+// Statistics of a part of a row, in powers of two: m the largest logit, s the
+// sum of e_j = 2^d_j and u the sum of e_j d_j, with d_j = (x_j - m) c and
+// c = scale / log 2.  m stays in units of the logits: x_j - m is exact where it
+// matters and cannot overflow to the wrong side for masks of the type's lowest
+// value, which (x_j c) - (m c) could.
+struct Stats {
+  float m, s, u;
+};
+
+__device__ __forceinline__ Stats empty_stats() { return {NEG_INF, 0.f, 0.f}; }
+
+// A finite reference to subtract: nothing but -inf so far leaves 0.
+__device__ __forceinline__ float reference(float m) { return m == NEG_INF ? 0.f : m; }
+
+// e d for e = 2^d: 0 where e is 0, also for d = -inf; NaN stays.
+__device__ __forceinline__ float weigh(float e, float d) { return e * fmaxf(d, -1e30f); }
+
+// a's sums moved to the larger maximum m.
+__device__ __forceinline__ void lower(Stats& a, float m, float c) {
+  if (a.m == m || a.s == 0.f) {
+    a.m = m;
+    return;
+  }
+  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+  a.u = f * a.u + weigh(f, d) * a.s;
+  a.s *= f;
+  a.m = m;
+}
+
+__device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  lower(a, m, c);
+  lower(b, m, c);
+  return {m, a.s + b.s, a.u + b.u};
+}
+
+__device__ __forceinline__ Stats shuffled_xor(const Stats& a, int lane_mask) {
+  return {__shfl_xor(a.m, lane_mask), __shfl_xor(a.s, lane_mask), __shfl_xor(a.u, lane_mask)};
+}
+
+// A row's results from the statistics of the whole row.
+struct RowScores {
+  float m, log_s, entropy;
+};
+__device__ __forceinline__ RowScores row_scores(const Stats& a) {
+  if (a.s == 0.f) return {NEG_INF, NEG_INF, 0.f};  // nothing but -inf
+  if (!(a.s < __builtin_inff()) || a.m == __builtin_inff()) {
+    const float nan = __builtin_nanf("");
+    return {nan, nan, nan};
+  }
+  const float l = __builtin_amdgcn_logf(a.s);  // base 2
+  return {a.m, LN2 * l, LN2 * (l - a.u / a.s)};
+}
+
+// log p of logit x in a row with these results.
+__device__ __forceinline__ float log_prob(float x, const RowScores& r, float scale) {
+  if (r.log_s == NEG_INF) return NEG_INF;
+  return (x - r.m) * scale - r.log_s;
+}
+
+__device__ __forceinline__ float given_log_prob(int32_t target, int64_t vocab, float x, const RowScores& r, float scale) {
+  if (target < 0) return 0.f;
+  return target < vocab ? log_prob(x, r, scale) : __builtin_nanf("");
+}
+
+// The gradient of a row with respect to its logits, G_j = a p_j + b p_j d_j
+// (+ at the given token: g), with p_j = 2^d_j and d_j = (x_j - m) c - log2 s.
+struct RowGrad {
+  float m, l2, a, b, g;
+  int32_t target;
+  bool zero;
+};
+__device__ __forceinline__ RowGrad row_grad(const int32_t* targets, const float* stats, const float* entropy,
+                                            const float* grad_logprobs, const float* grad_entropy, int64_t row,
+                                            int64_t vocab, float scale) {
+  RowGrad r;
+  r.target = targets ? targets[row] : -1;
+  r.m = stats[2 * row];
+  const float log_s = stats[2 * row + 1];
+  const float gl = grad_logprobs && r.target >= 0 ? grad_logprobs[row] : 0.f;
+  const float ge = grad_entropy ? grad_entropy[row] : 0.f;
+  const float h = grad_entropy ? entropy[row] : 0.f;
+  r.l2 = log_s * LOG2E;
+  r.a = -scale * (gl + ge * h);
+  r.b = -scale * ge * LN2;
+  r.g = scale * gl;
+  r.zero = (gl == 0.f && ge == 0.f) || log_s == NEG_INF;
+  if (r.target >= vocab) r.a = __builtin_nanf("");
+  return r;
+}
+__device__ __forceinline__ float grad_of(float x, float c, const RowGrad& r) {
+  const float d = fmaf(x - r.m, c, -r.l2), p = __builtin_amdgcn_exp2f(d);
+  return fmaf(weigh(p, d), r.b, p * r.a);
+}
+
+inline bool score_type(int32_t type) { return type == TT_F32 || type == TT_BF16 || type == TT_F16; }
+inline bool good_scale(float scale) { return scale > 0.f && scale < __builtin_inff(); }
+
+}  // namespace tt

@@ -1,0 +1,495 @@
+// tt_token_scores and its gradient: log probabilities of given tokens, entropy
+// and the top alternatives of rows of stored logits.
+//
+// Forward: one pass over the logits.  Every thread keeps a running maximum and
+// the two sums of a softmax (sum e and sum e d, which gives the entropy) of the
+// entries that it strides over.  The running maxima also find the alternatives:
+// the n_alt-th largest of 128 groups' maxima is a lower bound of the n_alt-th
+// largest logit, so entries below it are passed over, one comparison for each
+// 16-byte vector, and the few above it are kept in LDS and ordered at the end.
+#include "tt_scores.h"
+
+namespace tt {
+namespace {
+
+constexpr int SC_THREADS = 256;
+constexpr int SC_CANDS = 1024;     // candidates that are ordered in LDS
+constexpr int SC_SPLIT_COLS = 2048;  // fewest columns of a part of a row
+constexpr int SC_MAX_SPLITS = 64;  // parts of a row: one list per lane when they are joined
+constexpr int64_t SC_BLOCKS = 1024;  // blocks that fill the chip (4 per compute unit)
+
+// Parts of a row that several blocks take: one block takes a row whole where there are rows enough.
+int scores_splits(int64_t rows, int64_t vocab) {
+  if (rows <= 0 || rows >= SC_BLOCKS) return 1;
+  int64_t n = SC_BLOCKS / rows, most = vocab / SC_SPLIT_COLS;
+  if (n > most) n = most;
+  if (n > SC_MAX_SPLITS) n = SC_MAX_SPLITS;
+  return n < 1 ? 1 : (int)n;
+}
+
+// A part's statistics and its alternatives in descending order (0: none)
+struct PartHead {
+  Stats st;
+  float pad;
+};
+__host__ __device__ inline int64_t part_bytes(int n_alt) { return (int64_t)sizeof(PartHead) + 8 * (int64_t)n_alt; }
+
+// Order of alternatives: the larger logit, then the lower ID.  Never 0.
+__device__ __forceinline__ uint64_t alt_key(float x, uint32_t id) {
+  const uint32_t b = __float_as_uint(x + 0.f);  // (-0 equals 0)
+  const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
+  return ((uint64_t)o << 32) | (0xFFFFFFFFu - id);
+}
+__device__ __forceinline__ float alt_value(uint64_t key) {
+  const uint32_t o = (uint32_t)(key >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+__device__ __forceinline__ int32_t alt_id(uint64_t key) { return (int32_t)(0xFFFFFFFFu - (uint32_t)key); }
+
+template <class T>
+struct Vec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  T v[N];
+};
+template <class T>
+__device__ __forceinline__ Vec<T> load_vec(const T* p) {
+  Vec<T> r;
+  __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T)), 16);
+  return r;
+}
+template <class T>
+__device__ __forceinline__ Vec<T> load_vec_aligned(const T* p) {
+  Vec<T> r;
+  __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), 16);
+  return r;
+}
+
+// A thread's entries of columns [0, n) of p: 16-byte vectors of the aligned
+// middle, strided over the block, and one entry of the head or the tail each.
+template <class T>
+struct Span {
+  const T* p;
+  int64_t n, head, vecs, tail;
+  __device__ Span(const T* p_, int64_t n_) : p(p_), n(n_) {
+    constexpr int N = Vec<T>::N;
+    head = (int64_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int64_t)sizeof(T);
+    if (head > n) head = n;
+    vecs = (n - head) / N;
+    tail = head + vecs * N;
+  }
+};
+
+template <class T>
+struct ScoreArgs {
+  const T* logits;
+  int64_t rows, vocab, stride;
+  float scale;
+  const int32_t* targets;
+  float *logprobs, *stats, *entropy;
+  int n_alt;
+  int32_t* alt_ids;
+  float* alt_logprobs;
+  uint8_t* parts;  // workspace: rows * splits parts
+  int splits;
+};
+
+struct ScoreShared {
+  Stats st[SC_THREADS / 64];
+  float maxima[SC_THREADS];
+  uint64_t cands[SC_CANDS];
+  uint64_t best[TT_MAX_ALTERNATIVES];
+  float bound;
+  int n_cands, n_ties;
+};
+
+__device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(alt_key(x, 0) >> 32); }
+
+// A value that at least n_alt entries seen so far reach, from the threads'
+// running maxima: the n_alt-th largest of 128 maxima of two threads each, found
+// bit by bit (in order of values, down to LOWEST) in one wave.  -inf where fewer
+// than n_alt of them are larger.
+template <uint32_t LOWEST>
+__device__ __forceinline__ float bound_of(float mine, int n_alt, ScoreShared& sh) {
+  const int tid = threadIdx.x;
+  sh.maxima[tid] = mine;
+  __syncthreads();
+  if (tid < 64) {
+    const uint32_t a = ordered(fmaxf(sh.maxima[tid], sh.maxima[tid + 64]));
+    const uint32_t b = ordered(fmaxf(sh.maxima[tid + 128], sh.maxima[tid + 192]));
+    uint32_t key = 0;
+#pragma unroll
+    for (uint32_t bit = 0x80000000u; bit >= LOWEST; bit >>= 1) {
+      const uint32_t want = key | bit;
+      const int n = __popcll(__ballot(a >= want)) + __popcll(__ballot(b >= want));
+      if (n >= n_alt) key = want;
+    }
+    if (tid == 0) sh.bound = key <= 0x007FFFFFu ? NEG_INF : alt_value((uint64_t)key << 32);
+  }
+  __syncthreads();
+  return sh.bound;
+}
+
+// Orders the n candidates by counting the better ones (keys are distinct).
+__device__ __forceinline__ void order_candidates(int n, int n_alt, ScoreShared& sh) {
+  for (int i = threadIdx.x; i < n; i += SC_THREADS) {
+    const uint64_t k = sh.cands[i];
+    int place = 0;
+    for (int j = 0; j < n; j++) place += sh.cands[j] > k;
+    if (place < n_alt) sh.best[place] = k;
+  }
+}
+
+// The alternatives of a span whose candidates did not fit: `mine` is the
+// thread's largest entry, and bound_of() now speaks for the whole span.
+//  - Entries above the bound are collected again; if that falls short of n_alt,
+//    equal entries (masks of a finite value) follow in order of their IDs.
+//  - Should even the entries above it not fit, places are filled one by one.
+template <class T>
+__device__ __noinline__ void find_again(const Span<T>& sp, uint32_t first, int n_alt, float mine, ScoreShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const float bound = bound_of<1u>(mine, n_alt, sh);
+  if (tid == 0) sh.n_cands = 0;
+  __syncthreads();
+  for (int64_t j = tid; j < sp.n; j += SC_THREADS) {
+    const float x = (float)sp.p[j];
+    if (x > bound) {
+      const int at = atomicAdd(&sh.n_cands, 1);
+      if (at < SC_CANDS) sh.cands[at] = alt_key(x, first + (uint32_t)j);
+    }
+  }
+  __syncthreads();
+  const int n = sh.n_cands;
+  if (n <= SC_CANDS) {
+    order_candidates(n, n_alt, sh);
+    int have = n;
+    for (int64_t j0 = 0; j0 < sp.n && have < n_alt && bound > NEG_INF; j0 += SC_THREADS) {
+      const int64_t j = j0 + tid;
+      const bool tie = j < sp.n && (float)sp.p[j] == bound;
+      const uint64_t votes = __ballot(tie);
+      __syncthreads();
+      if (lane == 0) sh.maxima[wave] = (float)__popcll(votes);
+      __syncthreads();
+      int at = have + __popcll(votes & ((1ull << lane) - 1ull));
+      for (int w = 0; w < SC_THREADS / 64; w++) {
+        if (w < wave) at += (int)sh.maxima[w];
+        have += (int)sh.maxima[w];
+      }
+      if (tie && at < n_alt) sh.best[at] = alt_key(bound, first + (uint32_t)j);
+    }
+    __syncthreads();
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < n_alt; r++) {
+    uint64_t k = 0;  // the thread's best key below the last one
+    for (int64_t j = tid; j < sp.n; j += SC_THREADS) {
+      const uint64_t q = alt_key((float)sp.p[j], first + (uint32_t)j);
+      if (q < last && q > k) k = q;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t o = __shfl_xor(k, d);
+      k = o > k ? o : k;
+    }
+    __syncthreads();
+    if (lane == 0) sh.cands[wave] = k;
+    __syncthreads();
+    last = sh.cands[0];
+    for (int w = 1; w < SC_THREADS / 64; w++) last = sh.cands[w] > last ? sh.cands[w] : last;
+    if (tid == 0) sh.best[r] = last;
+  }
+  __syncthreads();
+}
+
+// One part of one row per block.
+template <class T, bool ALT>
+__global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
+  __shared__ ScoreShared sh;
+  constexpr int N = Vec<T>::N, U = 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row = blockIdx.x / a.splits;
+  const int part = (int)(blockIdx.x - row * a.splits);
+  const int64_t c0 = a.vocab * part / a.splits, c1 = a.vocab * (part + 1) / a.splits;
+  const T* p = a.logits + row * a.stride + c0;
+  const Span<T> sp(p, c1 - c0);
+  const float c = a.scale * LOG2E;
+  const uint32_t first = (uint32_t)c0;
+  if (ALT) {
+    if (tid < a.n_alt) sh.best[tid] = 0;
+    if (tid == 0) sh.n_cands = 0;
+  }
+
+  Stats st = empty_stats();
+  float bound = NEG_INF;
+  auto sums = [&](float x, float ref) {
+    const float d = (x - ref) * c, e = __builtin_amdgcn_exp2f(d);
+    st.s += e;
+    st.u += weigh(e, d);
+  };
+  auto keep = [&](float x, int64_t j) {
+    if (x >= bound && x > NEG_INF) {
+      const int at = atomicAdd(&sh.n_cands, 1);
+      if (at < SC_CANDS) sh.cands[at] = alt_key(x, first + (uint32_t)j);
+    }
+  };
+  // U vectors at a time share one move of the maximum.  The loop runs equally
+  // often in every thread: it holds barriers.
+  const int64_t steps = (sp.vecs + U * SC_THREADS - 1) / (U * SC_THREADS);
+  for (int64_t step = 0; step < steps; step++) {
+    const int64_t v = step * U * SC_THREADS + tid;
+    Vec<T> y[U];
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      if (v + k * SC_THREADS < sp.vecs) {
+        y[k] = load_vec_aligned(p + sp.head + (v + k * SC_THREADS) * N);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) y[k].v[i] = (T)NEG_INF;
+      }
+    }
+    float x[U][N], top[U], m = st.m;
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        x[k][i] = (float)y[k].v[i];
+        top[k] = i ? fmaxf(top[k], x[k][i]) : x[k][i];
+      }
+      m = fmaxf(m, top[k]);
+    }
+    lower(st, m, c);
+    const float ref = reference(m);
+#pragma unroll
+    for (int k = 0; k < U; k++)
+#pragma unroll
+      for (int i = 0; i < N; i++) sums(x[k][i], ref);
+    if (ALT) {
+      if ((step & (step + 1)) == 0) bound = bound_of<0x10000u>(st.m, a.n_alt, sh);  // after 1, 2, 4, 8 ... steps
+#pragma unroll
+      for (int k = 0; k < U; k++)
+        if (top[k] >= bound)
+#pragma unroll
+          for (int i = 0; i < N; i++) keep(x[k][i], sp.head + (v + k * SC_THREADS) * N + i);
+    }
+  }
+  if (ALT && steps == 0) __syncthreads();  // n_cands
+  auto edge = [&](int64_t j) {
+    const float x = (float)p[j], m = fmaxf(st.m, x);
+    lower(st, m, c);
+    sums(x, reference(m));
+    if (ALT) keep(x, j);
+  };
+  if (tid < sp.head) edge(tid);
+  if (sp.tail + tid < sp.n) edge(sp.tail + tid);
+  const float mine = st.m;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
+  if (lane == 0) sh.st[wave] = st;
+  __syncthreads();
+  st = sh.st[0];
+#pragma unroll
+  for (int w = 1; w < SC_THREADS / 64; w++) st = join(st, sh.st[w], c);
+
+  if (ALT) {
+    const int n = sh.n_cands;
+    if (n <= SC_CANDS) {
+      order_candidates(n, a.n_alt, sh);
+      __syncthreads();
+    } else {
+      __syncthreads();
+      find_again(sp, first, a.n_alt, mine, sh);
+    }
+  }
+  if (a.splits > 1) {
+    uint8_t* out = a.parts + (row * a.splits + part) * part_bytes(a.n_alt);
+    if (tid == 0) reinterpret_cast<PartHead*>(out)->st = st;
+    if (ALT && tid < a.n_alt) reinterpret_cast<uint64_t*>(out + sizeof(PartHead))[tid] = sh.best[tid];
+    return;
+  }
+  const RowScores r = row_scores(st);
+  if (tid == 0) {
+    const int32_t t = a.targets ? a.targets[row] : -1;
+    if (a.logprobs) a.logprobs[row] = given_log_prob(t, a.vocab, t >= 0 && t < a.vocab ? (float)p[t] : 0.f, r, a.scale);
+    if (a.stats) {
+      a.stats[2 * row] = r.m;
+      a.stats[2 * row + 1] = r.log_s;
+    }
+    if (a.entropy) a.entropy[row] = r.entropy;
+  }
+  if (ALT && tid < a.n_alt) {
+    const uint64_t k = sh.best[tid];
+    const bool nan = r.log_s != r.log_s;
+    a.alt_ids[row * a.n_alt + tid] = k && !nan ? alt_id(k) : -1;
+    a.alt_logprobs[row * a.n_alt + tid] = nan ? r.log_s : k ? log_prob(alt_value(k), r, a.scale) : NEG_INF;
+  }
+}
+
+// Joins the parts of a row: one wave per row, one part per lane.
+template <class T>
+__global__ __launch_bounds__(64) void scores_join_kernel(ScoreArgs<T> a) {
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x;
+  const float c = a.scale * LOG2E;
+  const uint8_t* in = a.parts + (row * a.splits + lane) * part_bytes(a.n_alt);
+  const bool have = lane < a.splits;
+  Stats st = have ? reinterpret_cast<const PartHead*>(in)->st : empty_stats();
+#pragma unroll
+  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
+  const RowScores r = row_scores(st);
+  const bool nan = r.log_s != r.log_s;
+  if (lane == 0) {
+    const int32_t t = a.targets ? a.targets[row] : -1;
+    if (a.logprobs)
+      a.logprobs[row] = given_log_prob(t, a.vocab, t >= 0 && t < a.vocab ? (float)a.logits[row * a.stride + t] : 0.f, r,
+                                       a.scale);
+    if (a.stats) {
+      a.stats[2 * row] = r.m;
+      a.stats[2 * row + 1] = r.log_s;
+    }
+    if (a.entropy) a.entropy[row] = r.entropy;
+  }
+  // the parts' lists are in order: the best of their heads is the next one
+  const uint64_t* list = reinterpret_cast<const uint64_t*>(in + sizeof(PartHead));
+  int at = 0;
+  uint64_t head = have && a.n_alt ? list[0] : 0;
+  for (int i = 0; i < a.n_alt; i++) {
+    uint64_t k = head;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t o = __shfl_xor(k, d);
+      k = o > k ? o : k;
+    }
+    if (k && head == k) {
+      at++;
+      head = at < a.n_alt ? list[at] : 0;
+    }
+    if (lane == 0) {
+      a.alt_ids[row * a.n_alt + i] = k && !nan ? alt_id(k) : -1;
+      a.alt_logprobs[row * a.n_alt + i] = nan ? r.log_s : k ? log_prob(alt_value(k), r, a.scale) : NEG_INF;
+    }
+  }
+}
+
+// Gradient: every entry is read once and written once.  A block takes up to
+// GR_COLS columns of a row; the stores are aligned, the loads may not be.
+constexpr int GR_U = 4;
+template <class T>
+constexpr int64_t grad_cols() { return (int64_t)SC_THREADS * Vec<T>::N * GR_U; }
+
+template <class T>
+struct GradArgs {
+  const T* logits;
+  T* grad;
+  int64_t rows, vocab, stride, grad_stride;
+  int64_t chunks;  // blocks per row
+  float scale;
+  const int32_t* targets;
+  const float *stats, *entropy, *grad_logprobs, *grad_entropy;
+};
+
+template <class T>
+__global__ __launch_bounds__(SC_THREADS) void scores_grad_kernel(GradArgs<T> a) {
+  constexpr int N = Vec<T>::N;
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  const T* in = a.logits + row * a.stride;
+  const Span<T> sp(a.grad + row * a.grad_stride, a.vocab);
+  T* out = a.grad + row * a.grad_stride;
+  const RowGrad g = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, row, a.vocab, a.scale);
+  const float c = a.scale * LOG2E;
+  auto one = [&](float x, bool given) {
+    if (g.zero) return (T)0.f;
+    const float y = grad_of(x, c, g);
+    return (T)(given ? y + g.g : y);
+  };
+  const int64_t v0 = chunk * SC_THREADS * GR_U + tid;
+  Vec<T> x[GR_U];
+#pragma unroll
+  for (int k = 0; k < GR_U; k++)
+    if (v0 + k * SC_THREADS < sp.vecs) x[k] = load_vec(in + sp.head + (v0 + k * SC_THREADS) * N);
+#pragma unroll
+  for (int k = 0; k < GR_U; k++) {
+    const int64_t v = v0 + k * SC_THREADS;
+    if (v < sp.vecs) {
+      Vec<T> y;
+      const int64_t at = g.target - (sp.head + v * N);  // place of the given token in this vector
+      if (at >= 0 && at < N) {
+#pragma unroll
+        for (int i = 0; i < N; i++) y.v[i] = one((float)x[k].v[i], i == (int)at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) y.v[i] = one((float)x[k].v[i], false);
+      }
+      __builtin_memcpy(__builtin_assume_aligned(out + sp.head + v * N, 16), &y, 16);
+    }
+  }
+  if (chunk == 0 && tid < sp.head) out[tid] = one((float)in[tid], tid == g.target);
+  if (chunk == a.chunks - 1 && sp.tail + tid < a.vocab) out[sp.tail + tid] = one((float)in[sp.tail + tid], sp.tail + tid == g.target);
+}
+
+template <class T>
+int run_scores(ScoreArgs<T> a, hipStream_t st) {
+  if (launch(a.n_alt ? scores_kernel<T, true> : scores_kernel<T, false>, dim3((uint32_t)(a.rows * a.splits)),
+             dim3(SC_THREADS), st, a) != hipSuccess)
+    return TT_ERR_HIP;
+  if (a.splits > 1 && launch(scores_join_kernel<T>, dim3((uint32_t)a.rows), dim3(64), st, a) != hipSuccess) return TT_ERR_HIP;
+  return TT_OK;
+}
+
+template <class T>
+int run_grad(GradArgs<T> a, hipStream_t st) {
+  const int64_t cols = grad_cols<T>();
+  a.chunks = (a.vocab + cols - 1) / cols;
+  if (a.rows > (int64_t)UINT32_MAX / SC_THREADS / a.chunks) return TT_ERR_TOO_LARGE;
+  return launch(scores_grad_kernel<T>, dim3((uint32_t)(a.rows * a.chunks)), dim3(SC_THREADS), st, a) == hipSuccess
+             ? TT_OK
+             : TT_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace tt
+
+using namespace tt;
+
+extern "C" int64_t tt_token_scores_workspace(int64_t rows, int64_t vocab, int32_t n_alt) {
+  if (rows < 0 || vocab < 1 || vocab > INT32_MAX || n_alt < 0 || n_alt > TT_MAX_ALTERNATIVES) return TT_ERR_BAD_ARG;
+  const int splits = scores_splits(rows, vocab);
+  return splits > 1 ? rows * splits * part_bytes(n_alt) : 0;
+}
+
+extern "C" int tt_token_scores(const void* logits, int32_t type, int64_t rows, int64_t vocab, int64_t stride, float scale,
+                               const int32_t* targets, float* logprobs, float* stats, float* entropy, int32_t n_alt,
+                               int32_t* alt_ids, float* alt_logprobs, void* workspace, int64_t workspace_bytes,
+                               void* stream) {
+  const int64_t need = tt_token_scores_workspace(rows, vocab, n_alt);
+  if (need < 0 || !score_type(type) || stride < vocab || !good_scale(scale) || workspace_bytes < need) return TT_ERR_BAD_ARG;
+  if (rows > (int64_t)UINT32_MAX / SC_THREADS) return TT_ERR_TOO_LARGE;
+  if (rows == 0) return TT_OK;
+  if (!logits || (need && !workspace) || (n_alt && (!alt_ids || !alt_logprobs))) return TT_ERR_NULL_ARG;
+  auto go = [&](auto zero) {
+    using T = decltype(zero);
+    return run_scores(ScoreArgs<T>{static_cast<const T*>(logits), rows, vocab, stride, scale, targets, logprobs, stats,
+                                   entropy, n_alt, alt_ids, alt_logprobs, static_cast<uint8_t*>(workspace),
+                                   scores_splits(rows, vocab)},
+                      static_cast<hipStream_t>(stream));
+  };
+  return type == TT_F32 ? go(float{}) : type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});
+}
+
+extern "C" int tt_token_scores_grad(const void* logits, int32_t type, int64_t rows, int64_t vocab, int64_t stride,
+                                    float scale, const int32_t* targets, const float* stats, const float* entropy,
+                                    const float* grad_logprobs, const float* grad_entropy, void* grad_logits,
+                                    int64_t grad_stride, void* stream) {
+  if (rows < 0 || vocab < 1 || vocab > INT32_MAX || !score_type(type) || stride < vocab || grad_stride < vocab ||
+      !good_scale(scale) || (grad_logits == logits && rows && grad_stride != stride))
+    return TT_ERR_BAD_ARG;
+  if (rows == 0) return TT_OK;
+  if (!logits || !grad_logits || !stats || (grad_entropy && !entropy)) return TT_ERR_NULL_ARG;
+  auto go = [&](auto zero) {
+    using T = decltype(zero);
+    return run_grad(GradArgs<T>{static_cast<const T*>(logits), static_cast<T*>(grad_logits), rows, vocab, stride,
+                                grad_stride, 0, scale, targets, stats, entropy, grad_logprobs, grad_entropy},
+                    static_cast<hipStream_t>(stream));
+  };
+  return type == TT_F32 ? go(float{}) : type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});
+}
