@@ -38,10 +38,37 @@ struct Operand {
 
 constexpr int BK = 64;  // entries of k that are staged at once: rows of 128 bytes in LDS
 
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// A buffer of 2 GiB from p on: what lies past it reads as 0.
+using Buffer = __attribute__((ext_vector_type(4))) uint32_t;
+constexpr uint32_t BUFFER_BYTES = 0x80000000u;
+__device__ __forceinline__ Buffer buffer_at(const void* p) {
+  const uint64_t at = (uint64_t)(uintptr_t)p;
+  return Buffer{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, BUFFER_BYTES, 0x00020000u};
+}
+// 16 bytes a lane from the buffer's byte `offset` to LDS, at `to` + 16 lane.
+// Written as assembly, since for the builtin the compiler makes every later
+// read of LDS wait for the load; there is no result register.  (m0 is the
+// compiler's to set before each use of its own; a write of it needs one wait
+// state before its use.)
+__device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
+}
+// Waits for all but the last N of this wave's loads and for its LDS reads, then
+// for the block's other waves.
+template <int N>
+__device__ __forceinline__ void loads_done_but() {
+  static_assert(N < 64, "field of s_waitcnt");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 template <class T, int BM_, int BN_, int WM_, int WN_, bool VEC_>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr bool VEC = VEC_;  // rows are aligned to 16 bytes and k is a multiple of 8
+  static constexpr bool DIRECT = VEC && BM == 256 && BN == 256;
   static constexpr int THREADS = 64 * WM * WN;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // 32 x 32 products of a wave
   using Elem = T;
@@ -69,8 +96,14 @@ struct Tile {
     return v;
   }
 
-  // acc += A[m0 ..][k0, k1) B[n0 ..][k0, k1); ends with every wave past its last read of sh
   static __device__ __forceinline__ void multiply(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
+                                                  int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
+    if constexpr (DIRECT) multiply_direct(a, b, m0, n0, k0, k1, sh, acc);
+    else multiply_staged(a, b, m0, n0, k0, k1, sh, acc);
+  }
+
+  // acc = A[m0 ..][k0, k1) B[n0 ..][k0, k1); ends with every wave past its last read of sh
+  static __device__ __forceinline__ void multiply_staged(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
                                                   int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int wm = wave / WN, wn = wave % WN;
@@ -131,6 +164,107 @@ struct Tile {
     }
   }
 
+  // The same for aligned operands, with the pieces loaded straight into LDS.
+  // The rows of a fragment for the next 16 entries of k are read while the
+  // matrix cores work on the last ones, across the change of stages too: the
+  // barrier stands before the last products of a stage, when its fragments are
+  // in registers, and the stage's buffer is then filled for the stage after the
+  // next.  Rows past an operand's last and entries past k1 are read as zeros;
+  // so are the two stages past the last, which keeps the loop free of branches.
+  static constexpr int WAVES = WM * WN, DA = BM / 8 / WAVES, DB = BN / 8 / WAVES;  // loads of 8 rows by a wave
+  static __device__ __forceinline__ void multiply_direct(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
+                                                         int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
+    static_assert(VEC && DA * WAVES * 8 == BM && DB * WAVES * 8 == BN, "whole loads");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    uint32_t oa[DA], ob[DB];  // byte offsets from the tile's first row
+    const int piece = (lane & 7) ^ (lane >> 3);  // (a load starts at a row that is a multiple of 8)
+#pragma unroll
+    for (int i = 0; i < DA; i++) {
+      const int64_t row = (wave * DA + i) * 8 + (lane >> 3);
+      oa[i] = m0 + row < a.rows ? (uint32_t)(row * a.stride + piece * 8) * 2 : BUFFER_BYTES;
+    }
+#pragma unroll
+    for (int i = 0; i < DB; i++) {
+      const int64_t row = (wave * DB + i) * 8 + (lane >> 3);
+      ob[i] = n0 + row < b.rows ? (uint32_t)(row * b.stride + piece * 8) * 2 : BUFFER_BYTES;
+    }
+    const T *pa = a.p + m0 * a.stride + k0, *pb = b.p + n0 * b.stride + k0;
+    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
+    const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
+    const int64_t mine = k1 - k0 - piece * 8;  // entries of k from this lane's piece on
+    const int stages_here = mine <= 0 ? 0 : (int)((mine + BK - 1) / BK);  // stages in which the lane has any
+    auto load_piece = [&](int stage, int i) {  // loads 0 .. DA + DB - 1 of a stage
+      const uint32_t at = stage & 1;
+      const bool real = stage < stages_here;
+      if (i < DA)
+        load_to_lds(buffer_at(pa + (int64_t)stage * BK), real ? oa[i < DA ? i : 0] : BUFFER_BYTES,
+                    la + at * (BM * BK * 2) + i * 1024);
+      else
+        load_to_lds(buffer_at(pb + (int64_t)stage * BK), real ? ob[i < DA ? 0 : i - DA] : BUFFER_BYTES,
+                    lb + at * (BN * BK * 2) + (i - DA) * 1024);
+    };
+    V8 fa[2][TM], fb[2][TN];
+    auto read = [&](int buf, int kk, int to) {
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+        fa[to][i] = *reinterpret_cast<const V8*>(&sh.a[buf][place(wm * TM * 32 + i * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+#pragma unroll
+      for (int j = 0; j < TN; j++)
+        fb[to][j] = *reinterpret_cast<const V8*>(&sh.b[buf][place(wn * TN * 32 + j * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+    };
+    auto one = [&](int from, int ij) {
+      const int i = ij / TN, j = ij % TN;
+      acc[i][j] = Mfma<T>::mul(fa[from][i], fb[from][j], acc[i][j]);
+    };
+#pragma unroll
+    for (int i = 0; i < DA + DB; i++) load_piece(0, i);
+#pragma unroll
+    for (int i = 0; i < DA + DB; i++) load_piece(1, i);
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+      for (int j = 0; j < TN; j++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+    loads_done_but<DA + DB>();
+    read(0, 0, 0);
+    const int steps = (int)((k1 - k0 + BK - 1) / BK);
+    int s = 0;
+    do {
+#pragma unroll
+      for (int kk = 0; kk < BK / 16 - 1; kk++) {
+        read(s & 1, kk + 1, (kk + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ij = 0; ij < TM * TN; ij++) one(kk & 1, ij);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      loads_done_but<0>();
+      read((s + 1) & 1, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ij = 0; ij < TM * TN; ij++) {  // the loads are issued between the products
+        one(1, ij);
+#pragma unroll
+        for (int i = ij * (DA + DB) / (TM * TN); i < (ij + 1) * (DA + DB) / (TM * TN); i++) load_piece(s + 2, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } while (++s < steps);
+    loads_done_but<0>();
+    // (what reads the accumulators by assembly has to wait for the last products itself)
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+  }
+
+  // One value of an accumulator, out of an accumulation register where the
+  // accumulators fill those: they stay there until each is used.
+  static __device__ __forceinline__ float value(const f32x16 (&acc)[TM][TN], int i, int j, int r) {
+    if (!DIRECT) return acc[i][j][r];
+    float x;
+    asm("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[i][j][r]));
+    return x;
+  }
+
   // Where accumulator r of product (i, j) lies: row m (four consecutive rows for
   // r = 4 g .. 4 g + 3) and column n of the tile.
   static __device__ __forceinline__ int row_of(int i, int group) {
@@ -151,6 +285,15 @@ __device__ __forceinline__ uint32_t die_order(uint32_t b, uint32_t n) {
   return die * per + (die < rest ? die : rest) + i;
 }
 
+// (m tile, n tile) of the id-th tile: groups of eight n tiles, all m tiles of a
+// group before the next, so that tiles that run together share rows of both.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t m_tiles, uint32_t n_tiles, int64_t& mt, int64_t& nt) {
+  const uint32_t group = id / (m_tiles * 8), first = group * 8, width = n_tiles - first < 8 ? n_tiles - first : 8;
+  const uint32_t in = id - group * m_tiles * 8;
+  mt = in / width;
+  nt = first + in % width;
+}
+
 // ---- forward ---------------------------------------------------------------
 
 struct Part {
@@ -169,48 +312,75 @@ struct HeadArgs {
 };
 
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS) void head_scores_kernel(HeadArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void head_scores_kernel(HeadArgs<typename Tl::Elem> a) {
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x);
-  const uint32_t mt = tile / (uint32_t)a.n_tiles, nt = tile % (uint32_t)a.n_tiles;
-  const int64_t m0 = (int64_t)mt * Tl::BM, n0 = (int64_t)nt * Tl::BN;
+  int64_t mt, nt;
+  tile_of(tile, (uint32_t)a.m_tiles, (uint32_t)a.n_tiles, mt, nt);
+  const int64_t m0 = mt * Tl::BM, n0 = nt * Tl::BN;
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
 
   const float c = a.scale * LOG2E;
   const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / Tl::WN;
   Part* joined = reinterpret_cast<Part*>(&sh);  // [WM][BN]
-  const int64_t vocab = a.weight.rows, rows = a.hidden.rows;
+  const int64_t rows = a.hidden.rows;
+  const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;  // entries of this tile
+  auto columns = [&](auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-  for (int j = 0; j < Tl::TN; j++) {
-    const int col = Tl::col_of(j);
-    const int64_t t = n0 + col;
-    const int64_t target = a.targets && t < rows ? a.targets[t] : -1;
-    float m = NEG_INF;
-#pragma unroll
-    for (int i = 0; i < Tl::TM; i++)
-#pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const int64_t v = m0 + Tl::row_of(i, r >> 2) + (r & 3);
-        if (v >= vocab) acc[i][j][r] = NEG_INF;
-        else if (v == target) a.given[t] = acc[i][j][r];
-        m = fmaxf(m, acc[i][j][r]);
+    for (int j = 0; j < Tl::TN; j++) {
+      const int col = Tl::col_of(j);
+      const int64_t t = n0 + col;
+      // an entry's place is 32 i + 8 (r / 4) + r % 4 from the lane's first one
+      int last = left - Tl::row_of(0, 0), given = -1;
+      if (a.targets && t < rows) {
+        const int64_t g = a.targets[t] - m0;
+        if (g >= 0 && g < left) given = (int)g - Tl::row_of(0, 0);
       }
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float ref = reference(m);
-    Stats st = {m, 0.f, 0.f};
+      auto entry = [&](int i, int r) {
+        const float x = Tl::value(acc, i, j, r);
+        return WHOLE || 32 * i + 8 * (r >> 2) + (r & 3) < last ? x : NEG_INF;
+      };
+      // (opaque, so that the comparisons of all entries are not made ahead and kept)
+      if (!WHOLE) asm volatile("" : "+v"(last));
+      float m = NEG_INF;
 #pragma unroll
-    for (int i = 0; i < Tl::TM; i++)
+      for (int i = 0; i < Tl::TM; i++)
 #pragma unroll
-      for (int r = 0; r < 16; r++) {
-        const float d = (acc[i][j][r] - ref) * c, e = __builtin_amdgcn_exp2f(d);
-        st.s += e;
-        st.u += weigh(e, d);
+        for (int r = 0; r < 16; r++) m = fmaxf(m, entry(i, r));
+      __builtin_amdgcn_sched_barrier(0);
+      const bool mine = given >= 0 && given < Tl::TM * 32 && !(given & 4);
+      if (__ballot(mine)) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < Tl::TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (32 * i + 8 * (r >> 2) + (r & 3) == given) x = Tl::value(acc, i, j, r);
+        if (mine) a.given[t] = x;
       }
-    st.s += __shfl_xor(st.s, 32);
-    st.u += __shfl_xor(st.u, 32);
-    if (lane < 32) joined[wm * Tl::BN + col] = {st.m, st.s, st.u, 0.f};
-  }
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float ref = reference(m);
+      float s0 = 0.f, u0 = 0.f;
+      if (!WHOLE) asm volatile("" : "+v"(last));
+#pragma unroll
+      for (int i = 0; i < Tl::TM; i++) {
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          const float d = (entry(i, r) - ref) * c, e = __builtin_amdgcn_exp2f(d);
+          s0 += e;
+          u0 += weigh(e, d);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (the accumulators do not fit the other registers all at once)
+      }
+      s0 += __shfl_xor(s0, 32);
+      u0 += __shfl_xor(u0, 32);
+      if (lane < 32) joined[wm * Tl::BN + col] = {m, s0, u0, 0.f};
+    }
+  };
+  if (left == Tl::BM) columns(std::true_type{});
+  else columns(std::false_type{});
   __syncthreads();
   for (int col = threadIdx.x; col < Tl::BN; col += Tl::THREADS) {
     if (n0 + col >= rows) break;
@@ -306,18 +476,19 @@ struct GradLogitsArgs {
   T* g;    // [padded rows][g_stride] or NULL
   T* gt;   // [piece][gt_stride] or NULL
   int64_t g_stride, gt_stride;
-  int32_t n_tiles;
+  int32_t m_tiles, n_tiles;
 };
 
 // G and its transpose, zero past the last row and the piece's last entry.
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS) void grad_logits_kernel(GradLogitsArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void grad_logits_kernel(GradLogitsArgs<typename Tl::Elem> a) {
   using T = typename Tl::Elem;
   using T4 = __attribute__((ext_vector_type(4))) T;
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x);
-  const uint32_t mt = tile / (uint32_t)a.n_tiles, nt = tile % (uint32_t)a.n_tiles;
-  const int64_t m0 = (int64_t)mt * Tl::BM, n0 = (int64_t)nt * Tl::BN;
+  int64_t mt, nt;
+  tile_of(tile, (uint32_t)a.m_tiles, (uint32_t)a.n_tiles, mt, nt);
+  const int64_t m0 = mt * Tl::BM, n0 = nt * Tl::BN;
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
   const float c = a.scale * LOG2E, factor = a.factor ? a.factor[0] : 1.f;
@@ -329,6 +500,7 @@ __global__ __launch_bounds__(Tl::THREADS) void grad_logits_kernel(GradLogitsArgs
     if (t < a.hidden.rows)
       g = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, t, a.vocab, a.scale);
     const int64_t given = g.target - a.first;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < Tl::TM; i++)
 #pragma unroll
@@ -339,7 +511,7 @@ __global__ __launch_bounds__(Tl::THREADS) void grad_logits_kernel(GradLogitsArgs
         for (int r = 0; r < 4; r++) {
           float y = 0.f;
           if (!g.zero && v + r < a.weight.rows) {
-            y = grad_of(acc[i][j][4 * q + r], c, g);
+            y = grad_of(Tl::value(acc, i, j, 4 * q + r), c, g);
             if (v + r == given) y += g.g;
           }
           out[r] = (T)(y * factor);
@@ -368,56 +540,63 @@ struct ProductArgs {
 
 // out[n][m] = sum_k A[m][k] B[n][k]
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS) void product_kernel(ProductArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void product_kernel(ProductArgs<typename Tl::Elem> a) {
   using T = typename Tl::Elem;
   using T4 = __attribute__((ext_vector_type(4))) T;
   using F4 = __attribute__((ext_vector_type(4))) float;
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x), tiles = (uint32_t)(a.m_tiles * a.n_tiles);
-  const uint32_t part = tile / tiles, nt = tile % tiles / (uint32_t)a.m_tiles, mt = tile % (uint32_t)a.m_tiles;
-  const int64_t m0 = (int64_t)mt * Tl::BM, n0 = (int64_t)nt * Tl::BN;
+  const uint32_t part = tile / tiles;
+  int64_t mt, nt;
+  tile_of(tile % tiles, (uint32_t)a.m_tiles, (uint32_t)a.n_tiles, mt, nt);
+  const int64_t m0 = mt * Tl::BM, n0 = nt * Tl::BN;
   const int64_t k0 = part * a.k_part, k1 = k0 + a.k_part < a.k ? k0 + a.k_part : a.k;
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.a, a.b, m0, n0, k0, k1, sh, acc);
   const float factor = a.factor ? a.factor[1] : 1.f;
+  const int left = a.a.rows - m0 < Tl::BM ? (int)(a.a.rows - m0) : Tl::BM;
+  // whole groups of four entries, aligned to their size, or entry by entry
+  const bool fours = a.a.rows % 4 == 0 && (a.out ? a.out_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 : true);
+  auto put = [&](auto whole) {
 #pragma unroll
-  for (int j = 0; j < Tl::TN; j++) {
-    const int64_t n = n0 + Tl::col_of(j);
-    if (n >= a.b.rows) continue;
+    for (int j = 0; j < Tl::TN; j++) {
+      const int64_t n = n0 + Tl::col_of(j);
+      if (n >= a.b.rows) continue;
+      T* out = a.out + n * a.out_stride + m0;
+      float* sums = a.sums + ((int64_t)part * a.b.rows + n) * a.a.rows + m0;
 #pragma unroll
-    for (int i = 0; i < Tl::TM; i++)
+      for (int i = 0; i < Tl::TM; i++)
 #pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int64_t m = m0 + Tl::row_of(i, q);
-        if (m >= a.a.rows) continue;
-        if (a.out) {
-          T* p = a.out + n * a.out_stride + m;
-          T4 y;
-#pragma unroll
-          for (int r = 0; r < 4; r++) y[r] = (T)(acc[i][j][4 * q + r] * factor);
-          if (m + 3 < a.a.rows && (reinterpret_cast<uintptr_t>(p) & 7) == 0) {
-            *reinterpret_cast<T4*>(p) = y;
-          } else {
-#pragma unroll
-            for (int r = 0; r < 4; r++)
-              if (m + r < a.a.rows) p[r] = y[r];
-          }
-        } else {
-          float* p = a.sums + ((int64_t)part * a.b.rows + n) * a.a.rows + m;
+        for (int q = 0; q < 4; q++) {
+          const int m = Tl::row_of(i, q);
+          if (m >= left) continue;
           F4 y;
+          T4 z;
 #pragma unroll
-          for (int r = 0; r < 4; r++) y[r] = acc[i][j][4 * q + r];
-          if (m + 3 < a.a.rows && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-            if (a.add) y += *reinterpret_cast<F4*>(p);
-            *reinterpret_cast<F4*>(p) = y;
+          for (int r = 0; r < 4; r++) {
+            y[r] = Tl::value(acc, i, j, 4 * q + r);
+            z[r] = (T)(y[r] * factor);
+          }
+          if (decltype(whole)::value) {
+            if (a.out) {
+              *reinterpret_cast<T4*>(out + m) = z;
+            } else {
+              if (a.add) y += *reinterpret_cast<F4*>(sums + m);
+              *reinterpret_cast<F4*>(sums + m) = y;
+            }
           } else {
-#pragma unroll
+#pragma unroll 1
             for (int r = 0; r < 4; r++)
-              if (m + r < a.a.rows) p[r] = a.add ? p[r] + y[r] : y[r];
+              if (m + r < left) {
+                if (a.out) out[m + r] = z[r];
+                else sums[m + r] = a.add ? sums[m + r] + y[r] : y[r];
+              }
           }
         }
-      }
-  }
+    }
+  };
+  if (fours) put(std::true_type{});
+  else put(std::false_type{});
 }
 
 // out[row][col] = factor * the sum of the parts
@@ -447,7 +626,8 @@ bool head_sizes(int64_t rows, int64_t vocab, int64_t width) {
 
 template <class T>
 bool vectors(const Operand<T>& o, int64_t k) {
-  return k % 8 == 0 && o.stride % 8 == 0 && reinterpret_cast<uintptr_t>(o.p) % 16 == 0;
+  return k % 8 == 0 && o.stride % 8 == 0 && reinterpret_cast<uintptr_t>(o.p) % 16 == 0 &&
+         o.stride <= ((int64_t)BUFFER_BYTES / 2 - 64) / 256;  // the tile's rows in one buffer
 }
 
 template <class Tl>
@@ -465,7 +645,7 @@ int forward_by_rows(const HeadArgs<T>& a, hipStream_t st) {
   if (rows <= 32) return run_forward<Tile<T, 128, 32, 4, 1, VEC>>(a, st);
   if (rows <= 64) return run_forward<Tile<T, 128, 64, 4, 1, VEC>>(a, st);
   if (rows <= 128) return run_forward<Tile<T, 256, 128, 4, 2, VEC>>(a, st);
-  return run_forward<Tile<T, 256, 256, 4, 2, VEC>>(a, st);
+  return run_forward<Tile<T, 256, 256, VEC ? 2 : 4, 2, VEC>>(a, st);
 }
 
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
@@ -520,8 +700,9 @@ hipError_t transpose(const Operand<T>& in, int64_t cols, T* out, int64_t padded,
 
 template <class Tl>
 hipError_t grad_logits(GradLogitsArgs<typename Tl::Elem> a, hipStream_t st) {
+  a.m_tiles = (int32_t)div_up(a.weight.rows, Tl::BM);
   a.n_tiles = (int32_t)div_up(a.hidden.rows, Tl::BN);
-  return launch(grad_logits_kernel<Tl>, dim3((uint32_t)(div_up(a.weight.rows, Tl::BM) * a.n_tiles)), dim3(Tl::THREADS), st, a);
+  return launch(grad_logits_kernel<Tl>, dim3((uint32_t)((int64_t)a.m_tiles * a.n_tiles)), dim3(Tl::THREADS), st, a);
 }
 
 template <class Tl>
@@ -536,7 +717,7 @@ template <class T>
 int run_gradients(const GradCall<T>& c, hipStream_t st) {
   const int64_t rows = c.hidden.rows, vocab = c.weight.rows;
   if (rows == 0) {  // grad_weight is the empty sum
-    using Whole = Tile<T, 256, 256, 4, 2, true>;
+    using Whole = Tile<T, 256, 256, 2, 2, true>;
     const ProductArgs<T> pa{{c.hidden.p, 0, c.width}, {c.hidden.p, 0, vocab}, 0, 1, 0, 0, nullptr, c.grad_weight,
                             c.grad_weight_stride, nullptr, false};
     return !c.grad_weight || product<Whole>(pa, st) == hipSuccess ? TT_OK : TT_ERR_HIP;
@@ -562,10 +743,10 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     const Operand<T> weight{c.weight.p + first * c.weight.stride, c.weight.stride, n};
     const GradLogitsArgs<T> ga{weight,  c.hidden,        c.width,        first, vocab,    c.scale, c.targets, c.stats,
                                c.entropy, c.grad_logprobs, c.grad_entropy, factor,
-                               c.grad_hidden ? g : nullptr, c.grad_weight ? gt : nullptr, n_padded, p.padded, 0};
-    if (bad(vec ? grad_logits<Tile<T, 256, 256, 4, 2, true>>(ga, st) : grad_logits<Tile<T, 256, 256, 4, 2, false>>(ga, st)))
+                               c.grad_hidden ? g : nullptr, c.grad_weight ? gt : nullptr, n_padded, p.padded, 0, 0};
+    if (bad(vec ? grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st) : grad_logits<Tile<T, 256, 256, 4, 2, false>>(ga, st)))
       return TT_ERR_HIP;
-    using Whole = Tile<T, 256, 256, 4, 2, true>;
+    using Whole = Tile<T, 256, 256, 2, 2, true>;
     if (c.grad_weight) {
       const ProductArgs<T> pa{{hidden_t, p.padded, c.width}, {gt, p.padded, n}, p.padded, p.padded, 0, 0, factor,
                               c.grad_weight + first * c.grad_weight_stride, c.grad_weight_stride, nullptr, false};
