@@ -1,10 +1,12 @@
 // tt_head_scores and its gradients: scores of logits = hidden weight^T that are
 // never stored, on the matrix cores.
 //
-// Every product here is C[m][n] = sum_k A[m][k] B[n][k] with both operands
-// contiguous in k, in tiles of BM x BN that eight (or four) waves share.  m runs
-// over the vocabulary in the scores, so a lane's accumulators hold entries of
-// one token's row and the softmax statistics are sums within the lane.
+// Every product here is C[m][n] = sum_k A[m][k] B[n][k] in tiles of BM x BN that
+// four (or eight) waves share.  m runs over the vocabulary in the scores, so a
+// lane's accumulators hold entries of one token's row and the softmax statistics
+// are sums within the lane.  The gradients take the gradient of the logits G as
+// it stands and hidden or weight as it stands: an operand may be contiguous in k
+// or in m (or n), and LDS transposes the latter on the way to the registers.
 #include "tt_scores.h"
 
 namespace tt {
@@ -17,6 +19,7 @@ struct Mfma;
 template <>
 struct Mfma<bf16_t> {
   using V8 = __attribute__((ext_vector_type(8))) bf16_t;
+  using V4 = __attribute__((ext_vector_type(4))) bf16_t;
   static __device__ __forceinline__ f32x16 mul(V8 a, V8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -24,12 +27,13 @@ struct Mfma<bf16_t> {
 template <>
 struct Mfma<f16_t> {
   using V8 = __attribute__((ext_vector_type(8))) f16_t;
+  using V4 = __attribute__((ext_vector_type(4))) f16_t;
   static __device__ __forceinline__ f32x16 mul(V8 a, V8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
 };
 
-// An operand: rows of k entries.
+// An operand: `rows` rows of k entries, or (by columns) k rows of `rows` entries.
 template <class T>
 struct Operand {
   const T* p;
@@ -64,7 +68,16 @@ __device__ __forceinline__ void loads_done_but() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_, bool VEC_>
+// Four entries of one column each lane: within 16 lanes, lane l reads four
+// entries of row l / 4 and receives column l of the 4 x 16 block.
+template <class V4>
+__device__ __forceinline__ V4 read_transposed(const void* p) {
+  using S4 = __attribute__((ext_vector_type(4))) short;
+  return __builtin_bit_cast(V4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4*)p));
+}
+
+// AC, BC: the operand is contiguous in m (n) instead of in k
+template <class T, int BM_, int BN_, int WM_, int WN_, bool VEC_, bool AC = false, bool BC = false>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr bool VEC = VEC_;  // rows are aligned to 16 bytes and k is a multiple of 8
@@ -73,6 +86,7 @@ struct Tile {
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // 32 x 32 products of a wave
   using Elem = T;
   using V8 = typename Mfma<T>::V8;
+  using V4 = typename Mfma<T>::V4;
   static constexpr int NA = BM * 8 / THREADS, NB = BN * 8 / THREADS;  // 16-byte pieces a thread stages
   static_assert(NA * THREADS == BM * 8 && NB * THREADS == BN * 8, "whole pieces");
   struct Shared {
@@ -83,6 +97,11 @@ struct Tile {
   // of a row are permuted by the row's low bits, so that the 32 rows that a wave
   // reads at one k lie in different banks.
   static __device__ __forceinline__ int place(int row, int piece) { return row * BK + ((piece ^ (row & 7)) << 3); }
+
+  // An operand by columns is staged as 64 rows of 256 entries; blocks of 32
+  // entries are permuted by this, so that the eight half rows that a wave reads
+  // at a time lie in different banks.
+  static __device__ __forceinline__ int spread(int row) { return (row & 3) | (row >> 1 & 4); }
 
   static __device__ __forceinline__ V8 load(const Operand<T>& o, int64_t row, int64_t k, int64_t k_end) {
     V8 v = {};
@@ -174,44 +193,73 @@ struct Tile {
   static constexpr int WAVES = WM * WN, DA = BM / 8 / WAVES, DB = BN / 8 / WAVES;  // loads of 8 rows by a wave
   static __device__ __forceinline__ void multiply_direct(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
                                                          int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
-    static_assert(VEC && DA * WAVES * 8 == BM && DB * WAVES * 8 == BN, "whole loads");
+    static_assert(VEC && DA * WAVES * 8 == BM && DB * WAVES * 8 == BN && (!AC || BM == 256) && (!BC || BN == 256), "whole loads");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    uint32_t oa[DA], ob[DB];  // byte offsets from the tile's first row
-    const int piece = (lane & 7) ^ (lane >> 3);  // (a load starts at a row that is a multiple of 8)
+    // Byte offsets of this lane's pieces from the tile's first entry, and the
+    // entries of k that a piece has left at stage 0.
+    uint32_t oa[DA], ob[DB];
+    auto offset = [&](const Operand<T>& o, int64_t first, int load, auto by_columns) {
+      if (decltype(by_columns)::value) {  // two rows of 256 entries
+        const int64_t row = load * 2 + (lane >> 5), col = ((((lane & 31) >> 2) ^ spread((int)row)) << 5) + (lane & 3) * 8;
+        return first + col < o.rows ? (uint32_t)(row * o.stride + col) * 2 : BUFFER_BYTES;
+      }
+      const int64_t row = load * 8 + (lane >> 3);  // eight rows of 64 entries
+      return first + row < o.rows ? (uint32_t)(row * o.stride + ((lane & 7) ^ (lane >> 3)) * 8) * 2 : BUFFER_BYTES;
+    };
+    auto stages_of = [&](int load, auto by_columns) {
+      const int64_t left = k1 - k0 - (decltype(by_columns)::value ? load * 2 + (lane >> 5) : ((lane & 7) ^ (lane >> 3)) * 8);
+      return left <= 0 ? 0 : (int)((left + BK - 1) / BK);  // stages in which the piece lies before k1
+    };
+    using A = std::integral_constant<bool, AC>;
+    using B = std::integral_constant<bool, BC>;
 #pragma unroll
-    for (int i = 0; i < DA; i++) {
-      const int64_t row = (wave * DA + i) * 8 + (lane >> 3);
-      oa[i] = m0 + row < a.rows ? (uint32_t)(row * a.stride + piece * 8) * 2 : BUFFER_BYTES;
-    }
+    for (int i = 0; i < DA; i++) oa[i] = offset(a, m0, wave * DA + i, A{});
 #pragma unroll
-    for (int i = 0; i < DB; i++) {
-      const int64_t row = (wave * DB + i) * 8 + (lane >> 3);
-      ob[i] = n0 + row < b.rows ? (uint32_t)(row * b.stride + piece * 8) * 2 : BUFFER_BYTES;
-    }
-    const T *pa = a.p + m0 * a.stride + k0, *pb = b.p + n0 * b.stride + k0;
+    for (int i = 0; i < DB; i++) ob[i] = offset(b, n0, wave * DB + i, B{});
+    const T* pa = AC ? a.p + k0 * a.stride + m0 : a.p + m0 * a.stride + k0;
+    const T* pb = BC ? b.p + k0 * b.stride + n0 : b.p + n0 * b.stride + k0;
+    const int64_t next_a = AC ? BK * a.stride : BK, next_b = BC ? BK * b.stride : BK;
     const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
     const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
-    const int64_t mine = k1 - k0 - piece * 8;  // entries of k from this lane's piece on
-    const int stages_here = mine <= 0 ? 0 : (int)((mine + BK - 1) / BK);  // stages in which the lane has any
+    // (rows of k: all but the last few stages hold all of a wave's rows)
+    const int stages_a = stages_of(wave * DA, A{}), stages_b = stages_of(wave * DB, B{});
+    const int full_stages = (int)((k1 - k0) / BK), rows_left = (int)((k1 - k0) % BK);
     auto load_piece = [&](int stage, int i) {  // loads 0 .. DA + DB - 1 of a stage
       const uint32_t at = stage & 1;
-      const bool real = stage < stages_here;
+      auto real = [&](int load, int stages, auto by_columns) {
+        if (!decltype(by_columns)::value) return stage < stages;
+        const int row = load * 2 + (lane >> 5);
+        return stage < full_stages || (stage == full_stages && row < rows_left);
+      };
       if (i < DA)
-        load_to_lds(buffer_at(pa + (int64_t)stage * BK), real ? oa[i < DA ? i : 0] : BUFFER_BYTES,
+        load_to_lds(buffer_at(pa + stage * next_a), real(wave * DA + i, stages_a, A{}) ? oa[i < DA ? i : 0] : BUFFER_BYTES,
                     la + at * (BM * BK * 2) + i * 1024);
       else
-        load_to_lds(buffer_at(pb + (int64_t)stage * BK), real ? ob[i < DA ? 0 : i - DA] : BUFFER_BYTES,
+        load_to_lds(buffer_at(pb + stage * next_b),
+                    real(wave * DB + i - DA, stages_b, B{}) ? ob[i < DA ? 0 : i - DA] : BUFFER_BYTES,
                     lb + at * (BN * BK * 2) + (i - DA) * 1024);
     };
     V8 fa[2][TM], fb[2][TN];
-    auto read = [&](int buf, int kk, int to) {
-#pragma unroll
-      for (int i = 0; i < TM; i++)
-        fa[to][i] = *reinterpret_cast<const V8*>(&sh.a[buf][place(wm * TM * 32 + i * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
-#pragma unroll
-      for (int j = 0; j < TN; j++)
-        fb[to][j] = *reinterpret_cast<const V8*>(&sh.b[buf][place(wn * TN * 32 + j * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+    // fragment of rows (columns) 32 i .. 32 i + 31 from `first` on, 16 entries of k from 16 kk on
+    auto fragment = [&](const T* p, int first, int kk, auto by_columns) {
+      if (decltype(by_columns)::value) {
+        const int row = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
+        const T* q = p + row * 256 + ((((first >> 5) ^ spread(row)) << 5) | ((lane >> 4 & 1) << 4) | ((lane & 3) << 2));
+        const V4 x = read_transposed<V4>(q), y = read_transposed<V4>(q + 4 * 256);
+        return (V8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+      return *reinterpret_cast<const V8*>(&p[place(first + (lane & 31), kk * 2 + (lane >> 5))]);
+    };
+    // fragment n of the next products, in the order in which those need them
+    constexpr int FRAGMENTS = TM + TN;
+    auto read_one = [&](int buf, int kk, int to, int n) {
+      if (n == 0 || n > TN) {
+        const int i = n == 0 ? 0 : n - TN;
+        fa[to][i] = fragment(sh.a[buf], wm * TM * 32 + i * 32, kk, A{});
+      } else {
+        fb[to][n - 1] = fragment(sh.b[buf], wn * TN * 32 + (n - 1) * 32, kk, B{});
+      }
     };
     auto one = [&](int from, int ij) {
       const int i = ij / TN, j = ij % TN;
@@ -228,27 +276,30 @@ struct Tile {
 #pragma unroll
         for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
     loads_done_but<DA + DB>();
-    read(0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < FRAGMENTS; n++) read_one(0, 0, 0, n);
     const int steps = (int)((k1 - k0 + BK - 1) / BK);
     int s = 0;
+    // Reads and loads are issued between the products: a wave issues in order,
+    // and a row of reads would leave its matrix core idle until LDS took them.
+    constexpr int P = TM * TN;
     do {
 #pragma unroll
-      for (int kk = 0; kk < BK / 16 - 1; kk++) {
-        read(s & 1, kk + 1, (kk + 1) & 1);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int kk = 0; kk < BK / 16; kk++) {
+        const bool last = kk == BK / 16 - 1;
+        if (last) loads_done_but<0>();
 #pragma unroll
-        for (int ij = 0; ij < TM * TN; ij++) one(kk & 1, ij);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      loads_done_but<0>();
-      read((s + 1) & 1, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int ij = 0; ij < P; ij++) {
+          one(kk & 1, ij);
 #pragma unroll
-      for (int ij = 0; ij < TM * TN; ij++) {  // the loads are issued between the products
-        one(1, ij);
+          for (int n = ij * FRAGMENTS / P; n < (ij + 1) * FRAGMENTS / P; n++)
+            read_one((last ? s + 1 : s) & 1, last ? 0 : kk + 1, (kk + 1) & 1, n);
+          if (last) {
 #pragma unroll
-        for (int i = ij * (DA + DB) / (TM * TN); i < (ij + 1) * (DA + DB) / (TM * TN); i++) load_piece(s + 2, i);
-        __builtin_amdgcn_sched_barrier(0);
+            for (int i = ij * (DA + DB) / P; i < (ij + 1) * (DA + DB) / P; i++) load_piece(s + 2, i);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     } while (++s < steps);
     loads_done_but<0>();
@@ -318,13 +369,19 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::T
   int64_t mt, nt;
   tile_of(tile, (uint32_t)a.m_tiles, (uint32_t)a.n_tiles, mt, nt);
   const int64_t m0 = mt * Tl::BM, n0 = nt * Tl::BN;
+  const int64_t rows = a.hidden.rows;
+  int targets[Tl::TN];  // (loaded ahead of the products)
+#pragma unroll
+  for (int j = 0; j < Tl::TN; j++) {
+    const int64_t t = n0 + Tl::col_of(j);
+    targets[j] = a.targets && t < rows ? a.targets[t] : -1;
+  }
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
 
   const float c = a.scale * LOG2E;
   const int lane = threadIdx.x & 63, wm = (threadIdx.x >> 6) / Tl::WN;
   Part* joined = reinterpret_cast<Part*>(&sh);  // [WM][BN]
-  const int64_t rows = a.hidden.rows;
   const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;  // entries of this tile
   auto columns = [&](auto whole) {
     constexpr bool WHOLE = decltype(whole)::value;
@@ -333,11 +390,9 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::T
       const int col = Tl::col_of(j);
       const int64_t t = n0 + col;
       // an entry's place is 32 i + 8 (r / 4) + r % 4 from the lane's first one
-      int last = left - Tl::row_of(0, 0), given = -1;
-      if (a.targets && t < rows) {
-        const int64_t g = a.targets[t] - m0;
-        if (g >= 0 && g < left) given = (int)g - Tl::row_of(0, 0);
-      }
+      int last = left - Tl::row_of(0, 0);
+      const int64_t in_tile = targets[j] - m0;
+      const int given = targets[j] >= 0 && in_tile >= 0 && in_tile < left ? (int)in_tile - Tl::row_of(0, 0) : -1;
       auto entry = [&](int i, int r) {
         const float x = Tl::value(acc, i, j, r);
         return WHOLE || 32 * i + 8 * (r >> 2) + (r & 3) < last ? x : NEG_INF;
@@ -449,20 +504,13 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, float mos
   out[1] = ldexpf(1.f, -e);
 }
 
-// out[c][r] = in[r][c] for r < rows, 0 for rows <= r < padded; 64 x 64 tiles.
+// Copies rows of any alignment into aligned ones with zeros behind them.
 template <class T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* in, int64_t stride, int64_t rows, int64_t cols, T* out,
-                                                        int64_t padded) {
-  __shared__ T tile[64][66];
-  const int64_t tiles_r = padded / 64;
-  const int64_t r0 = (blockIdx.x % tiles_r) * 64, c0 = (blockIdx.x / tiles_r) * 64;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll 4
-  for (int i = y; i < 64; i += 4) tile[i][x] = r0 + i < rows && c0 + x < cols ? in[(r0 + i) * stride + c0 + x] : (T)0.f;
-  __syncthreads();
-#pragma unroll 4
-  for (int i = y; i < 64; i += 4)
-    if (c0 + i < cols) out[(c0 + i) * padded + r0 + x] = tile[x][i];
+__global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < in.rows * stride; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / stride, col = i - row * stride;
+    out[i] = col < width ? in.p[row * in.stride + col] : (T)0.f;
+  }
 }
 
 template <class T>
@@ -473,57 +521,99 @@ struct GradLogitsArgs {
   const int32_t* targets;
   const float *stats, *entropy, *grad_logprobs, *grad_entropy;
   const float* factor;  // NULL: 1
-  T* g;    // [padded rows][g_stride] or NULL
-  T* gt;   // [piece][gt_stride] or NULL
-  int64_t g_stride, gt_stride;
+  T* g;                 // [g_rows][g_stride], both multiples of 64
+  int64_t g_stride, g_rows;
   int32_t m_tiles, n_tiles;
 };
 
-// G and its transpose, zero past the last row and the piece's last entry.
+// A wave's share of a tile, rounded, through LDS: n runs over its TN * 32 rows,
+// each of TM * 32 entries, so that 16 lanes store a row's 256 bytes.  The wave's
+// part of LDS is its own; 16-byte pieces of a row are permuted against bank
+// conflicts.
+template <class Tl, class V4>
+__device__ __forceinline__ void keep_four(typename Tl::Shared& sh, int i, int j, int q, V4 x) {
+  static_assert(Tl::TM == 4 && Tl::TN == 4, "rows of 256 bytes");
+  const int lane = threadIdx.x & 63, row = j * 32 + (lane & 31);
+  char* p = reinterpret_cast<char*>(&sh) + (threadIdx.x >> 6) * 32768 + row * 256;
+  *reinterpret_cast<V4*>(p + (((i * 4 + q) ^ (row & 15)) << 4) + (lane >> 5) * 8) = x;
+}
+// put(row, first entry, 8 entries) for every row of the wave's share
+template <class Tl, class F>
+__device__ __forceinline__ void for_rows(typename Tl::Shared& sh, F put) {
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / Tl::WN, wn = wave % Tl::WN;
+  const char* p = reinterpret_cast<const char*>(&sh) + wave * 32768;
+#pragma unroll 8
+  for (int k = 0; k < 32; k++) {
+    const int row = k * 4 + (lane >> 4), piece = lane & 15;
+    const auto x = *reinterpret_cast<const typename Tl::V8*>(p + row * 256 + ((piece ^ (row & 15)) << 4));
+    put(wn * 128 + row, wm * 128 + piece * 8, x);
+  }
+}
+
+// G, zero past the last row and the piece's last entry.
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void grad_logits_kernel(GradLogitsArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsArgs<typename Tl::Elem> a) {
   using T = typename Tl::Elem;
-  using T4 = __attribute__((ext_vector_type(4))) T;
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x);
   int64_t mt, nt;
   tile_of(tile, (uint32_t)a.m_tiles, (uint32_t)a.n_tiles, mt, nt);
   const int64_t m0 = mt * Tl::BM, n0 = nt * Tl::BN;
-  f32x16 acc[Tl::TM][Tl::TN];
-  Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
-  const float c = a.scale * LOG2E, factor = a.factor ? a.factor[0] : 1.f;
+  RowGrad grads[Tl::TN];  // (loaded ahead of the products)
 #pragma unroll
   for (int j = 0; j < Tl::TN; j++) {
     const int64_t t = n0 + Tl::col_of(j);
-    RowGrad g = {};
-    g.zero = true;
+    grads[j] = {};
+    grads[j].zero = true;
+    grads[j].target = -1;
     if (t < a.hidden.rows)
-      g = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, t, a.vocab, a.scale);
-    const int64_t given = g.target - a.first;
-    __builtin_amdgcn_sched_barrier(0);
+      grads[j] = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, t, a.vocab, a.scale);
+  }
+  const float c = a.scale * LOG2E, factor = a.factor ? a.factor[0] : 1.f;
+  f32x16 acc[Tl::TM][Tl::TN];
+  Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
+  const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;
+  auto columns = [&](auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-    for (int i = 0; i < Tl::TM; i++)
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int64_t v = m0 + Tl::row_of(i, q);
-        T4 out;
+    for (int j = 0; j < Tl::TN; j++) {
+      const RowGrad& g = grads[j];
+      // an entry's place is 32 i + 8 (r / 4) + r % 4 from the lane's first one
+      const int64_t at = g.target - a.first - m0 - Tl::row_of(0, 0);
+      const int given = g.target >= 0 && at >= 0 && at < Tl::TM * 32 ? (int)at : -1;
+      int last = left - Tl::row_of(0, 0);
+      if (!WHOLE) asm volatile("" : "+v"(last));  // (opaque: comparisons are not made ahead and kept)
+      __builtin_amdgcn_sched_barrier(0);
+      auto four = [&](int i, int q, auto with_given) {
+        typename Tl::V4 out;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-          float y = 0.f;
-          if (!g.zero && v + r < a.weight.rows) {
-            y = grad_of(Tl::value(acc, i, j, 4 * q + r), c, g);
-            if (v + r == given) y += g.g;
-          }
-          out[r] = (T)(y * factor);
+          const int place = 32 * i + 8 * q + r;
+          float y = grad_of(Tl::value(acc, i, j, 4 * q + r), c, g);
+          if (decltype(with_given)::value && place == given) y += g.g;
+          out[r] = (T)(!g.zero && (WHOLE || place < last) ? y * factor : 0.f);
         }
-        if (a.g && v < a.g_stride && t < a.gt_stride) *reinterpret_cast<T4*>(a.g + t * a.g_stride + v) = out;
-        if (a.gt && t < a.gt_stride) {
+        keep_four<Tl>(sh, i, j, q, out);
+      };
+      const bool any = __ballot(given >= 0);
 #pragma unroll
-          for (int r = 0; r < 4; r++)
-            if (v + r < a.weight.rows) a.gt[(v + r) * a.gt_stride + t] = out[r];
+      for (int i = 0; i < Tl::TM; i++) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          if (any) four(i, q, std::true_type{});
+          else four(i, q, std::false_type{});
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
-  }
+    }
+  };
+  if (left == Tl::BM) columns(std::true_type{});
+  else columns(std::false_type{});
+  for_rows<Tl>(sh, [&](int row, int m, typename Tl::V8 x) {
+    if (n0 + row < a.g_rows && m0 + m < a.g_stride)
+      *reinterpret_cast<typename Tl::V8*>(a.g + (n0 + row) * a.g_stride + m0 + m) = x;
+  });
 }
 
 template <class T>
@@ -534,15 +624,15 @@ struct ProductArgs {
   const float* factor;  // [1]: inverse of G's factor; NULL: 1
   T* out;               // [b.rows][out_stride]: the product, rounded (k_part >= k)
   int64_t out_stride;
+  int64_t out_width;    // entries of a row that are written, at most a.rows
   float* sums;          // or parts [k parts][b.rows][a.rows] in 32 bits,
   bool add;             // added to what is there
 };
 
 // out[n][m] = sum_k A[m][k] B[n][k]
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void product_kernel(ProductArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, 1) void product_kernel(ProductArgs<typename Tl::Elem> a) {
   using T = typename Tl::Elem;
-  using T4 = __attribute__((ext_vector_type(4))) T;
   using F4 = __attribute__((ext_vector_type(4))) float;
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x), tiles = (uint32_t)(a.m_tiles * a.n_tiles);
@@ -553,16 +643,12 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::T
   const int64_t k0 = part * a.k_part, k1 = k0 + a.k_part < a.k ? k0 + a.k_part : a.k;
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.a, a.b, m0, n0, k0, k1, sh, acc);
-  const float factor = a.factor ? a.factor[1] : 1.f;
-  const int left = a.a.rows - m0 < Tl::BM ? (int)(a.a.rows - m0) : Tl::BM;
-  // whole groups of four entries, aligned to their size, or entry by entry
-  const bool fours = a.a.rows % 4 == 0 && (a.out ? a.out_stride % 4 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7) == 0 : true);
-  auto put = [&](auto whole) {
+  if (!a.out) {
+    const int left = a.a.rows - m0 < Tl::BM ? (int)(a.a.rows - m0) : Tl::BM;  // (a multiple of 8)
 #pragma unroll
     for (int j = 0; j < Tl::TN; j++) {
       const int64_t n = n0 + Tl::col_of(j);
       if (n >= a.b.rows) continue;
-      T* out = a.out + n * a.out_stride + m0;
       float* sums = a.sums + ((int64_t)part * a.b.rows + n) * a.a.rows + m0;
 #pragma unroll
       for (int i = 0; i < Tl::TM; i++)
@@ -571,43 +657,51 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::T
           const int m = Tl::row_of(i, q);
           if (m >= left) continue;
           F4 y;
-          T4 z;
 #pragma unroll
-          for (int r = 0; r < 4; r++) {
-            y[r] = Tl::value(acc, i, j, 4 * q + r);
-            z[r] = (T)(y[r] * factor);
-          }
-          if (decltype(whole)::value) {
-            if (a.out) {
-              *reinterpret_cast<T4*>(out + m) = z;
-            } else {
-              if (a.add) y += *reinterpret_cast<F4*>(sums + m);
-              *reinterpret_cast<F4*>(sums + m) = y;
-            }
-          } else {
-#pragma unroll 1
-            for (int r = 0; r < 4; r++)
-              if (m + r < left) {
-                if (a.out) out[m + r] = z[r];
-                else sums[m + r] = a.add ? sums[m + r] + y[r] : y[r];
-              }
-          }
+          for (int r = 0; r < 4; r++) y[r] = Tl::value(acc, i, j, 4 * q + r);
+          if (a.add) y += *reinterpret_cast<F4*>(sums + m);
+          *reinterpret_cast<F4*>(sums + m) = y;
         }
     }
-  };
-  if (fours) put(std::true_type{});
-  else put(std::false_type{});
+    return;
+  }
+  const float factor = a.factor ? a.factor[1] : 1.f;
+#pragma unroll
+  for (int j = 0; j < Tl::TN; j++)
+#pragma unroll
+    for (int i = 0; i < Tl::TM; i++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        typename Tl::V4 z;
+#pragma unroll
+        for (int r = 0; r < 4; r++) z[r] = (T)(Tl::value(acc, i, j, 4 * q + r) * factor);
+        keep_four<Tl>(sh, i, j, q, z);
+      }
+  // whole pieces of 16 bytes, or entry by entry
+  const bool whole = a.out_width % 8 == 0 && a.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15) == 0;
+  for_rows<Tl>(sh, [&](int row, int m, typename Tl::V8 x) {
+    if (n0 + row >= a.b.rows || m0 + m >= a.out_width) return;
+    T* p = a.out + (n0 + row) * a.out_stride + m0 + m;
+    if (whole) {
+      *reinterpret_cast<typename Tl::V8*>(p) = x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (m0 + m + i < a.out_width) p[i] = x[i];
+    }
+  });
 }
 
-// out[row][col] = factor * the sum of the parts
+// out[row][col] = factor * the sum of the parts, for the first `cols` of their rows of `width`
 template <class T>
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t rows, int64_t cols,
-                                                        const float* factor, T* out, int64_t stride) {
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t rows, int64_t width,
+                                                        int64_t cols, const float* factor, T* out, int64_t stride) {
   const float f = factor ? factor[1] : 1.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
     float y = 0.f;
-    for (int p = 0; p < parts; p++) y += sums[p * rows * cols + i];
-    out[i / cols * stride + i % cols] = (T)(y * f);
+    const int64_t row = i / cols, col = i - row * cols;
+    for (int p = 0; p < parts; p++) y += sums[(p * rows + row) * width + col];
+    out[row * stride + col] = (T)(y * f);
   }
 }
 
@@ -616,6 +710,7 @@ __global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32
 constexpr int64_t up(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 constexpr int64_t div_up(int64_t x, int64_t n) { return (x + n - 1) / n; }
 constexpr int64_t PIECE = 256;    // the vocabulary is taken in multiples of this
+constexpr int64_t MOST_PIECE = 1 << 21;  // (256 rows of G, and of hidden and weight, lie in one buffer)
 constexpr int64_t CUS = 256;      // compute units
 
 int64_t forward_tile_rows(int64_t rows) { return rows <= 64 ? 128 : 256; }
@@ -651,12 +746,15 @@ int forward_by_rows(const HeadArgs<T>& a, hipStream_t st) {
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
 struct GradPlan {
   int64_t padded;         // rows, up to a multiple of 64
+  int64_t wide;           // width, up to a multiple of 8
   int64_t k_part, parts;  // parts of k in grad_hidden (of every piece alike, so that their sums can go on)
-  int64_t factor, hidden_t, sums, g, gt, weight_t, bytes;
+  int64_t factor, sums, g, hidden, weight, bytes;
 };
-GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece) {
+// pack: hidden and weight are copied to aligned rows
+GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
   GradPlan p;
   p.padded = up(rows, 64);
+  p.wide = up(width, 8);
   p.parts = CUS / (div_up(width, 256) * div_up(rows, 256));
   const int64_t most = div_up(piece, 1024);  // at least 16 steps of k each
   if (p.parts > most) p.parts = most;
@@ -670,11 +768,10 @@ GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece) {
     return was;
   };
   p.factor = take(8);
-  p.hidden_t = take(2 * width * p.padded);
-  p.sums = take(4 * p.parts * rows * width);
+  p.sums = take(4 * p.parts * rows * p.wide);
   p.g = take(2 * p.padded * piece);
-  p.gt = take(2 * p.padded * piece);
-  p.weight_t = take(2 * width * piece);
+  p.hidden = take(pack ? 2 * rows * p.wide : 0);
+  p.weight = take(pack ? 2 * piece * p.wide : 0);
   p.bytes = at;
   return p;
 }
@@ -689,20 +786,13 @@ struct GradCall {
   T *grad_hidden, *grad_weight;
   int64_t grad_hidden_stride, grad_weight_stride;
   uint8_t* work;
-  int64_t piece;
+  int64_t work_bytes;
 };
 
 template <class T>
-hipError_t transpose(const Operand<T>& in, int64_t cols, T* out, int64_t padded, hipStream_t st) {
-  return launch(transpose_kernel<T>, dim3((uint32_t)(padded / 64 * div_up(cols, 64))), dim3(256), st, in.p, in.stride,
-                in.rows, cols, out, padded);
-}
-
-template <class Tl>
-hipError_t grad_logits(GradLogitsArgs<typename Tl::Elem> a, hipStream_t st) {
-  a.m_tiles = (int32_t)div_up(a.weight.rows, Tl::BM);
-  a.n_tiles = (int32_t)div_up(a.hidden.rows, Tl::BN);
-  return launch(grad_logits_kernel<Tl>, dim3((uint32_t)((int64_t)a.m_tiles * a.n_tiles)), dim3(Tl::THREADS), st, a);
+hipError_t pack(const Operand<T>& in, int64_t width, T* out, int64_t stride, hipStream_t st) {
+  const int64_t blocks = div_up(in.rows * stride, 1024);
+  return launch(pack_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st, in, width, out, stride);
 }
 
 template <class Tl>
@@ -715,55 +805,73 @@ hipError_t product(ProductArgs<typename Tl::Elem> a, hipStream_t st) {
 
 template <class T>
 int run_gradients(const GradCall<T>& c, hipStream_t st) {
+  using Logits = Tile<T, 256, 256, 2, 2, true>;
+  using ByHidden = Tile<T, 256, 256, 2, 2, true, true, true>;   // grad_weight: sums over rows
+  using ByWeight = Tile<T, 256, 256, 2, 2, true, true, false>;  // grad_hidden: sums over the vocabulary
+  auto bad = [](hipError_t e) { return e != hipSuccess; };
   const int64_t rows = c.hidden.rows, vocab = c.weight.rows;
   if (rows == 0) {  // grad_weight is the empty sum
-    using Whole = Tile<T, 256, 256, 2, 2, true>;
-    const ProductArgs<T> pa{{c.hidden.p, 0, c.width}, {c.hidden.p, 0, vocab}, 0, 1, 0, 0, nullptr, c.grad_weight,
-                            c.grad_weight_stride, nullptr, false};
-    return !c.grad_weight || product<Whole>(pa, st) == hipSuccess ? TT_OK : TT_ERR_HIP;
+    const ProductArgs<T> pa{{nullptr, 0, up(c.width, 8)}, {nullptr, 0, vocab}, 0, 1, 0, 0, nullptr, c.grad_weight,
+                            c.grad_weight_stride, c.width, nullptr, false};
+    return !c.grad_weight || !bad(product<ByHidden>(pa, st)) ? TT_OK : TT_ERR_HIP;
   }
-  const GradPlan p = grad_plan(rows, c.width, c.piece);
-  float* factor = nullptr;
-  T* hidden_t = reinterpret_cast<T*>(c.work + p.hidden_t);
-  T* weight_t = reinterpret_cast<T*>(c.work + p.weight_t);
+  const bool aligned = vectors(c.hidden, c.width) && vectors(c.weight, c.width);
+  // the largest piece of the vocabulary that the workspace holds
+  int64_t piece = PIECE, most = up(vocab < MOST_PIECE ? vocab : MOST_PIECE, PIECE);
+  while (piece < most) {
+    const int64_t mid = up((piece + most) / 2, PIECE);
+    if (grad_plan(rows, c.width, mid, !aligned).bytes <= c.work_bytes) piece = mid;
+    else most = mid - PIECE;
+  }
+  const GradPlan p = grad_plan(rows, c.width, piece, !aligned);
+  const int64_t width = aligned ? c.width : p.wide;
   T* g = reinterpret_cast<T*>(c.work + p.g);
-  T* gt = reinterpret_cast<T*>(c.work + p.gt);
   float* sums = reinterpret_cast<float*>(c.work + p.sums);
-  const bool vec = vectors(c.hidden, c.width) && vectors(c.weight, c.width);
-  auto bad = [](hipError_t e) { return e != hipSuccess; };
+  const float* factor = nullptr;
   if (std::is_same<T, f16_t>::value) {
-    factor = reinterpret_cast<float*>(c.work + p.factor);
-    const float most = logf((float)vocab) + 0.5f;  // |p (log p + H)| <= 1/e + log(vocab)
-    if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, most, c.scale, c.grad_logprobs, c.grad_entropy, factor)))
+    float* f = reinterpret_cast<float*>(c.work + p.factor);
+    const float entropy = logf((float)vocab) + 0.5f;  // |p (log p + H)| <= 1/e + log(vocab)
+    if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, entropy, c.scale, c.grad_logprobs, c.grad_entropy, f)))
       return TT_ERR_HIP;
+    factor = f;
   }
-  if (c.grad_weight && bad(transpose(c.hidden, c.width, hidden_t, p.padded, st))) return TT_ERR_HIP;
-  for (int64_t first = 0; first < vocab; first += c.piece) {
-    const int64_t n = vocab - first < c.piece ? vocab - first : c.piece, n_padded = up(n, 64);
-    const Operand<T> weight{c.weight.p + first * c.weight.stride, c.weight.stride, n};
-    const GradLogitsArgs<T> ga{weight,  c.hidden,        c.width,        first, vocab,    c.scale, c.targets, c.stats,
-                               c.entropy, c.grad_logprobs, c.grad_entropy, factor,
-                               c.grad_hidden ? g : nullptr, c.grad_weight ? gt : nullptr, n_padded, p.padded, 0, 0};
-    if (bad(vec ? grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st) : grad_logits<Tile<T, 256, 256, 4, 2, false>>(ga, st)))
+  Operand<T> hidden = c.hidden;
+  if (!aligned) {
+    T* to = reinterpret_cast<T*>(c.work + p.hidden);
+    if (bad(pack(c.hidden, c.width, to, p.wide, st))) return TT_ERR_HIP;
+    hidden = {to, p.wide, rows};
+  }
+  const bool direct = p.parts == 1 && piece >= vocab;  // grad_hidden needs no sums in between
+  for (int64_t first = 0; first < vocab; first += piece) {
+    const int64_t n = vocab - first < piece ? vocab - first : piece, g_stride = up(n, 64);
+    Operand<T> weight{c.weight.p + first * c.weight.stride, c.weight.stride, n};
+    if (!aligned) {
+      T* to = reinterpret_cast<T*>(c.work + p.weight);
+      if (bad(pack(weight, c.width, to, p.wide, st))) return TT_ERR_HIP;
+      weight = {to, p.wide, n};
+    }
+    const int32_t m_tiles = (int32_t)div_up(n, Logits::BM), n_tiles = (int32_t)div_up(rows, Logits::BN);
+    const GradLogitsArgs<T> ga{weight,    hidden,          width,          first,  vocab, c.scale,  c.targets, c.stats,
+                               c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.padded,  m_tiles, n_tiles};
+    if (bad(launch(grad_logits_kernel<Logits>, dim3((uint32_t)((int64_t)m_tiles * n_tiles)), dim3(Logits::THREADS), st, ga)))
       return TT_ERR_HIP;
-    using Whole = Tile<T, 256, 256, 2, 2, true>;
     if (c.grad_weight) {
-      const ProductArgs<T> pa{{hidden_t, p.padded, c.width}, {gt, p.padded, n}, p.padded, p.padded, 0, 0, factor,
-                              c.grad_weight + first * c.grad_weight_stride, c.grad_weight_stride, nullptr, false};
-      if (bad(product<Whole>(pa, st))) return TT_ERR_HIP;
+      const ProductArgs<T> pa{{hidden.p, hidden.stride, width}, {g, g_stride, n}, rows, rows, 0, 0, factor,
+                              c.grad_weight + first * c.grad_weight_stride, c.grad_weight_stride, c.width, nullptr, false};
+      if (bad(product<ByHidden>(pa, st))) return TT_ERR_HIP;
     }
     if (c.grad_hidden) {
-      if (bad(transpose(weight, c.width, weight_t, n_padded, st))) return TT_ERR_HIP;
-      const ProductArgs<T> pa{{weight_t, n_padded, c.width}, {g, n_padded, rows}, n_padded, p.k_part, 0, 0, nullptr,
-                              nullptr, 0, sums, first > 0};
-      if (bad(product<Whole>(pa, st))) return TT_ERR_HIP;
+      const ProductArgs<T> pa{{weight.p, weight.stride, width}, {g, g_stride, rows}, n, direct ? n : p.k_part, 0, 0,
+                              direct ? factor : nullptr, direct ? c.grad_hidden : nullptr, c.grad_hidden_stride, c.width,
+                              sums, first > 0};
+      if (bad(product<ByWeight>(pa, st))) return TT_ERR_HIP;
     }
   }
-  if (c.grad_hidden) {
+  if (c.grad_hidden && !direct) {
     const int64_t blocks = div_up(rows * c.width, 256);
-    const int32_t used = (int32_t)div_up(up(vocab < c.piece ? vocab : c.piece, 64), p.k_part);  // parts of the first piece
+    const int32_t used = (int32_t)div_up(vocab < piece ? vocab : piece, p.k_part);  // parts of the first piece
     if (bad(launch(sum_parts_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st,
-                   static_cast<const float*>(sums), used, rows, c.width, static_cast<const float*>(factor), c.grad_hidden,
+                   static_cast<const float*>(sums), used, rows, width, c.width, factor, c.grad_hidden,
                    c.grad_hidden_stride)))
       return TT_ERR_HIP;
   }
@@ -814,7 +922,7 @@ extern "C" int tt_head_scores(const void* hidden, int64_t hidden_stride, const v
 extern "C" int64_t tt_head_scores_grad_workspace(int64_t rows, int64_t vocab, int64_t width, int32_t ample) {
   if (!head_sizes(rows, vocab, width)) return TT_ERR_BAD_ARG;
   if (rows == 0) return 0;
-  return grad_plan(rows, width, ample ? up(vocab, PIECE) : PIECE).bytes;
+  return grad_plan(rows, width, ample ? up(vocab < MOST_PIECE ? vocab : MOST_PIECE, PIECE) : PIECE, true).bytes;
 }
 
 extern "C" int tt_head_scores_grad(const void* hidden, int64_t hidden_stride, const void* weight, int64_t weight_stride,
@@ -830,25 +938,17 @@ extern "C" int tt_head_scores_grad(const void* hidden, int64_t hidden_stride, co
     return TT_ERR_BAD_ARG;
   if (!grad_hidden && !grad_weight) return TT_OK;
   if (!weight || (rows > 0 && (!hidden || !stats || !workspace || (grad_entropy && !entropy)))) return TT_ERR_NULL_ARG;
-  // launches of at most 2^32 threads
-  if (div_up(vocab, 256) * (div_up(rows, 256) + div_up(width, 256)) > (int64_t)UINT32_MAX / 512 ||
-      up(rows, 64) / 64 * div_up(width, 64) > (int64_t)UINT32_MAX / 256 ||
-      div_up(vocab, 64) * div_up(width, 64) > (int64_t)UINT32_MAX / 256)
+  // launches of at most 2^32 threads, rows within a buffer
+  if (width > MOST_PIECE || div_up(vocab, 256) * (div_up(rows, 256) + div_up(width, 256)) > (int64_t)UINT32_MAX / 512 ||
+      div_up(rows, 256) * div_up(width, 256) > (int64_t)UINT32_MAX / 512)
     return TT_ERR_TOO_LARGE;
-  // the largest piece of the vocabulary that the workspace holds
-  int64_t lo = 1, hi = div_up(vocab, PIECE);
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (rows == 0 || grad_plan(rows, width, mid * PIECE).bytes <= workspace_bytes) lo = mid;
-    else hi = mid - 1;
-  }
   auto go = [&](auto zero) {
     using T = decltype(zero);
     return run_gradients(GradCall<T>{{static_cast<const T*>(hidden), hidden_stride, rows},
                                      {static_cast<const T*>(weight), weight_stride, vocab},
                                      width, scale, targets, stats, entropy, grad_logprobs, grad_entropy,
                                      static_cast<T*>(grad_hidden), static_cast<T*>(grad_weight), grad_hidden_stride,
-                                     grad_weight_stride, static_cast<uint8_t*>(workspace), lo * PIECE},
+                                     grad_weight_stride, static_cast<uint8_t*>(workspace), workspace_bytes},
                          static_cast<hipStream_t>(stream));
   };
   return type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});
