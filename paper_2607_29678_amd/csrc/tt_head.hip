@@ -81,7 +81,7 @@ template <class T, int BM_, int BN_, int WM_, int WN_, bool VEC_, bool AC = fals
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr bool VEC = VEC_;  // rows are aligned to 16 bytes and k is a multiple of 8
-  static constexpr bool DIRECT = VEC && BM == 256 && BN == 256;
+  static constexpr bool DIRECT = VEC && BM == 256 && BN >= 128;
   static constexpr int THREADS = 64 * WM * WN;
   static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // 32 x 32 products of a wave
   using Elem = T;
@@ -89,19 +89,22 @@ struct Tile {
   using V4 = typename Mfma<T>::V4;
   static constexpr int NA = BM * 8 / THREADS, NB = BN * 8 / THREADS;  // 16-byte pieces a thread stages
   static_assert(NA * THREADS == BM * 8 && NB * THREADS == BN * 8, "whole pieces");
+  static constexpr bool STREAM = VEC && BM < 256;
+  static constexpr int STAGES = STREAM ? 3 : 2;
   struct Shared {
-    T a[2][BM * BK], b[2][BN * BK];
+    T a[STAGES][BM * BK], b[STAGES][BN * BK];
   };
 
   // Piece q of a stage: row q / 8, entries 8 (q % 8) and on.  In LDS the pieces
-  // of a row are permuted by the row's low bits, so that the 32 rows that a wave
-  // reads at one k lie in different banks.
-  static __device__ __forceinline__ int place(int row, int piece) { return row * BK + ((piece ^ (row & 7)) << 3); }
+  // of a row are permuted by the row's number, so that the 16 rows that are read
+  // at a time (two of them fill the 64 banks) lie in different banks.
+  static __device__ __forceinline__ int twist(int row) { return row >> 1 & 7; }
+  static __device__ __forceinline__ int place(int row, int piece) { return row * BK + ((piece ^ twist(row)) << 3); }
 
-  // An operand by columns is staged as 64 rows of 256 entries; blocks of 32
-  // entries are permuted by this, so that the eight half rows that a wave reads
+  // An operand by columns is staged as 64 rows of BM (BN) entries; blocks of 32
+  // entries are permuted by this, so that the four rows that half a wave reads
   // at a time lie in different banks.
-  static __device__ __forceinline__ int spread(int row) { return (row & 3) | (row >> 1 & 4); }
+  static __device__ __forceinline__ int spread(int row) { return row & 3; }
 
   static __device__ __forceinline__ V8 load(const Operand<T>& o, int64_t row, int64_t k, int64_t k_end) {
     V8 v = {};
@@ -118,6 +121,7 @@ struct Tile {
   static __device__ __forceinline__ void multiply(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
                                                   int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
     if constexpr (DIRECT) multiply_direct(a, b, m0, n0, k0, k1, sh, acc);
+    else if constexpr (STREAM) multiply_stream(a, b, m0, n0, k0, k1, sh, acc);
     else multiply_staged(a, b, m0, n0, k0, k1, sh, acc);
   }
 
@@ -193,60 +197,68 @@ struct Tile {
   static constexpr int WAVES = WM * WN, DA = BM / 8 / WAVES, DB = BN / 8 / WAVES;  // loads of 8 rows by a wave
   static __device__ __forceinline__ void multiply_direct(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
                                                          int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
-    static_assert(VEC && DA * WAVES * 8 == BM && DB * WAVES * 8 == BN && (!AC || BM == 256) && (!BC || BN == 256), "whole loads");
+    static_assert(VEC && DA * WAVES * 8 == BM && DB * WAVES * 8 == BN, "whole loads");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     // Byte offsets of this lane's pieces from the tile's first entry, and the
     // entries of k that a piece has left at stage 0.
     uint32_t oa[DA], ob[DB];
-    auto offset = [&](const Operand<T>& o, int64_t first, int load, auto by_columns) {
-      if (decltype(by_columns)::value) {  // two rows of 256 entries
-        const int64_t row = load * 2 + (lane >> 5), col = ((((lane & 31) >> 2) ^ spread((int)row)) << 5) + (lane & 3) * 8;
+    // (by columns a load holds 512 / BM rows: row_in() of its first row on)
+    auto row_in = [&](int load, int columns) { return load * (512 / columns) + lane / (columns / 8); };
+    auto offset = [&](const Operand<T>& o, int64_t first, int load, int columns, auto by_columns) {
+      if (decltype(by_columns)::value) {
+        const int64_t row = row_in(load, columns);
+        const int64_t col = (((lane % (columns / 8) >> 2) ^ spread((int)row)) << 5) + (lane & 3) * 8;
         return first + col < o.rows ? (uint32_t)(row * o.stride + col) * 2 : BUFFER_BYTES;
       }
       const int64_t row = load * 8 + (lane >> 3);  // eight rows of 64 entries
-      return first + row < o.rows ? (uint32_t)(row * o.stride + ((lane & 7) ^ (lane >> 3)) * 8) * 2 : BUFFER_BYTES;
-    };
-    auto stages_of = [&](int load, auto by_columns) {
-      const int64_t left = k1 - k0 - (decltype(by_columns)::value ? load * 2 + (lane >> 5) : ((lane & 7) ^ (lane >> 3)) * 8);
-      return left <= 0 ? 0 : (int)((left + BK - 1) / BK);  // stages in which the piece lies before k1
+      return first + row < o.rows ? (uint32_t)(row * o.stride + ((lane & 7) ^ twist((int)row)) * 8) * 2 : BUFFER_BYTES;
     };
     using A = std::integral_constant<bool, AC>;
     using B = std::integral_constant<bool, BC>;
 #pragma unroll
-    for (int i = 0; i < DA; i++) oa[i] = offset(a, m0, wave * DA + i, A{});
+    for (int i = 0; i < DA; i++) oa[i] = offset(a, m0, wave * DA + i, BM, A{});
 #pragma unroll
-    for (int i = 0; i < DB; i++) ob[i] = offset(b, n0, wave * DB + i, B{});
+    for (int i = 0; i < DB; i++) ob[i] = offset(b, n0, wave * DB + i, BN, B{});
     const T* pa = AC ? a.p + k0 * a.stride + m0 : a.p + m0 * a.stride + k0;
     const T* pb = BC ? b.p + k0 * b.stride + n0 : b.p + n0 * b.stride + k0;
     const int64_t next_a = AC ? BK * a.stride : BK, next_b = BC ? BK * b.stride : BK;
     const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
     const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
-    // (rows of k: all but the last few stages hold all of a wave's rows)
-    const int stages_a = stages_of(wave * DA, A{}), stages_b = stages_of(wave * DB, B{});
-    const int full_stages = (int)((k1 - k0) / BK), rows_left = (int)((k1 - k0) % BK);
+    // From the stage on that is not full, pieces past k1 are moved out of the buffer.
+    const int full_stages = (int)((k1 - k0) / BK), rest = (int)((k1 - k0) % BK);
+    auto cut = [&](int stage) {
+      const int here = stage > full_stages ? 0 : rest;
+      auto past = [&](int load, int columns, auto by_columns) {
+        const int row = decltype(by_columns)::value ? row_in(load, columns) : load * 8 + (lane >> 3);
+        return (decltype(by_columns)::value ? row : ((lane & 7) ^ twist(row)) * 8) >= here;
+      };
+#pragma unroll
+      for (int i = 0; i < DA; i++)
+        if (past(wave * DA + i, BM, A{})) oa[i] = BUFFER_BYTES;
+#pragma unroll
+      for (int i = 0; i < DB; i++)
+        if (past(wave * DB + i, BN, B{})) ob[i] = BUFFER_BYTES;
+    };
+    Buffer ba = buffer_at(pa), bb = buffer_at(pb);
     auto load_piece = [&](int stage, int i) {  // loads 0 .. DA + DB - 1 of a stage
       const uint32_t at = stage & 1;
-      auto real = [&](int load, int stages, auto by_columns) {
-        if (!decltype(by_columns)::value) return stage < stages;
-        const int row = load * 2 + (lane >> 5);
-        return stage < full_stages || (stage == full_stages && row < rows_left);
-      };
-      if (i < DA)
-        load_to_lds(buffer_at(pa + stage * next_a), real(wave * DA + i, stages_a, A{}) ? oa[i < DA ? i : 0] : BUFFER_BYTES,
-                    la + at * (BM * BK * 2) + i * 1024);
-      else
-        load_to_lds(buffer_at(pb + stage * next_b),
-                    real(wave * DB + i - DA, stages_b, B{}) ? ob[i < DA ? 0 : i - DA] : BUFFER_BYTES,
-                    lb + at * (BN * BK * 2) + (i - DA) * 1024);
+      if (i < DA) load_to_lds(ba, oa[i < DA ? i : 0], la + at * (BM * BK * 2) + i * 1024);
+      else load_to_lds(bb, ob[i < DA ? 0 : i - DA], lb + at * (BN * BK * 2) + (i - DA) * 1024);
+    };
+    // the buffers and offsets of a stage; stages are loaded in order
+    auto begin_stage = [&](int stage) {
+      ba = buffer_at(pa + stage * next_a);
+      bb = buffer_at(pb + stage * next_b);
+      if (stage >= full_stages) cut(stage);
     };
     V8 fa[2][TM], fb[2][TN];
     // fragment of rows (columns) 32 i .. 32 i + 31 from `first` on, 16 entries of k from 16 kk on
-    auto fragment = [&](const T* p, int first, int kk, auto by_columns) {
+    auto fragment = [&](const T* p, int first, int kk, int columns, auto by_columns) {
       if (decltype(by_columns)::value) {
         const int row = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
-        const T* q = p + row * 256 + ((((first >> 5) ^ spread(row)) << 5) | ((lane >> 4 & 1) << 4) | ((lane & 3) << 2));
-        const V4 x = read_transposed<V4>(q), y = read_transposed<V4>(q + 4 * 256);
+        const T* q = p + row * columns + ((((first >> 5) ^ spread(row)) << 5) | ((lane >> 4 & 1) << 4) | ((lane & 3) << 2));
+        const V4 x = read_transposed<V4>(q), y = read_transposed<V4>(q + 4 * columns);
         return (V8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
       }
       return *reinterpret_cast<const V8*>(&p[place(first + (lane & 31), kk * 2 + (lane >> 5))]);
@@ -256,17 +268,19 @@ struct Tile {
     auto read_one = [&](int buf, int kk, int to, int n) {
       if (n == 0 || n > TN) {
         const int i = n == 0 ? 0 : n - TN;
-        fa[to][i] = fragment(sh.a[buf], wm * TM * 32 + i * 32, kk, A{});
+        fa[to][i] = fragment(sh.a[buf], wm * TM * 32 + i * 32, kk, BM, A{});
       } else {
-        fb[to][n - 1] = fragment(sh.b[buf], wn * TN * 32 + (n - 1) * 32, kk, B{});
+        fb[to][n - 1] = fragment(sh.b[buf], wn * TN * 32 + (n - 1) * 32, kk, BN, B{});
       }
     };
     auto one = [&](int from, int ij) {
       const int i = ij / TN, j = ij % TN;
       acc[i][j] = Mfma<T>::mul(fa[from][i], fb[from][j], acc[i][j]);
     };
+    begin_stage(0);
 #pragma unroll
     for (int i = 0; i < DA + DB; i++) load_piece(0, i);
+    begin_stage(1);
 #pragma unroll
     for (int i = 0; i < DA + DB; i++) load_piece(1, i);
 #pragma unroll
@@ -287,7 +301,10 @@ struct Tile {
 #pragma unroll
       for (int kk = 0; kk < BK / 16; kk++) {
         const bool last = kk == BK / 16 - 1;
-        if (last) loads_done_but<0>();
+        if (last) {
+          begin_stage(s + 2);
+          loads_done_but<0>();
+        }
 #pragma unroll
         for (int ij = 0; ij < P; ij++) {
           one(kk & 1, ij);
@@ -305,6 +322,73 @@ struct Tile {
     loads_done_but<0>();
     // (what reads the accumulators by assembly has to wait for the last products itself)
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+  }
+
+  // The same for few columns, where the rows of A stream through once and
+  // nothing else counts: small tiles of two waves, three stages deep, so that
+  // a compute unit has up to 100 KB under way.
+  static __device__ __forceinline__ void multiply_stream(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
+                                                         int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    uint32_t oa[DA], ob[DB];
+    auto offset = [&](const Operand<T>& o, int64_t first, int row) {
+      return first + row < o.rows ? (uint32_t)(row * o.stride + ((lane & 7) ^ twist(row)) * 8) * 2 : BUFFER_BYTES;
+    };
+#pragma unroll
+    for (int i = 0; i < DA; i++) oa[i] = offset(a, m0, (wave * DA + i) * 8 + (lane >> 3));
+#pragma unroll
+    for (int i = 0; i < DB; i++) ob[i] = offset(b, n0, (wave * DB + i) * 8 + (lane >> 3));
+    const T *pa = a.p + m0 * a.stride + k0, *pb = b.p + n0 * b.stride + k0;
+    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
+    const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
+    const int full_stages = (int)((k1 - k0) / BK), rest = (int)((k1 - k0) % BK);
+    auto load_stage = [&](int stage, int buf) {  // in order of stages; past k1 zeros
+      if (stage >= full_stages) {
+        const int here = stage > full_stages ? 0 : rest;
+#pragma unroll
+        for (int i = 0; i < DA; i++)
+          if (((lane & 7) ^ twist((wave * DA + i) * 8 + (lane >> 3))) * 8 >= here) oa[i] = BUFFER_BYTES;
+#pragma unroll
+        for (int i = 0; i < DB; i++)
+          if (((lane & 7) ^ twist((wave * DB + i) * 8 + (lane >> 3))) * 8 >= here) ob[i] = BUFFER_BYTES;
+      }
+      const Buffer ba = buffer_at(pa + (int64_t)stage * BK), bb = buffer_at(pb + (int64_t)stage * BK);
+#pragma unroll
+      for (int i = 0; i < DA; i++) load_to_lds(ba, oa[i], la + buf * (BM * BK * 2) + i * 1024);
+#pragma unroll
+      for (int i = 0; i < DB; i++) load_to_lds(bb, ob[i], lb + buf * (BN * BK * 2) + i * 1024);
+    };
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+      for (int j = 0; j < TN; j++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
+    const int steps = (int)((k1 - k0 + BK - 1) / BK);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; i++) load_stage(i, i);
+    int buf = 0;
+    for (int s = 0; s < steps; s++) {
+      loads_done_but<(STAGES - 2) * (DA + DB)>();  // stage s is here, and every wave is past stage s - 1
+      load_stage(s + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; kk++) {
+        V8 fa[TM], fb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+          fa[i] = *reinterpret_cast<const V8*>(&sh.a[buf][place(wm * TM * 32 + i * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+#pragma unroll
+        for (int j = 0; j < TN; j++)
+          fb[j] = *reinterpret_cast<const V8*>(&sh.b[buf][place(wn * TN * 32 + j * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+          for (int j = 0; j < TN; j++) acc[i][j] = Mfma<T>::mul(fa[i], fb[j], acc[i][j]);
+      }
+      buf = buf == STAGES - 1 ? 0 : buf + 1;
+    }
+    loads_done_but<0>();
   }
 
   // One value of an accumulator, out of an accumulation register where the
@@ -363,7 +447,7 @@ struct HeadArgs {
 };
 
 template <class Tl>
-__global__ __launch_bounds__(Tl::THREADS, Tl::BM == 256 && Tl::BN == 256 ? Tl::THREADS / 256 : 2) void head_scores_kernel(HeadArgs<typename Tl::Elem> a) {
+__global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_kernel(HeadArgs<typename Tl::Elem> a) {
   __shared__ typename Tl::Shared sh;
   const uint32_t tile = die_order(blockIdx.x, gridDim.x);
   int64_t mt, nt;
@@ -532,9 +616,9 @@ struct GradLogitsArgs {
 // conflicts.
 template <class Tl, class V4>
 __device__ __forceinline__ void keep_four(typename Tl::Shared& sh, int i, int j, int q, V4 x) {
-  static_assert(Tl::TM == 4 && Tl::TN == 4, "rows of 256 bytes");
+  static_assert(Tl::TM == 4, "rows of 256 bytes");
   const int lane = threadIdx.x & 63, row = j * 32 + (lane & 31);
-  char* p = reinterpret_cast<char*>(&sh) + (threadIdx.x >> 6) * 32768 + row * 256;
+  char* p = reinterpret_cast<char*>(&sh) + ((threadIdx.x >> 6) * Tl::TN * 32 + row) * 256;
   *reinterpret_cast<V4*>(p + (((i * 4 + q) ^ (row & 15)) << 4) + (lane >> 5) * 8) = x;
 }
 // put(row, first entry, 8 entries) for every row of the wave's share
@@ -542,12 +626,12 @@ template <class Tl, class F>
 __device__ __forceinline__ void for_rows(typename Tl::Shared& sh, F put) {
   __syncthreads();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / Tl::WN, wn = wave % Tl::WN;
-  const char* p = reinterpret_cast<const char*>(&sh) + wave * 32768;
+  const char* p = reinterpret_cast<const char*>(&sh) + wave * Tl::TN * 32 * 256;
 #pragma unroll 8
-  for (int k = 0; k < 32; k++) {
+  for (int k = 0; k < Tl::TN * 8; k++) {
     const int row = k * 4 + (lane >> 4), piece = lane & 15;
     const auto x = *reinterpret_cast<const typename Tl::V8*>(p + row * 256 + ((piece ^ (row & 15)) << 4));
-    put(wn * 128 + row, wm * 128 + piece * 8, x);
+    put(wn * Tl::TN * 32 + row, wm * 128 + piece * 8, x);
   }
 }
 
@@ -713,7 +797,8 @@ constexpr int64_t PIECE = 256;    // the vocabulary is taken in multiples of thi
 constexpr int64_t MOST_PIECE = 1 << 21;  // (256 rows of G, and of hidden and weight, lie in one buffer)
 constexpr int64_t CUS = 256;      // compute units
 
-int64_t forward_tile_rows(int64_t rows) { return rows <= 64 ? 128 : 256; }
+constexpr int FEW_TILE = 64;  // vocabulary entries of a tile for up to 64 rows
+int64_t forward_tile_rows(int64_t rows) { return rows <= 64 ? FEW_TILE : 256; }
 
 bool head_sizes(int64_t rows, int64_t vocab, int64_t width) {
   return rows >= 0 && rows <= INT32_MAX && vocab >= 1 && vocab <= INT32_MAX && width >= 1 && width <= INT32_MAX;
@@ -734,13 +819,23 @@ int run_forward(HeadArgs<typename Tl::Elem> a, hipStream_t st) {
   return launch(head_scores_kernel<Tl>, dim3((uint32_t)(m * n)), dim3(Tl::THREADS), st, a) == hipSuccess ? TT_OK : TT_ERR_HIP;
 }
 
+// Whether tiles of 256 x 128 finish before tiles of 256 x 256: the tiles run in
+// rounds of one per compute unit, and a round of the narrow ones takes NARROW of
+// a round of the wide ones.
+constexpr double NARROW = 0.6;
+bool narrow(int64_t m, int64_t n, int64_t parts) {
+  const int64_t wide = div_up(div_up(m, 256) * div_up(n, 256) * parts, CUS);
+  return (double)div_up(div_up(m, 256) * div_up(n, 128) * parts, CUS) * NARROW < (double)wide;
+}
+
 template <class T, bool VEC>
 int forward_by_rows(const HeadArgs<T>& a, hipStream_t st) {
   const int64_t rows = a.hidden.rows;
-  if (rows <= 32) return run_forward<Tile<T, 128, 32, 4, 1, VEC>>(a, st);
-  if (rows <= 64) return run_forward<Tile<T, 128, 64, 4, 1, VEC>>(a, st);
-  if (rows <= 128) return run_forward<Tile<T, 256, 128, 4, 2, VEC>>(a, st);
-  return run_forward<Tile<T, 256, 256, VEC ? 2 : 4, 2, VEC>>(a, st);
+  if (rows <= 32) return run_forward<Tile<T, FEW_TILE, 32, 2, 1, VEC>>(a, st);
+  if (rows <= 64) return run_forward<Tile<T, FEW_TILE, 64, 2, 1, VEC>>(a, st);
+  if (!VEC) return run_forward<Tile<T, 256, 128, 4, 2, false>>(a, st);
+  if (narrow(a.weight.rows, rows, 1)) return run_forward<Tile<T, 256, 128, 2, 2, true>>(a, st);
+  return run_forward<Tile<T, 256, 256, 2, 2, true>>(a, st);
 }
 
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
@@ -803,17 +898,36 @@ hipError_t product(ProductArgs<typename Tl::Elem> a, hipStream_t st) {
                 dim3(Tl::THREADS), st, a);
 }
 
+// The products' tiles: grad_weight sums over rows, grad_hidden over the vocabulary.
+template <class T, int BN>
+using ByHidden = Tile<T, 256, BN, 2, 2, true, true, true>;
+template <class T, int BN>
+using ByWeight = Tile<T, 256, BN, 2, 2, true, true, false>;
+
+template <class T>
+hipError_t grad_weight_product(const ProductArgs<T>& a, hipStream_t st) {
+  return narrow(a.a.rows, a.b.rows, 1) ? product<ByHidden<T, 128>>(a, st) : product<ByHidden<T, 256>>(a, st);
+}
+template <class T>
+hipError_t grad_hidden_product(const ProductArgs<T>& a, hipStream_t st) {
+  return narrow(a.a.rows, a.b.rows, div_up(a.k, a.k_part)) ? product<ByWeight<T, 128>>(a, st)
+                                                          : product<ByWeight<T, 256>>(a, st);
+}
+template <class Tl>
+hipError_t grad_logits(GradLogitsArgs<typename Tl::Elem> a, hipStream_t st) {
+  a.m_tiles = (int32_t)div_up(a.weight.rows, Tl::BM);
+  a.n_tiles = (int32_t)div_up(a.hidden.rows, Tl::BN);
+  return launch(grad_logits_kernel<Tl>, dim3((uint32_t)((int64_t)a.m_tiles * a.n_tiles)), dim3(Tl::THREADS), st, a);
+}
+
 template <class T>
 int run_gradients(const GradCall<T>& c, hipStream_t st) {
-  using Logits = Tile<T, 256, 256, 2, 2, true>;
-  using ByHidden = Tile<T, 256, 256, 2, 2, true, true, true>;   // grad_weight: sums over rows
-  using ByWeight = Tile<T, 256, 256, 2, 2, true, true, false>;  // grad_hidden: sums over the vocabulary
   auto bad = [](hipError_t e) { return e != hipSuccess; };
   const int64_t rows = c.hidden.rows, vocab = c.weight.rows;
   if (rows == 0) {  // grad_weight is the empty sum
     const ProductArgs<T> pa{{nullptr, 0, up(c.width, 8)}, {nullptr, 0, vocab}, 0, 1, 0, 0, nullptr, c.grad_weight,
                             c.grad_weight_stride, c.width, nullptr, false};
-    return !c.grad_weight || !bad(product<ByHidden>(pa, st)) ? TT_OK : TT_ERR_HIP;
+    return !c.grad_weight || !bad(grad_weight_product(pa, st)) ? TT_OK : TT_ERR_HIP;
   }
   const bool aligned = vectors(c.hidden, c.width) && vectors(c.weight, c.width);
   // the largest piece of the vocabulary that the workspace holds
@@ -850,21 +964,21 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
       if (bad(pack(weight, c.width, to, p.wide, st))) return TT_ERR_HIP;
       weight = {to, p.wide, n};
     }
-    const int32_t m_tiles = (int32_t)div_up(n, Logits::BM), n_tiles = (int32_t)div_up(rows, Logits::BN);
     const GradLogitsArgs<T> ga{weight,    hidden,          width,          first,  vocab, c.scale,  c.targets, c.stats,
-                               c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.padded,  m_tiles, n_tiles};
-    if (bad(launch(grad_logits_kernel<Logits>, dim3((uint32_t)((int64_t)m_tiles * n_tiles)), dim3(Logits::THREADS), st, ga)))
+                               c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.padded,  0, 0};
+    if (bad(narrow(n, rows, 1) ? grad_logits<Tile<T, 256, 128, 2, 2, true>>(ga, st)
+                               : grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st)))
       return TT_ERR_HIP;
     if (c.grad_weight) {
       const ProductArgs<T> pa{{hidden.p, hidden.stride, width}, {g, g_stride, n}, rows, rows, 0, 0, factor,
                               c.grad_weight + first * c.grad_weight_stride, c.grad_weight_stride, c.width, nullptr, false};
-      if (bad(product<ByHidden>(pa, st))) return TT_ERR_HIP;
+      if (bad(grad_weight_product(pa, st))) return TT_ERR_HIP;
     }
     if (c.grad_hidden) {
       const ProductArgs<T> pa{{weight.p, weight.stride, width}, {g, g_stride, rows}, n, direct ? n : p.k_part, 0, 0,
                               direct ? factor : nullptr, direct ? c.grad_hidden : nullptr, c.grad_hidden_stride, c.width,
                               sums, first > 0};
-      if (bad(product<ByWeight>(pa, st))) return TT_ERR_HIP;
+      if (bad(grad_hidden_product(pa, st))) return TT_ERR_HIP;
     }
   }
   if (c.grad_hidden && !direct) {
@@ -939,8 +1053,8 @@ extern "C" int tt_head_scores_grad(const void* hidden, int64_t hidden_stride, co
   if (!grad_hidden && !grad_weight) return TT_OK;
   if (!weight || (rows > 0 && (!hidden || !stats || !workspace || (grad_entropy && !entropy)))) return TT_ERR_NULL_ARG;
   // launches of at most 2^32 threads, rows within a buffer
-  if (width > MOST_PIECE || div_up(vocab, 256) * (div_up(rows, 256) + div_up(width, 256)) > (int64_t)UINT32_MAX / 512 ||
-      div_up(rows, 256) * div_up(width, 256) > (int64_t)UINT32_MAX / 512)
+  if (width > MOST_PIECE || div_up(vocab, 128) * (div_up(rows, 128) + div_up(width, 128)) > (int64_t)UINT32_MAX / 256 ||
+      div_up(rows, 128) * div_up(width, 256) * 256 > (int64_t)UINT32_MAX / 256)
     return TT_ERR_TOO_LARGE;
   auto go = [&](auto zero) {
     using T = decltype(zero);

@@ -85,6 +85,13 @@ def test_strides(gpu, kind, pad, shift):
         check(*make(rows, 900, 128, kind, 7, pad, shift))
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab,width", [(256, 50_257, 72), (250, 50_001, 520), (1000, 20_011, 64), (513, 60_003, 192)])
+def test_many_tiles(gpu, kind, rows, vocab, width):
+    """Enough tiles to fill the compute units, with both tile widths among them."""
+    check(*make(rows, vocab, width, kind, rows))
+
+
 def test_targets_and_scale(gpu):
     hidden, weight, t = make(300, 1281, 128, torch.bfloat16, 8)
     t[0], t[1], t[2], t[299] = -1, 1281, 1280, 0
@@ -206,6 +213,13 @@ def test_grad_vocabularies(gpu, kind, vocab):
 @pytest.mark.parametrize("width", [1, 7, 8, 64, 65, 200, 513])
 def test_grad_widths(gpu, kind, width):
     check_grad(*make(90, 700, width, kind, width), *grads(90))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab,width", [(256, 50_257, 72), (250, 50_001, 1024), (1000, 20_011, 64), (513, 60_003, 192)])
+def test_grad_many_tiles(gpu, kind, rows, vocab, width):
+    """Enough tiles to fill the compute units, with both tile widths among them."""
+    check_grad(*make(rows, vocab, width, kind, rows), *grads(rows))
 
 
 @pytest.mark.parametrize("room", [0.0, 0.2, 0.5, 0.99])
