@@ -487,7 +487,7 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
 #pragma unroll
       for (int i = 0; i < Tl::TM; i++)
 #pragma unroll
-        for (int r = 0; r < 16; r++) m = fmaxf(m, entry(i, r));
+        for (int r = 0; r < 16; r++) m = larger(m, entry(i, r));
       __builtin_amdgcn_sched_barrier(0);
       const bool mine = given >= 0 && given < Tl::TM * 32 && !(given & 4);
       if (__ballot(mine)) {
@@ -499,23 +499,23 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
             if (32 * i + 8 * (r >> 2) + (r & 3) == given) x = Tl::value(acc, i, j, r);
         if (mine) a.given[t] = x;
       }
-      m = fmaxf(m, __shfl_xor(m, 32));
-      const float ref = reference(m);
-      float s0 = 0.f, u0 = 0.f;
+      m = larger(m, __shfl_xor(m, 32));
+      const Reference ref = reference(m, c);
+      Stats st = {m, 0.f, 0.f};
       if (!WHOLE) asm volatile("" : "+v"(last));
+      auto sums = [&](auto plain) {
 #pragma unroll
-      for (int i = 0; i < Tl::TM; i++) {
+        for (int i = 0; i < Tl::TM; i++) {
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-          const float d = (entry(i, r) - ref) * c, e = __builtin_amdgcn_exp2f(d);
-          s0 += e;
-          u0 += weigh(e, d);
+          for (int r = 0; r < 16; r++) add_entry<decltype(plain)::value>(st, entry(i, r), ref, c);
+          __builtin_amdgcn_sched_barrier(0);  // (the accumulators do not fit the other registers all at once)
         }
-        __builtin_amdgcn_sched_barrier(0);  // (the accumulators do not fit the other registers all at once)
-      }
-      s0 += __shfl_xor(s0, 32);
-      u0 += __shfl_xor(u0, 32);
-      if (lane < 32) joined[wm * Tl::BN + col] = {m, s0, u0, 0.f};
+      };
+      if (__ballot(!is_plain(m, c)) == 0) sums(std::true_type{});
+      else sums(std::false_type{});
+      st.s += __shfl_xor(st.s, 32);
+      st.u += __shfl_xor(st.u, 32);
+      if (lane < 32) joined[wm * Tl::BN + col] = {m, st.s, st.u, 0.f};
     }
   };
   if (left == Tl::BM) columns(std::true_type{});
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
 #pragma unroll
   for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
   if (lane) return;
-  const RowScores r = row_scores(st);
+  const RowScores r = row_scores(st, c);
   const int32_t t = targets ? targets[row] : -1;
   if (logprobs) logprobs[row] = given_log_prob(t, vocab, t >= 0 && t < vocab ? given[row] : 0.f, r, scale);
   if (stats) {

@@ -16,37 +16,64 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
 
+// The larger of two, NaN if either is: a row's maximum carries its NaNs.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // Statistics of a part of a row, in powers of two: m the largest logit, s the
-// sum of e_j = 2^d_j and u the sum of e_j d_j, with d_j = (x_j - m) c and
-// c = scale / log 2.  m stays in units of the logits: x_j - m is exact where it
-// matters and cannot overflow to the wrong side for masks of the type's lowest
-// value, which (x_j c) - (m c) could.
+// sum of e_j = 2^d_j and u the sum of e_j d_j, d_j = x_j c - R with c =
+// scale / log 2 and R the rounded product m c.  How far R is off m c is made up
+// for wherever sums of different m meet (rounded_off), so that one fused
+// multiply-add an entry gives d_j.  Where m c is too large for that (masks of
+// the type's lowest value overflow), d_j = (x_j - m) c.  d_j is held at -126 or
+// more: 2^-126 is nothing next to the largest entry's 1, and 0 times -inf does
+// not arise.
 struct Stats {
   float m, s, u;
 };
+constexpr float PLAIN_MOST = 1048576.f;
+constexpr float LEAST_EXPONENT = -126.f;
 
 __device__ __forceinline__ Stats empty_stats() { return {NEG_INF, 0.f, 0.f}; }
 
-// A finite reference to subtract: nothing but -inf so far leaves 0.
-__device__ __forceinline__ float reference(float m) { return m == NEG_INF ? 0.f : m; }
+// d_j = max((x_j - base) c + off, -126); base is 0 for all but huge m
+struct Reference {
+  float base, off;
+};
+__device__ __forceinline__ bool is_plain(float m, float c) { return m == NEG_INF || fabsf(m * c) < PLAIN_MOST; }
+__device__ __forceinline__ Reference reference(float m, float c) {
+  if (m == NEG_INF) return {0.f, 0.f};
+  return is_plain(m, c) ? Reference{0.f, -(m * c)} : Reference{m, 0.f};
+}
+// R - m c
+__device__ __forceinline__ float rounded_off(float m, float c) {
+  return m != NEG_INF && is_plain(m, c) ? -fmaf(m, c, -(m * c)) : 0.f;
+}
+// PLAIN: base is known to be 0
+template <bool PLAIN>
+__device__ __forceinline__ void add_entry(Stats& st, float x, const Reference& r, float c) {
+  const float d = fmaxf(fmaf(PLAIN ? x : x - r.base, c, r.off), LEAST_EXPONENT), e = __builtin_amdgcn_exp2f(d);
+  st.s += e;
+  st.u = fmaf(e, d, st.u);
+}
 
 // e d for e = 2^d: 0 where e is 0, also for d = -inf; NaN stays.
 __device__ __forceinline__ float weigh(float e, float d) { return e * fmaxf(d, -1e30f); }
 
 // a's sums moved to the larger maximum m.
 __device__ __forceinline__ void lower(Stats& a, float m, float c) {
-  if (a.m == m || a.s == 0.f) {
-    a.m = m;
+  if (a.m == m) return;
+  if (a.m == NEG_INF) {
+    a = {m, 0.f, 0.f};
     return;
   }
-  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
-  a.u = f * a.u + weigh(f, d) * a.s;
+  const float d = (a.m - m) * c + (rounded_off(a.m, c) - rounded_off(m, c)), f = __builtin_amdgcn_exp2f(d);
+  a.u = fmaf(f, a.u, weigh(f, d) * a.s);
   a.s *= f;
   a.m = m;
 }
 
 __device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
-  const float m = fmaxf(a.m, b.m);
+  const float m = larger(a.m, b.m);
   lower(a, m, c);
   lower(b, m, c);
   return {m, a.s + b.s, a.u + b.u};
@@ -60,14 +87,14 @@ __device__ __forceinline__ Stats shuffled_xor(const Stats& a, int lane_mask) {
 struct RowScores {
   float m, log_s, entropy;
 };
-__device__ __forceinline__ RowScores row_scores(const Stats& a) {
-  if (a.s == 0.f) return {NEG_INF, NEG_INF, 0.f};  // nothing but -inf
-  if (!(a.s < __builtin_inff()) || a.m == __builtin_inff()) {
+__device__ __forceinline__ RowScores row_scores(const Stats& a, float c) {
+  if (a.m == NEG_INF) return {NEG_INF, NEG_INF, 0.f};  // nothing but -inf
+  if (a.m != a.m || a.m == __builtin_inff()) {
     const float nan = __builtin_nanf("");
     return {nan, nan, nan};
   }
   const float l = __builtin_amdgcn_logf(a.s);  // base 2
-  return {a.m, LN2 * l, LN2 * (l - a.u / a.s)};
+  return {a.m, LN2 * (l + rounded_off(a.m, c)), LN2 * (l - a.u / a.s)};
 }
 
 // log p of logit x in a row with these results.

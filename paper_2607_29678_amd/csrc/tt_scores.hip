@@ -6,14 +6,16 @@
 // entries that it strides over.  The running maxima also find the alternatives:
 // the n_alt-th largest of 128 groups' maxima is a lower bound of the n_alt-th
 // largest logit, so entries below it are passed over, one comparison for each
-// 16-byte vector, and the few above it are kept in LDS and ordered at the end.
+// 16-byte vector, and the few vectors that reach it are kept in LDS; what they
+// hold above the last bound is ordered at the end.
 #include "tt_scores.h"
 
 namespace tt {
 namespace {
 
 constexpr int SC_THREADS = 256;
-constexpr int SC_CANDS = 1024;     // candidates that are ordered in LDS
+constexpr int SC_VECS = 192;       // 16-byte vectors with a possible alternative that a wave keeps in LDS
+constexpr int SC_CANDS = 512;      // candidates that are ordered there
 constexpr int SC_SPLIT_COLS = 2048;  // fewest columns of a part of a row
 constexpr int SC_MAX_SPLITS = 64;  // parts of a row: one list per lane when they are joined
 constexpr int64_t SC_BLOCKS = 1024;  // blocks that fill the chip (4 per compute unit)
@@ -30,7 +32,7 @@ int scores_splits(int64_t rows, int64_t vocab) {
 // A part's statistics and its alternatives in descending order (0: none)
 struct PartHead {
   Stats st;
-  float pad;
+  float given;  // logit of the given token, in the part that holds it
 };
 __host__ __device__ inline int64_t part_bytes(int n_alt) { return (int64_t)sizeof(PartHead) + 8 * (int64_t)n_alt; }
 
@@ -57,11 +59,12 @@ __device__ __forceinline__ Vec<T> load_vec(const T* p) {
   __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T)), 16);
   return r;
 }
+// Aligned, and not kept in the caches: a row is read once (7.1 TB/s on reads of
+// 4 GiB against 6.3 with ordinary loads).
 template <class T>
-__device__ __forceinline__ Vec<T> load_vec_aligned(const T* p) {
-  Vec<T> r;
-  __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), 16);
-  return r;
+__device__ __forceinline__ Vec<T> load_vec_once(const T* p) {
+  using U4 = __attribute__((ext_vector_type(4))) uint32_t;
+  return __builtin_bit_cast(Vec<T>, __builtin_nontemporal_load(reinterpret_cast<const U4*>(p)));
 }
 
 // A thread's entries of columns [0, n) of p: 16-byte vectors of the aligned
@@ -91,15 +94,20 @@ struct ScoreArgs {
   float* alt_logprobs;
   uint8_t* parts;  // workspace: rows * splits parts
   int splits;
+  int64_t per_part;  // columns of a part
 };
 
-struct ScoreShared {
+struct SumShared {
   Stats st[SC_THREADS / 64];
+};
+struct ScoreShared : SumShared {
   float maxima[SC_THREADS];
+  alignas(16) uint8_t vec[SC_THREADS / 64][SC_VECS][16];
+  uint32_t vec_at[SC_THREADS / 64][SC_VECS];
   uint64_t cands[SC_CANDS];
   uint64_t best[TT_MAX_ALTERNATIVES];
   float bound;
-  int n_cands, n_ties;
+  int n_vecs[SC_THREADS / 64], n_cands;
 };
 
 __device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(alt_key(x, 0) >> 32); }
@@ -145,7 +153,7 @@ __device__ __forceinline__ void order_candidates(int n, int n_alt, ScoreShared& 
 //    equal entries (masks of a finite value) follow in order of their IDs.
 //  - Should even the entries above it not fit, places are filled one by one.
 template <class T>
-__device__ __noinline__ void find_again(const Span<T>& sp, uint32_t first, int n_alt, float mine, ScoreShared& sh) {
+__device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, int n_alt, float mine, ScoreShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const float bound = bound_of<1u>(mine, n_alt, sh);
   if (tid == 0) sh.n_cands = 0;
@@ -204,80 +212,104 @@ __device__ __noinline__ void find_again(const Span<T>& sp, uint32_t first, int n
 // One part of one row per block.
 template <class T, bool ALT>
 __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
-  __shared__ ScoreShared sh;
-  constexpr int N = Vec<T>::N, U = 4;
+  __shared__ std::conditional_t<ALT, ScoreShared, SumShared> sh;
+  constexpr int N = Vec<T>::N, U = ALT ? 2 : 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x / a.splits;
-  const int part = (int)(blockIdx.x - row * a.splits);
-  const int64_t c0 = a.vocab * part / a.splits, c1 = a.vocab * (part + 1) / a.splits;
+  const uint32_t row32 = blockIdx.x / (uint32_t)a.splits, part = blockIdx.x - row32 * (uint32_t)a.splits;
+  const int64_t row = row32;
+  const int64_t c0 = a.per_part * part, c1 = c0 + a.per_part < a.vocab ? c0 + a.per_part : a.vocab;
   const T* p = a.logits + row * a.stride + c0;
   const Span<T> sp(p, c1 - c0);
   const float c = a.scale * LOG2E;
   const uint32_t first = (uint32_t)c0;
-  if (ALT) {
+  if constexpr (ALT) {
     if (tid < a.n_alt) sh.best[tid] = 0;
     if (tid == 0) sh.n_cands = 0;
   }
 
+  // the given token's logit (loaded ahead of the sums)
+  const int32_t target = a.targets ? a.targets[row] : -1;
+  const bool holds_given = target >= c0 && target < c1;
+  const float x_given = holds_given ? (float)p[target - c0] : 0.f;
+
   Stats st = empty_stats();
   float bound = NEG_INF;
-  auto sums = [&](float x, float ref) {
-    const float d = (x - ref) * c, e = __builtin_amdgcn_exp2f(d);
-    st.s += e;
-    st.u += weigh(e, d);
-  };
-  auto keep = [&](float x, int64_t j) {
-    if (x >= bound && x > NEG_INF) {
-      const int at = atomicAdd(&sh.n_cands, 1);
-      if (at < SC_CANDS) sh.cands[at] = alt_key(x, first + (uint32_t)j);
-    }
-  };
   // U vectors at a time share one move of the maximum.  The loop runs equally
-  // often in every thread: it holds barriers.
-  const int64_t steps = (sp.vecs + U * SC_THREADS - 1) / (U * SC_THREADS);
-  for (int64_t step = 0; step < steps; step++) {
-    const int64_t v = step * U * SC_THREADS + tid;
-    Vec<T> y[U];
+  // often in every thread: it holds barriers.  The vectors of the next step are
+  // under way while the last ones are summed; in the last step a thread repeats
+  // the last vector where it has none, and takes it for -inf.
+  constexpr int STEP = U * SC_THREADS;
+  const int vecs = (int)sp.vecs, steps = (vecs + STEP - 1) / STEP;
+  const T* body = p + sp.head;
+  Vec<T> y[U];
+  auto fetch = [&](int step) {
 #pragma unroll
     for (int k = 0; k < U; k++) {
-      if (v + k * SC_THREADS < sp.vecs) {
-        y[k] = load_vec_aligned(p + sp.head + (v + k * SC_THREADS) * N);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; i++) y[k].v[i] = (T)NEG_INF;
-      }
+      const int v = step * STEP + k * SC_THREADS + tid;
+      y[k] = load_vec_once(body + (int64_t)(v < vecs ? v : vecs - 1) * N);
     }
+  };
+  int n_vecs = 0;  // vectors that this wave has kept
+  auto take = [&](int step, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    const int v = step * STEP + tid, here = vecs - step * STEP;  // vectors of this step
     float x[U][N], top[U], m = st.m;
-#pragma unroll
-    for (int k = 0; k < U; k++) {
-#pragma unroll
-      for (int i = 0; i < N; i++) {
-        x[k][i] = (float)y[k].v[i];
-        top[k] = i ? fmaxf(top[k], x[k][i]) : x[k][i];
-      }
-      m = fmaxf(m, top[k]);
-    }
-    lower(st, m, c);
-    const float ref = reference(m);
 #pragma unroll
     for (int k = 0; k < U; k++)
 #pragma unroll
-      for (int i = 0; i < N; i++) sums(x[k][i], ref);
-    if (ALT) {
+      for (int i = 0; i < N; i++) x[k][i] = (float)y[k].v[i];
+    if (step + 1 < steps) fetch(step + 1);
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      top[k] = NEG_INF;
+      if (!WHOLE && k * SC_THREADS >= here) continue;  // (the same for every thread)
+      if (!WHOLE && k * SC_THREADS + tid >= here) {
+#pragma unroll
+        for (int i = 0; i < N; i++) x[k][i] = NEG_INF;
+      }
+      top[k] = x[k][0];
+#pragma unroll
+      for (int i = 1; i < N; i++) top[k] = larger(top[k], x[k][i]);
+      m = larger(m, top[k]);
+    }
+    lower(st, m, c);
+    const Reference ref = reference(m, c);
+    auto sums = [&](auto plain) {
+#pragma unroll
+      for (int k = 0; k < U; k++) {
+        if (!WHOLE && k * SC_THREADS >= here) continue;
+#pragma unroll
+        for (int i = 0; i < N; i++) add_entry<decltype(plain)::value>(st, x[k][i], ref, c);
+      }
+    };
+    if (__ballot(!is_plain(m, c)) == 0) sums(std::true_type{});
+    else sums(std::false_type{});
+    if constexpr (ALT) {
       if ((step & (step + 1)) == 0) bound = bound_of<0x10000u>(st.m, a.n_alt, sh);  // after 1, 2, 4, 8 ... steps
 #pragma unroll
-      for (int k = 0; k < U; k++)
-        if (top[k] >= bound)
+      for (int k = 0; k < U; k++) {
+        const bool mine = top[k] >= bound && top[k] > NEG_INF;
+        const uint64_t votes = __ballot(mine);
+        if (votes == 0) continue;
+        const int at = n_vecs + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(votes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)votes, 0));
+        if (mine && at < SC_VECS) {
+          Vec<T> z;
 #pragma unroll
-          for (int i = 0; i < N; i++) keep(x[k][i], sp.head + (v + k * SC_THREADS) * N + i);
+          for (int i = 0; i < N; i++) z.v[i] = (T)x[k][i];
+          __builtin_memcpy(sh.vec[wave][at], &z, 16);
+          sh.vec_at[wave][at] = (uint32_t)(sp.head + (int64_t)(v + k * SC_THREADS) * N);
+        }
+        n_vecs += __popcll(votes);
+      }
     }
-  }
-  if (ALT && steps == 0) __syncthreads();  // n_cands
+  };
+  if (steps > 0) fetch(0);
+  for (int step = 0; step + 1 < steps; step++) take(step, std::true_type{});
+  if (steps > 0) take(steps - 1, std::false_type{});
   auto edge = [&](int64_t j) {
-    const float x = (float)p[j], m = fmaxf(st.m, x);
+    const float x = (float)p[j], m = larger(st.m, x);
     lower(st, m, c);
-    sums(x, reference(m));
-    if (ALT) keep(x, j);
+    add_entry<false>(st, x, reference(m, c), c);
   };
   if (tid < sp.head) edge(tid);
   if (sp.tail + tid < sp.n) edge(sp.tail + tid);
@@ -290,9 +322,29 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
 #pragma unroll
   for (int w = 1; w < SC_THREADS / 64; w++) st = join(st, sh.st[w], c);
 
-  if (ALT) {
+  if constexpr (ALT) {
+    if (steps == 0) bound = bound_of<0x10000u>(mine, a.n_alt, sh);
+    auto keep = [&](float x, uint32_t j) {
+      if (x >= bound && x > NEG_INF) {
+        const int at = atomicAdd(&sh.n_cands, 1);
+        if (at < SC_CANDS) sh.cands[at] = alt_key(x, first + j);
+      }
+    };
+    // every wave looks through what it kept itself
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const bool all_kept = n_vecs <= SC_VECS;
+    for (int i = lane; all_kept && i < n_vecs * N; i += 64)
+      keep((float)reinterpret_cast<const T*>(sh.vec[wave])[i], sh.vec_at[wave][i / N] + i % N);
+    if (lane == 0) sh.n_vecs[wave] = n_vecs;
+    if (tid < sp.head) keep((float)p[tid], tid);
+    if (sp.tail + tid < sp.n) keep((float)p[sp.tail + tid], (uint32_t)sp.tail + tid);
+    __syncthreads();
     const int n = sh.n_cands;
-    if (n <= SC_CANDS) {
+    bool fits = n <= SC_CANDS;
+#pragma unroll
+    for (int w = 0; w < SC_THREADS / 64; w++) fits &= sh.n_vecs[w] <= SC_VECS;
+    if (fits) {
       order_candidates(n, a.n_alt, sh);
       __syncthreads();
     } else {
@@ -302,71 +354,116 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
   }
   if (a.splits > 1) {
     uint8_t* out = a.parts + (row * a.splits + part) * part_bytes(a.n_alt);
-    if (tid == 0) reinterpret_cast<PartHead*>(out)->st = st;
-    if (ALT && tid < a.n_alt) reinterpret_cast<uint64_t*>(out + sizeof(PartHead))[tid] = sh.best[tid];
+    if (tid == 0) *reinterpret_cast<PartHead*>(out) = {st, x_given};
+    if constexpr (ALT)
+      if (tid < a.n_alt) reinterpret_cast<uint64_t*>(out + sizeof(PartHead))[tid] = sh.best[tid];
     return;
   }
-  const RowScores r = row_scores(st);
+  const RowScores r = row_scores(st, c);
   if (tid == 0) {
-    const int32_t t = a.targets ? a.targets[row] : -1;
-    if (a.logprobs) a.logprobs[row] = given_log_prob(t, a.vocab, t >= 0 && t < a.vocab ? (float)p[t] : 0.f, r, a.scale);
+    if (a.logprobs) a.logprobs[row] = given_log_prob(target, a.vocab, x_given, r, a.scale);
     if (a.stats) {
       a.stats[2 * row] = r.m;
       a.stats[2 * row + 1] = r.log_s;
     }
     if (a.entropy) a.entropy[row] = r.entropy;
   }
-  if (ALT && tid < a.n_alt) {
-    const uint64_t k = sh.best[tid];
-    const bool nan = r.log_s != r.log_s;
-    a.alt_ids[row * a.n_alt + tid] = k && !nan ? alt_id(k) : -1;
-    a.alt_logprobs[row * a.n_alt + tid] = nan ? r.log_s : k ? log_prob(alt_value(k), r, a.scale) : NEG_INF;
+  if constexpr (ALT) {
+    if (tid < a.n_alt) {
+      const uint64_t k = sh.best[tid];
+      const bool nan = r.log_s != r.log_s;
+      a.alt_ids[row * a.n_alt + tid] = k && !nan ? alt_id(k) : -1;
+      a.alt_logprobs[row * a.n_alt + tid] = nan ? r.log_s : k ? log_prob(alt_value(k), r, a.scale) : NEG_INF;
+    }
   }
 }
 
-// Joins the parts of a row: one wave per row, one part per lane.
+// Joins the parts of a row.  The parts' lists are in order, so that n_alt
+// entries reach the least of their entries of one place; those are ordered.
 template <class T>
-__global__ __launch_bounds__(64) void scores_join_kernel(ScoreArgs<T> a) {
+__global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a) {
+  __shared__ uint64_t lists[SC_MAX_SPLITS * TT_MAX_ALTERNATIVES];  // [splits][n_alt]
+  __shared__ uint64_t cands[SC_CANDS];
+  __shared__ uint64_t least;
+  __shared__ int found;
   const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x;
+  const int tid = threadIdx.x, k = a.n_alt, n = a.splits * k;
   const float c = a.scale * LOG2E;
-  const uint8_t* in = a.parts + (row * a.splits + lane) * part_bytes(a.n_alt);
-  const bool have = lane < a.splits;
-  Stats st = have ? reinterpret_cast<const PartHead*>(in)->st : empty_stats();
+  const uint8_t* in = a.parts + row * a.splits * part_bytes(k);
+  PartHead head = {empty_stats(), 0.f};
+  if ((tid & 63) < a.splits) head = *reinterpret_cast<const PartHead*>(in + (tid & 63) * part_bytes(k));
+  const int32_t t = a.targets ? a.targets[row] : -1;
+  if (tid == 0) {
+    least = ~0ull;
+    found = 0;
+  }
+  if (k) {
+    for (int i = tid; i < n; i += SC_THREADS) {
+      const int part = i / k;
+      lists[i] = reinterpret_cast<const uint64_t*>(in + part * part_bytes(k) + sizeof(PartHead))[i - part * k];
+    }
+    __syncthreads();
+    const int level = (k + a.splits - 1) / a.splits - 1;  // every list's entry of this place: n_alt entries reach the least
+    if (n > SC_THREADS && tid < a.splits) atomicMin(reinterpret_cast<unsigned long long*>(&least), (unsigned long long)lists[tid * k + level]);
+  }
+  const float x_given = __shfl(head.given, t >= 0 && t < a.vocab ? (int)(t / a.per_part) : 0);
+  Stats st = head.st;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
-  const RowScores r = row_scores(st);
+  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);  // (every wave for itself)
+  const RowScores r = row_scores(st, c);
   const bool nan = r.log_s != r.log_s;
-  if (lane == 0) {
-    const int32_t t = a.targets ? a.targets[row] : -1;
-    if (a.logprobs)
-      a.logprobs[row] = given_log_prob(t, a.vocab, t >= 0 && t < a.vocab ? (float)a.logits[row * a.stride + t] : 0.f, r,
-                                       a.scale);
+  if (tid == 0) {
+    if (a.logprobs) a.logprobs[row] = given_log_prob(t, a.vocab, x_given, r, a.scale);
     if (a.stats) {
       a.stats[2 * row] = r.m;
       a.stats[2 * row + 1] = r.log_s;
     }
     if (a.entropy) a.entropy[row] = r.entropy;
   }
-  // the parts' lists are in order: the best of their heads is the next one
-  const uint64_t* list = reinterpret_cast<const uint64_t*>(in + sizeof(PartHead));
-  int at = 0;
-  uint64_t head = have && a.n_alt ? list[0] : 0;
-  for (int i = 0; i < a.n_alt; i++) {
-    uint64_t k = head;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-      const uint64_t o = __shfl_xor(k, d);
-      k = o > k ? o : k;
+  if (!k) return;
+  if (n <= SC_THREADS) {  // all of them are ordered
+    const uint64_t key = tid < n ? lists[tid] : 0;
+    int place = 0, some = 0;
+    for (int j = 0; j < n; j++) {
+      place += lists[j] > key;
+      some += lists[j] != 0;
     }
-    if (k && head == k) {
-      at++;
-      head = at < a.n_alt ? list[at] : 0;
+    if (key && place < k) {
+      a.alt_ids[row * k + place] = nan ? -1 : alt_id(key);
+      a.alt_logprobs[row * k + place] = nan ? r.log_s : log_prob(alt_value(key), r, a.scale);
     }
-    if (lane == 0) {
-      a.alt_ids[row * a.n_alt + i] = k && !nan ? alt_id(k) : -1;
-      a.alt_logprobs[row * a.n_alt + i] = nan ? r.log_s : k ? log_prob(alt_value(k), r, a.scale) : NEG_INF;
+    if (tid < k && tid >= some) {
+      a.alt_ids[row * k + tid] = -1;
+      a.alt_logprobs[row * k + tid] = nan ? r.log_s : NEG_INF;
     }
+    return;
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += SC_THREADS) {
+    const uint64_t key = lists[i];
+    if (key && key >= least) {
+      const int at = atomicAdd(&found, 1);
+      if (at < SC_CANDS) cands[at] = key;
+    }
+  }
+  __syncthreads();
+  // places by counting the better candidates; where there are too many to keep
+  // (rows that are masked in some parts), among all lists
+  const bool fits = found <= SC_CANDS;
+  const uint64_t* from = fits ? cands : lists;
+  const int total = fits ? found : n;
+  for (int i = tid; i < total; i += SC_THREADS) {
+    const uint64_t key = from[i];
+    if (key < least || key == 0) continue;
+    int place = 0;
+    for (int j = 0; j < total; j++) place += from[j] > key;
+    if (place >= k) continue;
+    a.alt_ids[row * k + place] = nan ? -1 : alt_id(key);
+    a.alt_logprobs[row * k + place] = nan ? r.log_s : log_prob(alt_value(key), r, a.scale);
+  }
+  if (tid >= found && tid < k) {
+    a.alt_ids[row * k + tid] = -1;
+    a.alt_logprobs[row * k + tid] = nan ? r.log_s : NEG_INF;
   }
 }
 
@@ -432,7 +529,8 @@ int run_scores(ScoreArgs<T> a, hipStream_t st) {
   if (launch(a.n_alt ? scores_kernel<T, true> : scores_kernel<T, false>, dim3((uint32_t)(a.rows * a.splits)),
              dim3(SC_THREADS), st, a) != hipSuccess)
     return TT_ERR_HIP;
-  if (a.splits > 1 && launch(scores_join_kernel<T>, dim3((uint32_t)a.rows), dim3(64), st, a) != hipSuccess) return TT_ERR_HIP;
+  if (a.splits > 1 && launch(scores_join_kernel<T>, dim3((uint32_t)a.rows), dim3(SC_THREADS), st, a) != hipSuccess)
+    return TT_ERR_HIP;
   return TT_OK;
 }
 
@@ -466,11 +564,12 @@ extern "C" int tt_token_scores(const void* logits, int32_t type, int64_t rows, i
   if (rows > (int64_t)UINT32_MAX / SC_THREADS) return TT_ERR_TOO_LARGE;
   if (rows == 0) return TT_OK;
   if (!logits || (need && !workspace) || (n_alt && (!alt_ids || !alt_logprobs))) return TT_ERR_NULL_ARG;
+  const int splits = scores_splits(rows, vocab);
   auto go = [&](auto zero) {
     using T = decltype(zero);
     return run_scores(ScoreArgs<T>{static_cast<const T*>(logits), rows, vocab, stride, scale, targets, logprobs, stats,
                                    entropy, n_alt, alt_ids, alt_logprobs, static_cast<uint8_t*>(workspace),
-                                   scores_splits(rows, vocab)},
+                                   splits, (vocab + splits - 1) / splits},
                       static_cast<hipStream_t>(stream));
   };
   return type == TT_F32 ? go(float{}) : type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});

@@ -12,36 +12,41 @@ to belong to the tensors' device, and return at once.  The C calls trust the sha
 so every shape, type and stride is checked here; a mismatch raises ``ValueError``.
 """
 
-import ctypes
+import functools
+import struct
 
 from . import _lib
 
-_TYPES = {"torch.float32": _lib.TT_F32, "torch.bfloat16": _lib.TT_BF16, "torch.float16": _lib.TT_F16}
+_NAMES = {"torch.float32": _lib.TT_F32, "torch.bfloat16": _lib.TT_BF16, "torch.float16": _lib.TT_F16, "torch.int32": "i32",
+          "torch.int64": "i64", "torch.uint8": "u8"}
+_F32, _I32, _I64, _U8 = _lib.TT_F32, "i32", "i64", "u8"
+_codes = {}  # dtype -> its code (the types' names are long to make)
 
 
-def _same_device(first, *others):
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("tensors are on different devices: %s and %s" % (first.device, t.device))
+def _code(dtype):
+    try:
+        return _codes[dtype]
+    except KeyError:
+        return _codes.setdefault(dtype, _NAMES.get(str(dtype)))
 
 
-def _flat(t, name, dtype, shape):
-    """Address of a contiguous device tensor of this type and shape; None for None."""
+def _flat(t, name, code, shape, device):
+    """Address of a contiguous tensor of this type and shape on this device; None for None."""
     if t is None:
         return None
-    if str(t.dtype) != dtype or tuple(t.shape) != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s device tensor of shape %s, not %s %s on %s"
-                         % (name, dtype, shape, t.dtype, tuple(t.shape), t.device))
+    if t.shape != shape or _code(t.dtype) != code or t.get_device() != device or device < 0 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s device tensor of shape %s, on device %d with the others, not %s %s on %s"
+                         % (name, {v: k for k, v in _NAMES.items()}[code], shape, device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
-def _matrix(t, name, dtype=None, shape=None):
+def _matrix(t, name, device, dtype=None, shape=None):
     """(address, row stride) of a device matrix whose rows are contiguous and do not overlap."""
-    if t.dim() != 2 or not t.is_cuda or (dtype is not None and t.dtype != dtype) or \
-            (shape is not None and tuple(t.shape) != shape):
-        raise ValueError("%s must be a device matrix%s%s, not %s %s on %s"
+    if t.dim() != 2 or t.get_device() != device or device < 0 or (dtype is not None and t.dtype != dtype) or \
+            (shape is not None and t.shape != shape):
+        raise ValueError("%s must be a device matrix%s%s, on device %d with the others, not %s %s on %s"
                          % (name, "" if dtype is None else " of %s" % dtype, "" if shape is None else " of shape %s" % (shape,),
-                            t.dtype, tuple(t.shape), t.device))
+                            device, t.dtype, tuple(t.shape), t.device))
     rows, cols = t.shape
     stride, step = t.stride()
     if cols > 1 and step != 1:
@@ -54,26 +59,36 @@ def _matrix(t, name, dtype=None, shape=None):
 
 
 def _type_of(t, name, allowed):
-    code = _TYPES.get(str(t.dtype))
+    code = _code(t.dtype)
     if code not in allowed:
         raise ValueError("%s has type %s, which this call does not take" % (name, t.dtype))
     return code
 
 
-def _room(workspace, need):
-    if need <= 0 and workspace is None:
+def _room(workspace, need, device):
+    if workspace is None:
+        if need > 0:
+            raise ValueError("a workspace of %d bytes is needed" % need)
         return None, 0
-    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous() or str(workspace.dtype) != "torch.uint8":
-        raise ValueError("workspace must be a contiguous uint8 device tensor of at least %d bytes" % need)
-    if workspace.numel() < need or workspace.data_ptr() % 256:
-        raise ValueError("workspace must hold %d bytes, aligned to 256: it has %d" % (need, workspace.numel()))
-    return workspace.data_ptr(), workspace.numel()
+    if _code(workspace.dtype) != _U8 or workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on device %d" % device)
+    size, p = workspace.numel(), workspace.data_ptr()
+    if size < need or p % 256:
+        raise ValueError("workspace must hold %d bytes, aligned to 256: it has %d" % (need, size))
+    return p, size
 
 
-def _need(size):
+@functools.lru_cache(maxsize=256)
+def _need(name, *sizes):
+    """A workspace size: a function of sizes alone."""
+    size = getattr(_lib.load(), name)(*sizes)
     if size < 0:
-        raise _lib.TokTierError(int(size), "workspace size")
+        raise _lib.TokTierError(int(size), name)
     return int(size)
+
+
+# tt_step, packed as the compiler lays it out
+_STEP = struct.Struct("@iii4xqqq15P")
 
 
 def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets, lengths, pages, slots, positions, requests,
@@ -87,27 +102,29 @@ def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets,
     token, as many as the step may hold; ``result`` (int64, two entries) receives the number of
     tokens and the free pages left, or a negative error code and the count as it was.
     """
-    n, room = len(cached), len(slots)
-    _same_device(cached, fresh, tables, free_pages, free_count, offsets, lengths, pages, slots, positions, requests, result,
-                 held, ids, targets)
-    table, stride = _matrix(tables, "tables")
-    if str(tables.dtype) != "torch.int32" or tables.shape[0] != n:
+    d, each, room, free = cached.get_device(), cached.shape, slots.shape, free_pages.shape
+    n = each[0]
+    table, stride = _matrix(tables, "tables", d)
+    width = tables.shape[1]
+    if _code(tables.dtype) != _I32 or tables.shape[0] != n:
         raise ValueError("tables must be an int32 matrix of %d rows, not %s %s" % (n, tables.dtype, tuple(tables.shape)))
-    i32, i64 = "torch.int32", "torch.int64"
-    step = _lib.Step(n, page_size, tables.shape[1], stride, room, len(free_pages),
-                     _flat(cached, "cached", i32, (n,)), _flat(fresh, "fresh", i32, (n,)), _flat(held, "held", i32, (n,)),
-                     _flat(ids, "ids", i32, (room,)), _flat(free_pages, "free_pages", i32, (len(free_pages),)),
-                     _flat(free_count, "free_count", i64, (1,)), table, _flat(offsets, "offsets", i32, (n + 1,)),
-                     _flat(lengths, "lengths", i32, (n,)), _flat(pages, "pages", i32, (n,)),
-                     _flat(slots, "slots", i64, (room,)), _flat(positions, "positions", i32, (room,)),
-                     _flat(requests, "requests", i32, (room,)), _flat(targets, "targets", i32, (room,)),
-                     _flat(result, "result", i64, (2,)))
-    _lib.check(_lib.load().tt_step_plan(ctypes.byref(step), stream), "tt_step_plan")
+    if len(each) != 1 or len(room) != 1 or len(free) != 1:
+        raise ValueError("cached, slots and free_pages must have one dimension")
+    step = _STEP.pack(
+        n, page_size, width, stride, room[0], free[0], _flat(cached, "cached", _I32, each, d) or 0,
+        _flat(fresh, "fresh", _I32, each, d) or 0, _flat(held, "held", _I32, each, d) or 0,
+        _flat(ids, "ids", _I32, room, d) or 0, _flat(free_pages, "free_pages", _I32, free, d) or 0,
+        _flat(free_count, "free_count", _I64, (1,), d) or 0, table or 0, _flat(offsets, "offsets", _I32, (n + 1,), d) or 0,
+        _flat(lengths, "lengths", _I32, each, d) or 0, _flat(pages, "pages", _I32, each, d) or 0,
+        _flat(slots, "slots", _I64, room, d) or 0, _flat(positions, "positions", _I32, room, d) or 0,
+        _flat(requests, "requests", _I32, room, d) or 0, _flat(targets, "targets", _I32, room, d) or 0,
+        _flat(result, "result", _I64, (2,), d) or 0)
+    _lib.check(_lib.load().tt_step_plan(step, stream), "tt_step_plan")
 
 
 def token_scores_workspace(rows, vocab, n_alt=0) -> int:
     """``tt_token_scores_workspace``: bytes of workspace that ``token_scores`` needs (0: none)."""
-    return _need(_lib.load().tt_token_scores_workspace(rows, vocab, n_alt))
+    return _need("tt_token_scores_workspace", rows, vocab, n_alt)
 
 
 def token_scores(logits, targets, logprobs=None, stats=None, entropy=None, alt_ids=None, alt_logprobs=None, scale=1.0,
@@ -118,48 +135,46 @@ def token_scores(logits, targets, logprobs=None, stats=None, entropy=None, alt_i
     (float32 [rows, 2]) and ``alt_ids`` (int32), ``alt_logprobs`` (float32) [rows, k] for the ``k``
     best alternatives; outputs that are None are not computed.
     """
-    p, stride = _matrix(logits, "logits")
+    d = logits.get_device()
+    p, stride = _matrix(logits, "logits", d)
     kind = _type_of(logits, "logits", (0, 1, 2))
     rows, vocab = logits.shape
-    _same_device(logits, targets, logprobs, stats, entropy, alt_ids, alt_logprobs, workspace)
     if (alt_ids is None) != (alt_logprobs is None):
         raise ValueError("alt_ids and alt_logprobs come together")
-    k = 0 if alt_ids is None else int(alt_ids.shape[-1])
-    f32 = "torch.float32"
-    lib = _lib.load()
-    room, size = _room(workspace, _need(lib.tt_token_scores_workspace(rows, vocab, k)))
-    _lib.check(lib.tt_token_scores(
-        p, kind, rows, vocab, stride, scale, _flat(targets, "targets", "torch.int32", (rows,)),
-        _flat(logprobs, "logprobs", f32, (rows,)), _flat(stats, "stats", f32, (rows, 2)),
-        _flat(entropy, "entropy", f32, (rows,)), k, _flat(alt_ids, "alt_ids", "torch.int32", (rows, k)),
-        _flat(alt_logprobs, "alt_logprobs", f32, (rows, k)), room, size, stream), "tt_token_scores")
+    k = 0 if alt_ids is None else alt_ids.shape[-1]
+    room, size = _room(workspace, _need("tt_token_scores_workspace", rows, vocab, k), d)
+    _lib.check(_lib.load().tt_token_scores(
+        p, kind, rows, vocab, stride, scale, _flat(targets, "targets", _I32, (rows,), d),
+        _flat(logprobs, "logprobs", _F32, (rows,), d), _flat(stats, "stats", _F32, (rows, 2), d),
+        _flat(entropy, "entropy", _F32, (rows,), d), k, _flat(alt_ids, "alt_ids", _I32, (rows, k), d),
+        _flat(alt_logprobs, "alt_logprobs", _F32, (rows, k), d), room, size, stream), "tt_token_scores")
 
 
 def token_scores_grad(logits, targets, stats, entropy, grad_logprobs, grad_entropy, grad_logits, scale=1.0, stream=None):
     """``tt_token_scores_grad``: gradient with respect to the logits, into ``grad_logits`` (the
     logits' type and shape; may be the logits).  ``targets``, ``grad_logprobs`` and ``grad_entropy``
     may be None; ``entropy`` may be None with ``grad_entropy``."""
-    p, stride = _matrix(logits, "logits")
+    d = logits.get_device()
+    p, stride = _matrix(logits, "logits", d)
     kind = _type_of(logits, "logits", (0, 1, 2))
     rows, vocab = logits.shape
-    q, grad_stride = _matrix(grad_logits, "grad_logits", logits.dtype, (rows, vocab))
-    _same_device(logits, targets, stats, entropy, grad_logprobs, grad_entropy, grad_logits)
-    f32 = "torch.float32"
+    q, grad_stride = _matrix(grad_logits, "grad_logits", d, logits.dtype, (rows, vocab))
+    one = (rows,)
     _lib.check(_lib.load().tt_token_scores_grad(
-        p, kind, rows, vocab, stride, scale, _flat(targets, "targets", "torch.int32", (rows,)),
-        _flat(stats, "stats", f32, (rows, 2)), _flat(entropy, "entropy", f32, (rows,)),
-        _flat(grad_logprobs, "grad_logprobs", f32, (rows,)), _flat(grad_entropy, "grad_entropy", f32, (rows,)),
+        p, kind, rows, vocab, stride, scale, _flat(targets, "targets", _I32, one, d),
+        _flat(stats, "stats", _F32, (rows, 2), d), _flat(entropy, "entropy", _F32, one, d),
+        _flat(grad_logprobs, "grad_logprobs", _F32, one, d), _flat(grad_entropy, "grad_entropy", _F32, one, d),
         q, grad_stride, stream), "tt_token_scores_grad")
 
 
 def head_scores_workspace(rows, vocab, width) -> int:
     """``tt_head_scores_workspace``: bytes of workspace that ``head_scores`` needs."""
-    return _need(_lib.load().tt_head_scores_workspace(rows, vocab, width))
+    return _need("tt_head_scores_workspace", rows, vocab, width)
 
 
-def _head(hidden, weight):
-    h, h_stride = _matrix(hidden, "hidden")
-    w, w_stride = _matrix(weight, "weight", hidden.dtype)
+def _head(hidden, weight, device):
+    h, h_stride = _matrix(hidden, "hidden", device)
+    w, w_stride = _matrix(weight, "weight", device, hidden.dtype)
     kind = _type_of(hidden, "hidden", (1, 2))
     if weight.shape[1] != hidden.shape[1]:
         raise ValueError("hidden has rows of %d entries, weight of %d" % (hidden.shape[1], weight.shape[1]))
@@ -169,36 +184,34 @@ def _head(hidden, weight):
 def head_scores(hidden, weight, targets, logprobs=None, stats=None, entropy=None, scale=1.0, workspace=None, stream=None):
     """``tt_head_scores``: the scores of ``hidden @ weight.T`` (bfloat16 or float16) without storing it;
     arguments as those of ``token_scores``."""
-    head = _head(hidden, weight)
+    d = hidden.get_device()
+    head = _head(hidden, weight, d)
     rows, vocab, width = head[5:]
-    _same_device(hidden, weight, targets, logprobs, stats, entropy, workspace)
-    f32 = "torch.float32"
-    lib = _lib.load()
-    room, size = _room(workspace, _need(lib.tt_head_scores_workspace(rows, vocab, width)))
-    _lib.check(lib.tt_head_scores(
-        *head, scale, _flat(targets, "targets", "torch.int32", (rows,)), _flat(logprobs, "logprobs", f32, (rows,)),
-        _flat(stats, "stats", f32, (rows, 2)), _flat(entropy, "entropy", f32, (rows,)), room, size, stream), "tt_head_scores")
+    room, size = _room(workspace, _need("tt_head_scores_workspace", rows, vocab, width), d)
+    _lib.check(_lib.load().tt_head_scores(
+        *head, scale, _flat(targets, "targets", _I32, (rows,), d), _flat(logprobs, "logprobs", _F32, (rows,), d),
+        _flat(stats, "stats", _F32, (rows, 2), d), _flat(entropy, "entropy", _F32, (rows,), d), room, size, stream),
+        "tt_head_scores")
 
 
 def head_scores_grad_workspace(rows, vocab, width, ample=True) -> int:
     """``tt_head_scores_grad_workspace``: the least bytes of workspace, or (``ample``) those up to
     which more room helps."""
-    return _need(_lib.load().tt_head_scores_grad_workspace(rows, vocab, width, int(bool(ample))))
+    return _need("tt_head_scores_grad_workspace", rows, vocab, width, 1 if ample else 0)
 
 
 def head_scores_grad(hidden, weight, targets, stats, entropy, grad_logprobs, grad_entropy, grad_hidden, grad_weight,
                      scale=1.0, workspace=None, stream=None):
     """``tt_head_scores_grad``: gradients with respect to ``hidden`` and ``weight`` (either output may
     be None); the other arguments as those of ``token_scores_grad``."""
-    head = _head(hidden, weight)
+    d = hidden.get_device()
+    head = _head(hidden, weight, d)
     rows, vocab, width = head[5:]
-    _same_device(hidden, weight, targets, stats, entropy, grad_logprobs, grad_entropy, grad_hidden, grad_weight, workspace)
-    gh = (None, width) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", hidden.dtype, (rows, width))
-    gw = (None, width) if grad_weight is None else _matrix(grad_weight, "grad_weight", hidden.dtype, (vocab, width))
-    f32 = "torch.float32"
-    lib = _lib.load()
-    room, size = _room(workspace, _need(lib.tt_head_scores_grad_workspace(rows, vocab, width, 0)))
-    _lib.check(lib.tt_head_scores_grad(
-        *head, scale, _flat(targets, "targets", "torch.int32", (rows,)), _flat(stats, "stats", f32, (rows, 2)),
-        _flat(entropy, "entropy", f32, (rows,)), _flat(grad_logprobs, "grad_logprobs", f32, (rows,)),
-        _flat(grad_entropy, "grad_entropy", f32, (rows,)), *gh, *gw, room, size, stream), "tt_head_scores_grad")
+    gh = (None, width) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", d, hidden.dtype, (rows, width))
+    gw = (None, width) if grad_weight is None else _matrix(grad_weight, "grad_weight", d, hidden.dtype, (vocab, width))
+    one = (rows,)
+    room, size = _room(workspace, _need("tt_head_scores_grad_workspace", rows, vocab, width, 0), d)
+    _lib.check(_lib.load().tt_head_scores_grad(
+        *head, scale, _flat(targets, "targets", _I32, one, d), _flat(stats, "stats", _F32, (rows, 2), d),
+        _flat(entropy, "entropy", _F32, one, d), _flat(grad_logprobs, "grad_logprobs", _F32, one, d),
+        _flat(grad_entropy, "grad_entropy", _F32, one, d), *gh, *gw, room, size, stream), "tt_head_scores_grad")

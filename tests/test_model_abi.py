@@ -36,6 +36,14 @@ def test_step_matches_the_header():
     assert [(n, t) for n, t in _lib.Step._fields_] == want
 
 
+def test_packed_step_is_the_struct():
+    from paper_2607_29678_amd import model
+
+    values = list(range(1, 22))
+    step = _lib.Step.from_buffer_copy(model._STEP.pack(*values))
+    assert [getattr(step, n) for n, _ in _lib.Step._fields_] == values
+
+
 def _step(**change):
     s = _lib.Step(4, 16, 10, 10, 64, 100, *range(P, P + 15 * 64, 64))
     for k, v in change.items():
