@@ -546,8 +546,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
     const Part q = parts[row * n_parts + i];
     st = join(st, Stats{q.m, q.s, q.u}, c);
   }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
+  st = wave_join(st, c);
   if (lane) return;
   const RowScores r = row_scores(st, c);
   const int32_t t = targets ? targets[row] : -1;

@@ -79,8 +79,18 @@ __device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
   return {m, a.s + b.s, a.u + b.u};
 }
 
-__device__ __forceinline__ Stats shuffled_xor(const Stats& a, int lane_mask) {
-  return {__shfl_xor(a.m, lane_mask), __shfl_xor(a.s, lane_mask), __shfl_xor(a.u, lane_mask)};
+// The wave's statistics in every lane: one move to the wave's maximum, then sums.
+__device__ __forceinline__ Stats wave_join(Stats a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) m = larger(m, __shfl_xor(m, d));
+  lower(a, m, c);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    a.s += __shfl_xor(a.s, d);
+    a.u += __shfl_xor(a.u, d);
+  }
+  return a;
 }
 
 // A row's results from the statistics of the whole row.

@@ -20,6 +20,11 @@ constexpr int SC_SPLIT_COLS = 2048;  // fewest columns of a part of a row
 constexpr int SC_MAX_SPLITS = 64;  // parts of a row: one list per lane when they are joined
 constexpr int64_t SC_BLOCKS = 1024;  // blocks that fill the chip (4 per compute unit)
 
+// Many short rows: a wave takes a row, and the reductions at a row's end are one
+// wave's (8,192 rows of 8,449 in bf16: 29 us against 39 with a block a row, with
+// 20 alternatives 52 against 61; at 16,384 entries 47 against 49, at 32,000 alike).
+constexpr int64_t WAVE_ROWS = 2048, WAVE_VOCAB = 16384;
+
 // Parts of a row that several blocks take: one block takes a row whole where there are rows enough.
 int scores_splits(int64_t rows, int64_t vocab) {
   if (rows <= 0 || rows >= SC_BLOCKS) return 1;
@@ -54,10 +59,14 @@ struct Vec {
   T v[N];
 };
 template <class T>
-__device__ __forceinline__ Vec<T> load_vec(const T* p) {
-  Vec<T> r;
-  __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T)), 16);
-  return r;
+__device__ __forceinline__ Vec<T> load_vec(const T* p) {  // of any alignment
+  using U4 = __attribute__((ext_vector_type(4), aligned(2))) uint32_t;
+  return __builtin_bit_cast(Vec<T>, (__attribute__((ext_vector_type(4))) uint32_t)__builtin_nontemporal_load(reinterpret_cast<const U4*>(p)));
+}
+template <class T>
+__device__ __forceinline__ void store_vec_once(T* p, const Vec<T>& v) {
+  using U4 = __attribute__((ext_vector_type(4))) uint32_t;
+  __builtin_nontemporal_store(__builtin_bit_cast(U4, v), reinterpret_cast<U4*>(p));
 }
 // Aligned, and not kept in the caches: a row is read once (7.1 TB/s on reads of
 // 4 GiB against 6.3 with ordinary loads).
@@ -97,33 +106,39 @@ struct ScoreArgs {
   int64_t per_part;  // columns of a part
 };
 
+template <int THREADS>
 struct SumShared {
-  Stats st[SC_THREADS / 64];
+  Stats st[THREADS / 64];
 };
-struct ScoreShared : SumShared {
-  float maxima[SC_THREADS];
-  alignas(16) uint8_t vec[SC_THREADS / 64][SC_VECS][16];
-  uint32_t vec_at[SC_THREADS / 64][SC_VECS];
-  uint64_t cands[SC_CANDS];
+template <int THREADS>
+struct ScoreShared : SumShared<THREADS> {
+  float maxima[THREADS];
+  alignas(16) uint8_t vec[THREADS / 64][SC_VECS][16];
+  uint32_t vec_at[THREADS / 64][SC_VECS];
+  alignas(16) uint64_t cands[SC_CANDS];
   uint64_t best[TT_MAX_ALTERNATIVES];
   float bound;
-  int n_vecs[SC_THREADS / 64], n_cands;
+  int n_vecs[THREADS / 64], n_cands;
 };
 
 __device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(alt_key(x, 0) >> 32); }
 
 // A value that at least n_alt entries seen so far reach, from the threads'
-// running maxima: the n_alt-th largest of 128 maxima of two threads each, found
-// bit by bit (in order of values, down to LOWEST) in one wave.  -inf where fewer
+// running maxima: the n_alt-th largest of 128 maxima of two threads each (of 64
+// threads: of their own), found bit by bit (in order of values, down to LOWEST) in one wave.  -inf where fewer
 // than n_alt of them are larger.
-template <uint32_t LOWEST>
-__device__ __forceinline__ float bound_of(float mine, int n_alt, ScoreShared& sh) {
+template <uint32_t LOWEST, int THREADS>
+__device__ __forceinline__ float bound_of(float mine, int n_alt, ScoreShared<THREADS>& sh) {
   const int tid = threadIdx.x;
   sh.maxima[tid] = mine;
   __syncthreads();
   if (tid < 64) {
-    const uint32_t a = ordered(fmaxf(sh.maxima[tid], sh.maxima[tid + 64]));
-    const uint32_t b = ordered(fmaxf(sh.maxima[tid + 128], sh.maxima[tid + 192]));
+    static_assert(THREADS == 64 || THREADS == 256, "one or four maxima a lane");
+    uint32_t a = ordered(sh.maxima[tid]), b = 0;
+    if constexpr (THREADS == 256) {
+      a = ordered(fmaxf(sh.maxima[tid], sh.maxima[tid + 64]));
+      b = ordered(fmaxf(sh.maxima[tid + 128], sh.maxima[tid + 192]));
+    }
     uint32_t key = 0;
 #pragma unroll
     for (uint32_t bit = 0x80000000u; bit >= LOWEST; bit >>= 1) {
@@ -137,12 +152,28 @@ __device__ __forceinline__ float bound_of(float mine, int n_alt, ScoreShared& sh
   return sh.bound;
 }
 
+// How many of the n keys are better; zeros up to a multiple of 8 follow them.
+__device__ __forceinline__ int better(const uint64_t* keys, int n, uint64_t key) {
+  using U64x2 = __attribute__((ext_vector_type(2))) uint64_t;
+  int count = 0;
+  for (int j = 0; j < n; j += 8) {
+    U64x2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) q[i] = *reinterpret_cast<const U64x2*>(keys + j + 2 * i);
+#pragma unroll
+    for (int i = 0; i < 4; i++) count += (q[i][0] > key) + (q[i][1] > key);
+  }
+  return count;
+}
+
 // Orders the n candidates by counting the better ones (keys are distinct).
-__device__ __forceinline__ void order_candidates(int n, int n_alt, ScoreShared& sh) {
-  for (int i = threadIdx.x; i < n; i += SC_THREADS) {
+template <int THREADS>
+__device__ __forceinline__ void order_candidates(int n, int n_alt, ScoreShared<THREADS>& sh) {
+  if (threadIdx.x < 8 && n + threadIdx.x < SC_CANDS) sh.cands[n + threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += THREADS) {
     const uint64_t k = sh.cands[i];
-    int place = 0;
-    for (int j = 0; j < n; j++) place += sh.cands[j] > k;
+    const int place = better(sh.cands, n, k);
     if (place < n_alt) sh.best[place] = k;
   }
 }
@@ -152,13 +183,14 @@ __device__ __forceinline__ void order_candidates(int n, int n_alt, ScoreShared& 
 //  - Entries above the bound are collected again; if that falls short of n_alt,
 //    equal entries (masks of a finite value) follow in order of their IDs.
 //  - Should even the entries above it not fit, places are filled one by one.
-template <class T>
-__device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, int n_alt, float mine, ScoreShared& sh) {
+template <class T, int THREADS>
+__device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, int n_alt, float mine,
+                                           ScoreShared<THREADS>& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const float bound = bound_of<1u>(mine, n_alt, sh);
+  const float bound = bound_of<1u, THREADS>(mine, n_alt, sh);
   if (tid == 0) sh.n_cands = 0;
   __syncthreads();
-  for (int64_t j = tid; j < sp.n; j += SC_THREADS) {
+  for (int64_t j = tid; j < sp.n; j += THREADS) {
     const float x = (float)sp.p[j];
     if (x > bound) {
       const int at = atomicAdd(&sh.n_cands, 1);
@@ -170,7 +202,7 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
   if (n <= SC_CANDS) {
     order_candidates(n, n_alt, sh);
     int have = n;
-    for (int64_t j0 = 0; j0 < sp.n && have < n_alt && bound > NEG_INF; j0 += SC_THREADS) {
+    for (int64_t j0 = 0; j0 < sp.n && have < n_alt && bound > NEG_INF; j0 += THREADS) {
       const int64_t j = j0 + tid;
       const bool tie = j < sp.n && (float)sp.p[j] == bound;
       const uint64_t votes = __ballot(tie);
@@ -178,7 +210,7 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
       if (lane == 0) sh.maxima[wave] = (float)__popcll(votes);
       __syncthreads();
       int at = have + __popcll(votes & ((1ull << lane) - 1ull));
-      for (int w = 0; w < SC_THREADS / 64; w++) {
+      for (int w = 0; w < THREADS / 64; w++) {
         if (w < wave) at += (int)sh.maxima[w];
         have += (int)sh.maxima[w];
       }
@@ -190,7 +222,7 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
   uint64_t last = ~0ull;
   for (int r = 0; r < n_alt; r++) {
     uint64_t k = 0;  // the thread's best key below the last one
-    for (int64_t j = tid; j < sp.n; j += SC_THREADS) {
+    for (int64_t j = tid; j < sp.n; j += THREADS) {
       const uint64_t q = alt_key((float)sp.p[j], first + (uint32_t)j);
       if (q < last && q > k) k = q;
     }
@@ -203,16 +235,16 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
     if (lane == 0) sh.cands[wave] = k;
     __syncthreads();
     last = sh.cands[0];
-    for (int w = 1; w < SC_THREADS / 64; w++) last = sh.cands[w] > last ? sh.cands[w] : last;
+    for (int w = 1; w < THREADS / 64; w++) last = sh.cands[w] > last ? sh.cands[w] : last;
     if (tid == 0) sh.best[r] = last;
   }
   __syncthreads();
 }
 
 // One part of one row per block.
-template <class T, bool ALT>
-__global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
-  __shared__ std::conditional_t<ALT, ScoreShared, SumShared> sh;
+template <class T, bool ALT, int THREADS>
+__global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
+  __shared__ std::conditional_t<ALT, ScoreShared<THREADS>, SumShared<THREADS>> sh;
   constexpr int N = Vec<T>::N, U = ALT ? 2 : 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t row32 = blockIdx.x / (uint32_t)a.splits, part = blockIdx.x - row32 * (uint32_t)a.splits;
@@ -238,14 +270,14 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
   // often in every thread: it holds barriers.  The vectors of the next step are
   // under way while the last ones are summed; in the last step a thread repeats
   // the last vector where it has none, and takes it for -inf.
-  constexpr int STEP = U * SC_THREADS;
+  constexpr int STEP = U * THREADS;
   const int vecs = (int)sp.vecs, steps = (vecs + STEP - 1) / STEP;
   const T* body = p + sp.head;
   Vec<T> y[U];
   auto fetch = [&](int step) {
 #pragma unroll
     for (int k = 0; k < U; k++) {
-      const int v = step * STEP + k * SC_THREADS + tid;
+      const int v = step * STEP + k * THREADS + tid;
       y[k] = load_vec_once(body + (int64_t)(v < vecs ? v : vecs - 1) * N);
     }
   };
@@ -262,8 +294,8 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
 #pragma unroll
     for (int k = 0; k < U; k++) {
       top[k] = NEG_INF;
-      if (!WHOLE && k * SC_THREADS >= here) continue;  // (the same for every thread)
-      if (!WHOLE && k * SC_THREADS + tid >= here) {
+      if (!WHOLE && k * THREADS >= here) continue;  // (the same for every thread)
+      if (!WHOLE && k * THREADS + tid >= here) {
 #pragma unroll
         for (int i = 0; i < N; i++) x[k][i] = NEG_INF;
       }
@@ -277,7 +309,7 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
     auto sums = [&](auto plain) {
 #pragma unroll
       for (int k = 0; k < U; k++) {
-        if (!WHOLE && k * SC_THREADS >= here) continue;
+        if (!WHOLE && k * THREADS >= here) continue;
 #pragma unroll
         for (int i = 0; i < N; i++) add_entry<decltype(plain)::value>(st, x[k][i], ref, c);
       }
@@ -285,7 +317,7 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
     if (__ballot(!is_plain(m, c)) == 0) sums(std::true_type{});
     else sums(std::false_type{});
     if constexpr (ALT) {
-      if ((step & (step + 1)) == 0) bound = bound_of<0x10000u>(st.m, a.n_alt, sh);  // after 1, 2, 4, 8 ... steps
+      if ((step & (step + 1)) == 0) bound = bound_of<0x10000u, THREADS>(st.m, a.n_alt, sh);  // after 1, 2, 4, 8 ... steps
 #pragma unroll
       for (int k = 0; k < U; k++) {
         const bool mine = top[k] >= bound && top[k] > NEG_INF;
@@ -297,7 +329,7 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
 #pragma unroll
           for (int i = 0; i < N; i++) z.v[i] = (T)x[k][i];
           __builtin_memcpy(sh.vec[wave][at], &z, 16);
-          sh.vec_at[wave][at] = (uint32_t)(sp.head + (int64_t)(v + k * SC_THREADS) * N);
+          sh.vec_at[wave][at] = (uint32_t)(sp.head + (int64_t)(v + k * THREADS) * N);
         }
         n_vecs += __popcll(votes);
       }
@@ -314,16 +346,17 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
   if (tid < sp.head) edge(tid);
   if (sp.tail + tid < sp.n) edge(sp.tail + tid);
   const float mine = st.m;
+  st = wave_join(st, c);
+  if constexpr (THREADS > 64) {
+    if (lane == 0) sh.st[wave] = st;
+    __syncthreads();
+    st = sh.st[0];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);
-  if (lane == 0) sh.st[wave] = st;
-  __syncthreads();
-  st = sh.st[0];
-#pragma unroll
-  for (int w = 1; w < SC_THREADS / 64; w++) st = join(st, sh.st[w], c);
+    for (int w = 1; w < THREADS / 64; w++) st = join(st, sh.st[w], c);
+  }
 
   if constexpr (ALT) {
-    if (steps == 0) bound = bound_of<0x10000u>(mine, a.n_alt, sh);
+    if (steps == 0) bound = bound_of<0x10000u, THREADS>(mine, a.n_alt, sh);
     auto keep = [&](float x, uint32_t j) {
       if (x >= bound && x > NEG_INF) {
         const int at = atomicAdd(&sh.n_cands, 1);
@@ -343,7 +376,7 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
     const int n = sh.n_cands;
     bool fits = n <= SC_CANDS;
 #pragma unroll
-    for (int w = 0; w < SC_THREADS / 64; w++) fits &= sh.n_vecs[w] <= SC_VECS;
+    for (int w = 0; w < THREADS / 64; w++) fits &= sh.n_vecs[w] <= SC_VECS;
     if (fits) {
       order_candidates(n, a.n_alt, sh);
       __syncthreads();
@@ -382,34 +415,24 @@ __global__ __launch_bounds__(SC_THREADS) void scores_kernel(ScoreArgs<T> a) {
 // entries reach the least of their entries of one place; those are ordered.
 template <class T>
 __global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a) {
-  __shared__ uint64_t lists[SC_MAX_SPLITS * TT_MAX_ALTERNATIVES];  // [splits][n_alt]
-  __shared__ uint64_t cands[SC_CANDS];
+  __shared__ __align__(16) uint64_t lists[SC_MAX_SPLITS * TT_MAX_ALTERNATIVES];  // [splits][n_alt]
+  __shared__ __align__(16) uint64_t cands[SC_CANDS];
   __shared__ uint64_t least;
   __shared__ int found;
   const int64_t row = blockIdx.x;
-  const int tid = threadIdx.x, k = a.n_alt, n = a.splits * k;
+  const int tid = threadIdx.x, lane = tid & 63, k = a.n_alt, n = a.splits * k;
   const float c = a.scale * LOG2E;
   const uint8_t* in = a.parts + row * a.splits * part_bytes(k);
   PartHead head = {empty_stats(), 0.f};
-  if ((tid & 63) < a.splits) head = *reinterpret_cast<const PartHead*>(in + (tid & 63) * part_bytes(k));
+  if (lane < a.splits) head = *reinterpret_cast<const PartHead*>(in + lane * part_bytes(k));
   const int32_t t = a.targets ? a.targets[row] : -1;
-  if (tid == 0) {
-    least = ~0ull;
-    found = 0;
-  }
-  if (k) {
-    for (int i = tid; i < n; i += SC_THREADS) {
-      const int part = i / k;
-      lists[i] = reinterpret_cast<const uint64_t*>(in + part * part_bytes(k) + sizeof(PartHead))[i - part * k];
-    }
-    __syncthreads();
-    const int level = (k + a.splits - 1) / a.splits - 1;  // every list's entry of this place: n_alt entries reach the least
-    if (n > SC_THREADS && tid < a.splits) atomicMin(reinterpret_cast<unsigned long long*>(&least), (unsigned long long)lists[tid * k + level]);
+  if (tid == 0) found = 0;
+  for (int i = tid; i < ((n + 7) & ~7); i += SC_THREADS) {
+    const int part = i / (k ? k : 1);
+    lists[i] = i < n ? reinterpret_cast<const uint64_t*>(in + part * part_bytes(k) + sizeof(PartHead))[i - part * k] : 0;
   }
   const float x_given = __shfl(head.given, t >= 0 && t < a.vocab ? (int)(t / a.per_part) : 0);
-  Stats st = head.st;
-#pragma unroll
-  for (int d = 32; d; d >>= 1) st = join(st, shuffled_xor(st, d), c);  // (every wave for itself)
+  const Stats st = wave_join(head.st, c);  // (every wave for itself)
   const RowScores r = row_scores(st, c);
   const bool nan = r.log_s != r.log_s;
   if (tid == 0) {
@@ -421,22 +444,16 @@ __global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a)
     if (a.entropy) a.entropy[row] = r.entropy;
   }
   if (!k) return;
-  if (n <= SC_THREADS) {  // all of them are ordered
-    const uint64_t key = tid < n ? lists[tid] : 0;
-    int place = 0, some = 0;
-    for (int j = 0; j < n; j++) {
-      place += lists[j] > key;
-      some += lists[j] != 0;
+  __syncthreads();
+  if (tid < 64) {
+    const int level = (k + a.splits - 1) / a.splits - 1;  // every list's entry of this place: n_alt entries reach the least
+    uint64_t low = lane < a.splits ? lists[lane * k + level] : ~0ull;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+      const uint64_t o = __shfl_xor(low, d);
+      low = o < low ? o : low;
     }
-    if (key && place < k) {
-      a.alt_ids[row * k + place] = nan ? -1 : alt_id(key);
-      a.alt_logprobs[row * k + place] = nan ? r.log_s : log_prob(alt_value(key), r, a.scale);
-    }
-    if (tid < k && tid >= some) {
-      a.alt_ids[row * k + tid] = -1;
-      a.alt_logprobs[row * k + tid] = nan ? r.log_s : NEG_INF;
-    }
-    return;
+    if (tid == 0) least = low;
   }
   __syncthreads();
   for (int i = tid; i < n; i += SC_THREADS) {
@@ -450,13 +467,13 @@ __global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a)
   // places by counting the better candidates; where there are too many to keep
   // (rows that are masked in some parts), among all lists
   const bool fits = found <= SC_CANDS;
-  const uint64_t* from = fits ? cands : lists;
   const int total = fits ? found : n;
+  if (fits && tid < 8 && found + tid < SC_CANDS) cands[found + tid] = 0;
+  __syncthreads();
   for (int i = tid; i < total; i += SC_THREADS) {
-    const uint64_t key = from[i];
+    const uint64_t key = fits ? cands[i] : lists[i];
     if (key < least || key == 0) continue;
-    int place = 0;
-    for (int j = 0; j < total; j++) place += from[j] > key;
+    const int place = fits ? better(cands, total, key) : better(lists, total, key);
     if (place >= k) continue;
     a.alt_ids[row * k + place] = nan ? -1 : alt_id(key);
     a.alt_logprobs[row * k + place] = nan ? r.log_s : log_prob(alt_value(key), r, a.scale);
@@ -467,67 +484,82 @@ __global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a)
   }
 }
 
-// Gradient: every entry is read once and written once.  A block takes up to
-// GR_COLS columns of a row; the stores are aligned, the loads may not be.
+// Gradient: every entry is read once and written once.  A block takes a run of
+// steps of one row, the next step's vectors under way while it writes the last;
+// the stores are aligned, the loads may not be.
 constexpr int GR_U = 4;
+constexpr int64_t GR_BLOCKS = 4096;  // blocks wanted: two rounds of eight a compute unit
 template <class T>
-constexpr int64_t grad_cols() { return (int64_t)SC_THREADS * Vec<T>::N * GR_U; }
+constexpr int64_t grad_step() { return (int64_t)SC_THREADS * Vec<T>::N * GR_U; }
 
 template <class T>
 struct GradArgs {
   const T* logits;
   T* grad;
   int64_t rows, vocab, stride, grad_stride;
-  int64_t chunks;  // blocks per row
   float scale;
   const int32_t* targets;
   const float *stats, *entropy, *grad_logprobs, *grad_entropy;
+  int chunks, steps;  // blocks of a row, steps of a block
 };
 
 template <class T>
 __global__ __launch_bounds__(SC_THREADS) void scores_grad_kernel(GradArgs<T> a) {
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, STEP = SC_THREADS * GR_U;
   const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  const uint32_t row32 = blockIdx.x / (uint32_t)a.chunks, chunk = blockIdx.x - row32 * (uint32_t)a.chunks;
+  const int64_t row = row32;
   const T* in = a.logits + row * a.stride;
-  const Span<T> sp(a.grad + row * a.grad_stride, a.vocab);
   T* out = a.grad + row * a.grad_stride;
+  const Span<T> sp(out, a.vocab);
+  const int vecs = (int)sp.vecs;
+  int v = (int)chunk * a.steps * STEP + tid;
+  Vec<T> y[GR_U];
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < GR_U; k++)
+      if (first + k * SC_THREADS < vecs) y[k] = load_vec(in + sp.head + (int64_t)(first + k * SC_THREADS) * N);
+  };
+  fetch(v);
   const RowGrad g = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, row, a.vocab, a.scale);
   const float c = a.scale * LOG2E;
   auto one = [&](float x, bool given) {
     if (g.zero) return (T)0.f;
-    const float y = grad_of(x, c, g);
-    return (T)(given ? y + g.g : y);
+    const float z = grad_of(x, c, g);
+    return (T)(given ? z + g.g : z);
   };
-  const int64_t v0 = chunk * SC_THREADS * GR_U + tid;
-  Vec<T> x[GR_U];
+  for (int step = 0; step < a.steps && v - tid < vecs; step++, v += STEP) {
+    Vec<T> x[GR_U];
 #pragma unroll
-  for (int k = 0; k < GR_U; k++)
-    if (v0 + k * SC_THREADS < sp.vecs) x[k] = load_vec(in + sp.head + (v0 + k * SC_THREADS) * N);
+    for (int k = 0; k < GR_U; k++) x[k] = y[k];
+    if (step + 1 < a.steps) fetch(v + STEP);
 #pragma unroll
-  for (int k = 0; k < GR_U; k++) {
-    const int64_t v = v0 + k * SC_THREADS;
-    if (v < sp.vecs) {
-      Vec<T> y;
-      const int64_t at = g.target - (sp.head + v * N);  // place of the given token in this vector
+    for (int k = 0; k < GR_U; k++) {
+      const int w = v + k * SC_THREADS;
+      if (w >= vecs) continue;
+      Vec<T> z;
+      const int64_t at = g.target - (sp.head + (int64_t)w * N);  // place of the given token in this vector
       if (at >= 0 && at < N) {
 #pragma unroll
-        for (int i = 0; i < N; i++) y.v[i] = one((float)x[k].v[i], i == (int)at);
+        for (int i = 0; i < N; i++) z.v[i] = one((float)x[k].v[i], i == (int)at);
       } else {
 #pragma unroll
-        for (int i = 0; i < N; i++) y.v[i] = one((float)x[k].v[i], false);
+        for (int i = 0; i < N; i++) z.v[i] = one((float)x[k].v[i], false);
       }
-      __builtin_memcpy(__builtin_assume_aligned(out + sp.head + v * N, 16), &y, 16);
+      store_vec_once(out + sp.head + (int64_t)w * N, z);
     }
   }
   if (chunk == 0 && tid < sp.head) out[tid] = one((float)in[tid], tid == g.target);
-  if (chunk == a.chunks - 1 && sp.tail + tid < a.vocab) out[sp.tail + tid] = one((float)in[sp.tail + tid], sp.tail + tid == g.target);
+  if (chunk + 1 == (uint32_t)a.chunks && sp.tail + tid < a.vocab)
+    out[sp.tail + tid] = one((float)in[sp.tail + tid], sp.tail + tid == g.target);
 }
 
 template <class T>
 int run_scores(ScoreArgs<T> a, hipStream_t st) {
-  if (launch(a.n_alt ? scores_kernel<T, true> : scores_kernel<T, false>, dim3((uint32_t)(a.rows * a.splits)),
-             dim3(SC_THREADS), st, a) != hipSuccess)
+  const bool wave = a.rows >= WAVE_ROWS && a.vocab <= WAVE_VOCAB;
+  auto* kernel = wave ? a.n_alt ? scores_kernel<T, true, 64> : scores_kernel<T, false, 64>
+                      : a.n_alt ? scores_kernel<T, true, SC_THREADS> : scores_kernel<T, false, SC_THREADS>;
+  if (launch(kernel, dim3((uint32_t)(a.rows * a.splits)), dim3(wave ? 64 : SC_THREADS), st, a) != hipSuccess)
     return TT_ERR_HIP;
   if (a.splits > 1 && launch(scores_join_kernel<T>, dim3((uint32_t)a.rows), dim3(SC_THREADS), st, a) != hipSuccess)
     return TT_ERR_HIP;
@@ -536,8 +568,11 @@ int run_scores(ScoreArgs<T> a, hipStream_t st) {
 
 template <class T>
 int run_grad(GradArgs<T> a, hipStream_t st) {
-  const int64_t cols = grad_cols<T>();
-  a.chunks = (a.vocab + cols - 1) / cols;
+  const int64_t all = (a.vocab + grad_step<T>() - 1) / grad_step<T>();  // steps of a row
+  int64_t chunks = a.rows >= GR_BLOCKS ? 1 : GR_BLOCKS / a.rows;
+  if (chunks > all) chunks = all;
+  a.steps = (int)((all + chunks - 1) / chunks);
+  a.chunks = (int)((all + a.steps - 1) / a.steps);
   if (a.rows > (int64_t)UINT32_MAX / SC_THREADS / a.chunks) return TT_ERR_TOO_LARGE;
   return launch(scores_grad_kernel<T>, dim3((uint32_t)(a.rows * a.chunks)), dim3(SC_THREADS), st, a) == hipSuccess
              ? TT_OK
@@ -587,7 +622,7 @@ extern "C" int tt_token_scores_grad(const void* logits, int32_t type, int64_t ro
   auto go = [&](auto zero) {
     using T = decltype(zero);
     return run_grad(GradArgs<T>{static_cast<const T*>(logits), static_cast<T*>(grad_logits), rows, vocab, stride,
-                                grad_stride, 0, scale, targets, stats, entropy, grad_logprobs, grad_entropy},
+                                grad_stride, scale, targets, stats, entropy, grad_logprobs, grad_entropy, 0, 0},
                     static_cast<hipStream_t>(stream));
   };
   return type == TT_F32 ? go(float{}) : type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});

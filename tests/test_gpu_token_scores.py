@@ -151,6 +151,34 @@ def test_rows_without_a_distribution(gpu, kind, rows):
     assert float(got["logprobs"][0]) == 0.0 and float(got["entropy"][0]) == 0.0
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab,shift", [(4099, 0), (1281, 3), (65, 1), (9001, 0)])
+def test_many_short_rows(gpu, kind, vocab, shift):
+    """Rows that one wave takes, with masks, ties, sorted rows and rows without a distribution among them."""
+    rows = 2100
+    z, t = logits_of(rows, vocab, kind, vocab, 2, shift)
+    whole = z.clone()
+    low = torch.finfo(kind).min
+    z[0] = -INF
+    z[1] = low
+    z[2] = 1.5
+    z[3] = torch.sort(z[3].float()).values.to(kind)
+    z[4] = torch.sort(z[4].float(), descending=True).values.to(kind)
+    z[5, vocab // 2] = math.nan
+    z[6, vocab - 1] = INF
+    for r, (mask, left) in enumerate([(-INF, 3), (low, 3), (-INF, 1), (low, vocab // 2), (-INF, vocab // 2)], 7):
+        z[r] = mask
+        keep = torch.randperm(vocab, generator=torch.Generator().manual_seed(r))[:left].to("cuda")
+        z[r, keep] = whole[r, keep]
+    z[20:40] = torch.round(z[20:40].float()).to(kind)
+    z[41] = 0.0
+    z[41, 1::2] = -0.0
+    cols = torch.arange(vocab, device="cuda")
+    z[42] = torch.where((cols // (16 // z.element_size())) % 64 == 5, cols.float() % 50 + 1, torch.zeros(vocab, device="cuda")).to(kind)
+    for n_alt in (0, 1, 20, 64):
+        check(z, t, n_alt)
+
+
 def test_targets(gpu):
     z, t = logits_of(40, 1281, torch.float32, 14)
     t[3], t[4], t[5], t[6] = -1, -2**31, 1281, 2**31 - 1
@@ -264,6 +292,14 @@ def test_grad_vocabularies(gpu, kind, vocab):
     t[1] = -1
     check_grad(z, t, *grads(9))
     check_grad(z, t, *grads(9, entropy=False))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(1, 100_257), (70, 100_257), (700, 33_000), (4097, 1281), (4100, 20_011)])
+def test_grad_rows(gpu, kind, rows, vocab):
+    """One block a row, several blocks a row, several steps a block."""
+    z, t = logits_of(rows, vocab, kind, rows)
+    check_grad(z, t, *grads(rows))
 
 
 @pytest.mark.parametrize("kind", TYPES)
