@@ -40,6 +40,7 @@ struct Operand {
   int64_t stride, rows;
 };
 
+constexpr int CUS = 256;  // compute units
 constexpr int BK = 64;  // entries of k that are staged at once: rows of 128 bytes in LDS
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
@@ -57,8 +58,11 @@ __device__ __forceinline__ Buffer buffer_at(const void* p) {
 // read of LDS wait for the load; there is no result register.  (m0 is the
 // compiler's to set before each use of its own; a write of it needs one wait
 // state before its use.)
+// ONCE: what is read once does not stay in the caches.
+template <bool ONCE = false>
 __device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
+  if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(offset), "s"(from));
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
 }
 // Waits for all but the last N of this wave's loads and for its LDS reads, then
 // for the block's other waves.
@@ -89,10 +93,8 @@ struct Tile {
   using V4 = typename Mfma<T>::V4;
   static constexpr int NA = BM * 8 / THREADS, NB = BN * 8 / THREADS;  // 16-byte pieces a thread stages
   static_assert(NA * THREADS == BM * 8 && NB * THREADS == BN * 8, "whole pieces");
-  static constexpr bool STREAM = VEC && BM < 256;
-  static constexpr int STAGES = STREAM ? 3 : 2;
   struct Shared {
-    T a[STAGES][BM * BK], b[STAGES][BN * BK];
+    T a[2][BM * BK], b[2][BN * BK];
   };
 
   // Piece q of a stage: row q / 8, entries 8 (q % 8) and on.  In LDS the pieces
@@ -121,7 +123,6 @@ struct Tile {
   static __device__ __forceinline__ void multiply(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
                                                   int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
     if constexpr (DIRECT) multiply_direct(a, b, m0, n0, k0, k1, sh, acc);
-    else if constexpr (STREAM) multiply_stream(a, b, m0, n0, k0, k1, sh, acc);
     else multiply_staged(a, b, m0, n0, k0, k1, sh, acc);
   }
 
@@ -324,73 +325,6 @@ struct Tile {
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
   }
 
-  // The same for few columns, where the rows of A stream through once and
-  // nothing else counts: small tiles of two waves, three stages deep, so that
-  // a compute unit has up to 100 KB under way.
-  static __device__ __forceinline__ void multiply_stream(const Operand<T>& a, const Operand<T>& b, int64_t m0, int64_t n0,
-                                                         int64_t k0, int64_t k1, Shared& sh, f32x16 (&acc)[TM][TN]) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / WN, wn = wave % WN;
-    uint32_t oa[DA], ob[DB];
-    auto offset = [&](const Operand<T>& o, int64_t first, int row) {
-      return first + row < o.rows ? (uint32_t)(row * o.stride + ((lane & 7) ^ twist(row)) * 8) * 2 : BUFFER_BYTES;
-    };
-#pragma unroll
-    for (int i = 0; i < DA; i++) oa[i] = offset(a, m0, (wave * DA + i) * 8 + (lane >> 3));
-#pragma unroll
-    for (int i = 0; i < DB; i++) ob[i] = offset(b, n0, (wave * DB + i) * 8 + (lane >> 3));
-    const T *pa = a.p + m0 * a.stride + k0, *pb = b.p + n0 * b.stride + k0;
-    const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
-    const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
-    const int full_stages = (int)((k1 - k0) / BK), rest = (int)((k1 - k0) % BK);
-    auto load_stage = [&](int stage, int buf) {  // in order of stages; past k1 zeros
-      if (stage >= full_stages) {
-        const int here = stage > full_stages ? 0 : rest;
-#pragma unroll
-        for (int i = 0; i < DA; i++)
-          if (((lane & 7) ^ twist((wave * DA + i) * 8 + (lane >> 3))) * 8 >= here) oa[i] = BUFFER_BYTES;
-#pragma unroll
-        for (int i = 0; i < DB; i++)
-          if (((lane & 7) ^ twist((wave * DB + i) * 8 + (lane >> 3))) * 8 >= here) ob[i] = BUFFER_BYTES;
-      }
-      const Buffer ba = buffer_at(pa + (int64_t)stage * BK), bb = buffer_at(pb + (int64_t)stage * BK);
-#pragma unroll
-      for (int i = 0; i < DA; i++) load_to_lds(ba, oa[i], la + buf * (BM * BK * 2) + i * 1024);
-#pragma unroll
-      for (int i = 0; i < DB; i++) load_to_lds(bb, ob[i], lb + buf * (BN * BK * 2) + i * 1024);
-    };
-#pragma unroll
-    for (int i = 0; i < TM; i++)
-#pragma unroll
-      for (int j = 0; j < TN; j++)
-#pragma unroll
-        for (int r = 0; r < 16; r++) acc[i][j][r] = 0.f;
-    const int steps = (int)((k1 - k0 + BK - 1) / BK);
-#pragma unroll
-    for (int i = 0; i < STAGES - 1; i++) load_stage(i, i);
-    int buf = 0;
-    for (int s = 0; s < steps; s++) {
-      loads_done_but<(STAGES - 2) * (DA + DB)>();  // stage s is here, and every wave is past stage s - 1
-      load_stage(s + STAGES - 1, buf == 0 ? STAGES - 1 : buf - 1);
-#pragma unroll
-      for (int kk = 0; kk < BK / 16; kk++) {
-        V8 fa[TM], fb[TN];
-#pragma unroll
-        for (int i = 0; i < TM; i++)
-          fa[i] = *reinterpret_cast<const V8*>(&sh.a[buf][place(wm * TM * 32 + i * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
-#pragma unroll
-        for (int j = 0; j < TN; j++)
-          fb[j] = *reinterpret_cast<const V8*>(&sh.b[buf][place(wn * TN * 32 + j * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
-#pragma unroll
-        for (int i = 0; i < TM; i++)
-#pragma unroll
-          for (int j = 0; j < TN; j++) acc[i][j] = Mfma<T>::mul(fa[i], fb[j], acc[i][j]);
-      }
-      buf = buf == STAGES - 1 ? 0 : buf + 1;
-    }
-    loads_done_but<0>();
-  }
-
   // One value of an accumulator, out of an accumulation register where the
   // accumulators fill those: they stay there until each is used.
   static __device__ __forceinline__ float value(const f32x16 (&acc)[TM][TN], int i, int j, int r) {
@@ -533,6 +467,161 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
   }
 }
 
+// The same for up to 64 rows, where the weights stream through once and nothing
+// else counts.  Small blocks of two waves, as many as LDS holds, take every
+// so-many-th tile of 64 vocabulary entries; their stages follow each other across
+// tiles, so that two of them are always under way, past the caches.
+// Blocks begin at different k: rows are often a power of two apart, and blocks in
+// step would ask the same few memory channels.
+// Every lane keeps the statistics of its own entries of a column to the end.
+template <class T, int BN_>
+struct Stream {
+  using Elem = T;
+  using Tl = Tile<T, 64, BN_, 2, 1, true>;
+  static constexpr int BN = BN_, STAGES = 3, DA = 4, DB = BN / 16;  // loads of a wave in a stage
+  static constexpr int BLOCKS = CUS * (BN == 32 ? 4 : 3);  // as many as LDS holds at once
+  struct Shared {
+    T a[STAGES][64 * BK], b[STAGES][BN * BK];
+    Part joined[2][BN];
+  };
+};
+
+template <class S>
+__global__ __launch_bounds__(128, 1) void head_stream_kernel(HeadArgs<typename S::Elem> a) {
+  using T = typename S::Elem;
+  using Tl = typename S::Tl;
+  using V8 = typename Tl::V8;
+  constexpr int DA = S::DA, DB = S::DB, STAGES = S::STAGES, BN = S::BN;
+  __shared__ typename S::Shared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int blocks = gridDim.x, steps = (int)((a.width + BK - 1) / BK);
+  const int64_t vocab = a.weight.rows, rows = a.hidden.rows;
+  int targets[Tl::TN];
+#pragma unroll
+  for (int j = 0; j < Tl::TN; j++) {
+    const int64_t t = j * 32 + (lane & 31);
+    targets[j] = a.targets && t < rows ? a.targets[t] : -1;
+  }
+  uint32_t oa[DA], ob[DB];
+  auto place_of = [&](int row, int64_t stride) { return (uint32_t)(row * stride + ((lane & 7) ^ Tl::twist(row)) * 8) * 2; };
+#pragma unroll
+  for (int i = 0; i < DA; i++) oa[i] = place_of((wave * DA + i) * 8 + (lane >> 3), a.weight.stride);
+#pragma unroll
+  for (int i = 0; i < DB; i++) {
+    const int row = (wave * DB + i) * 8 + (lane >> 3);
+    ob[i] = row < rows ? place_of(row, a.hidden.stride) : BUFFER_BYTES;
+  }
+  const uint32_t la = __builtin_amdgcn_readfirstlane(lds_address(sh.a) + wave * DA * 1024);
+  const uint32_t lb = __builtin_amdgcn_readfirstlane(lds_address(sh.b) + wave * DB * 1024);
+
+  // the next stage to load
+  int64_t load_m0 = (int64_t)blockIdx.x * 64;
+  const int phase = blockIdx.x % steps, whole = (int)(a.width / BK);
+  int load_i = 0, load_k = phase, load_buf = 0;
+  const T* load_tile = a.weight.p + load_m0 * a.weight.stride;
+  auto load_stage = [&] {
+    const Buffer ba = buffer_at(load_tile + load_k * BK), bb = buffer_at(a.hidden.p + load_k * BK);
+    const uint32_t ta = la + load_buf * (64 * BK * 2), tb = lb + load_buf * (BN * BK * 2);
+    if (load_m0 + 64 <= vocab && load_k < whole) {
+#pragma unroll
+      for (int i = 0; i < DA; i++) load_to_lds<true>(ba, oa[i], ta + i * 1024);
+#pragma unroll
+      for (int i = 0; i < DB; i++) load_to_lds(bb, ob[i], tb + i * 1024);
+    } else {  // the last entries of k or of the vocabulary, and the stages past the last tile: zeros behind them
+      const int64_t k_left = a.width - (int64_t)load_k * BK, rows_left = vocab - load_m0;
+#pragma unroll
+      for (int i = 0; i < DA; i++) {
+        const int row = (wave * DA + i) * 8 + (lane >> 3);
+        const bool real = ((lane & 7) ^ Tl::twist(row)) * 8 < k_left && row < rows_left;
+        load_to_lds<true>(ba, real ? oa[i] : BUFFER_BYTES, ta + i * 1024);
+      }
+#pragma unroll
+      for (int i = 0; i < DB; i++) {
+        const int row = (wave * DB + i) * 8 + (lane >> 3);
+        const bool real = ((lane & 7) ^ Tl::twist(row)) * 8 < k_left && rows_left > 0;
+        load_to_lds(bb, real ? ob[i] : BUFFER_BYTES, tb + i * 1024);
+      }
+    }
+    load_buf = load_buf == STAGES - 1 ? 0 : load_buf + 1;
+    if (++load_k == steps) load_k = 0;
+    if (++load_i == steps) {
+      load_i = 0;
+      load_m0 += (int64_t)blocks * 64;
+      load_tile += (int64_t)blocks * 64 * a.weight.stride;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; i++) load_stage();
+
+  const float c = a.scale * LOG2E;
+  Stats st[Tl::TN];
+#pragma unroll
+  for (int j = 0; j < Tl::TN; j++) st[j] = empty_stats();
+  int buf = 0;
+  for (int64_t m0 = (int64_t)blockIdx.x * 64; m0 < vocab; m0 += (int64_t)blocks * 64) {
+    f32x16 acc[Tl::TN], odd[Tl::TN];  // (two sums: a product need not wait for the last one)
+#pragma unroll
+    for (int j = 0; j < Tl::TN; j++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) acc[j][r] = odd[j][r] = 0.f;
+    for (int k = 0; k < steps; k++) {
+      loads_done_but<(STAGES - 2) * (DA + DB)>();  // this stage is here, and both waves are past the last one
+      V8 fa[BK / 16], fb[Tl::TN][BK / 16];
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; kk++) {
+        fa[kk] = *reinterpret_cast<const V8*>(&sh.a[buf][Tl::place(wave * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+#pragma unroll
+        for (int j = 0; j < Tl::TN; j++)
+          fb[j][kk] = *reinterpret_cast<const V8*>(&sh.b[buf][Tl::place(j * 32 + (lane & 31), kk * 2 + (lane >> 5))]);
+      }
+      load_stage();
+#pragma unroll
+      for (int kk = 0; kk < BK / 16; kk += 2)
+#pragma unroll
+        for (int j = 0; j < Tl::TN; j++) {
+          acc[j] = Mfma<T>::mul(fa[kk], fb[j][kk], acc[j]);
+          odd[j] = Mfma<T>::mul(fa[kk + 1], fb[j][kk + 1], odd[j]);
+        }
+      buf = buf == STAGES - 1 ? 0 : buf + 1;
+    }
+#pragma unroll
+    for (int j = 0; j < Tl::TN; j++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) acc[j][r] += odd[j][r];
+    const int64_t mine = m0 + wave * 32 + (lane >> 5) * 4;  // entry 8 (r / 4) + r % 4 from here on
+    const int last = vocab - mine < 32 ? (int)(vocab - mine) : 32;
+#pragma unroll
+    for (int j = 0; j < Tl::TN; j++) {
+      const int64_t given = targets[j] - mine;
+      float m = st[j].m;
+#pragma unroll
+      for (int r = 0; r < 16; r++) {
+        const int at = 8 * (r >> 2) + (r & 3);
+        if (at == given) a.given[j * 32 + (lane & 31)] = acc[j][r];
+        if (at >= last) acc[j][r] = NEG_INF;
+        m = larger(m, acc[j][r]);
+      }
+      lower(st[j], m, c);
+      const Reference ref = reference(m, c);
+#pragma unroll
+      for (int r = 0; r < 16; r++) add_entry<false>(st[j], acc[j][r], ref, c);
+    }
+  }
+  loads_done_but<0>();
+#pragma unroll
+  for (int j = 0; j < Tl::TN; j++) {
+    const Stats o = {__shfl_xor(st[j].m, 32), __shfl_xor(st[j].s, 32), __shfl_xor(st[j].u, 32)};
+    st[j] = join(st[j], o, c);
+    if (lane < 32) sh.joined[wave][j * 32 + lane] = {st[j].m, st[j].s, st[j].u, 0.f};
+  }
+  __syncthreads();
+  if (tid < BN && tid < rows) {
+    const Part &p = sh.joined[0][tid], &q = sh.joined[1][tid];
+    const Stats all = join(Stats{p.m, p.s, p.u}, Stats{q.m, q.s, q.u}, c);
+    a.parts[tid * blocks + blockIdx.x] = {all.m, all.s, all.u, 0.f};
+  }
+}
+
 // Joins a row's parts: one wave per row.
 __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const float* given, int32_t n_parts,
                                                         int64_t rows, int64_t vocab, float scale, const int32_t* targets,
@@ -541,16 +630,30 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
   const int lane = threadIdx.x & 63;
   if (row >= rows) return;
   const float c = scale * LOG2E;
+  const int32_t t = targets ? targets[row] : -1;
+  const float x_given = t >= 0 && t < vocab ? given[row] : 0.f;
   Stats st = empty_stats();
-  for (int i = lane; i < n_parts; i += 64) {
-    const Part q = parts[row * n_parts + i];
-    st = join(st, Stats{q.m, q.s, q.u}, c);
+  constexpr int U = 8;
+  for (int i = lane; i - lane < n_parts; i += 64 * U) {
+    Part q[U];
+#pragma unroll
+    for (int k = 0; k < U; k++) q[k] = i + 64 * k < n_parts ? parts[row * n_parts + i + 64 * k] : Part{NEG_INF, 0.f, 0.f, 0.f};
+    float m = st.m;
+#pragma unroll
+    for (int k = 0; k < U; k++) m = larger(m, q[k].m);
+    lower(st, m, c);
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      Stats o = {q[k].m, q[k].s, q[k].u};
+      lower(o, m, c);
+      st.s += o.s;
+      st.u += o.u;
+    }
   }
   st = wave_join(st, c);
   if (lane) return;
   const RowScores r = row_scores(st, c);
-  const int32_t t = targets ? targets[row] : -1;
-  if (logprobs) logprobs[row] = given_log_prob(t, vocab, t >= 0 && t < vocab ? given[row] : 0.f, r, scale);
+  if (logprobs) logprobs[row] = given_log_prob(t, vocab, x_given, r, scale);
   if (stats) {
     stats[2 * row] = r.m;
     stats[2 * row + 1] = r.log_s;
@@ -794,7 +897,6 @@ constexpr int64_t up(int64_t x, int64_t n) { return (x + n - 1) / n * n; }
 constexpr int64_t div_up(int64_t x, int64_t n) { return (x + n - 1) / n; }
 constexpr int64_t PIECE = 256;    // the vocabulary is taken in multiples of this
 constexpr int64_t MOST_PIECE = 1 << 21;  // (256 rows of G, and of hidden and weight, lie in one buffer)
-constexpr int64_t CUS = 256;      // compute units
 
 constexpr int FEW_TILE = 64;  // vocabulary entries of a tile for up to 64 rows
 int64_t forward_tile_rows(int64_t rows) { return rows <= 64 ? FEW_TILE : 256; }
@@ -809,13 +911,20 @@ bool vectors(const Operand<T>& o, int64_t k) {
          o.stride <= ((int64_t)BUFFER_BYTES / 2 - 64) / 256;  // the tile's rows in one buffer
 }
 
+// Both set the number of a row's parts.
 template <class Tl>
-int run_forward(HeadArgs<typename Tl::Elem> a, hipStream_t st) {
+int run_forward(HeadArgs<typename Tl::Elem>& a, hipStream_t st) {
   const int64_t m = div_up(a.weight.rows, Tl::BM), n = div_up(a.hidden.rows, Tl::BN);
   if (m * n > (int64_t)UINT32_MAX / Tl::THREADS) return TT_ERR_TOO_LARGE;
   a.m_tiles = (int32_t)m;
   a.n_tiles = (int32_t)n;
   return launch(head_scores_kernel<Tl>, dim3((uint32_t)(m * n)), dim3(Tl::THREADS), st, a) == hipSuccess ? TT_OK : TT_ERR_HIP;
+}
+template <class S>
+int run_stream(HeadArgs<typename S::Elem>& a, hipStream_t st) {
+  const int64_t tiles = div_up(a.weight.rows, 64);
+  a.m_tiles = (int32_t)(tiles < S::BLOCKS ? tiles : S::BLOCKS);
+  return launch(head_stream_kernel<S>, dim3((uint32_t)a.m_tiles), dim3(128), st, a) == hipSuccess ? TT_OK : TT_ERR_HIP;
 }
 
 // Whether tiles of 256 x 128 finish before tiles of 256 x 256: the tiles run in
@@ -828,10 +937,11 @@ bool narrow(int64_t m, int64_t n, int64_t parts) {
 }
 
 template <class T, bool VEC>
-int forward_by_rows(const HeadArgs<T>& a, hipStream_t st) {
+int forward_by_rows(HeadArgs<T>& a, hipStream_t st) {
   const int64_t rows = a.hidden.rows;
-  if (rows <= 32) return run_forward<Tile<T, FEW_TILE, 32, 2, 1, VEC>>(a, st);
-  if (rows <= 64) return run_forward<Tile<T, FEW_TILE, 64, 2, 1, VEC>>(a, st);
+  if (VEC && rows <= 32) return run_stream<Stream<T, 32>>(a, st);
+  if (VEC && rows <= 64) return run_stream<Stream<T, 64>>(a, st);
+  if (rows <= 64) return run_forward<Tile<T, FEW_TILE, 64, 2, 1, false>>(a, st);
   if (!VEC) return run_forward<Tile<T, 256, 128, 4, 2, false>>(a, st);
   if (narrow(a.weight.rows, rows, 1)) return run_forward<Tile<T, 256, 128, 2, 2, true>>(a, st);
   return run_forward<Tile<T, 256, 256, 2, 2, true>>(a, st);
@@ -1015,19 +1125,21 @@ extern "C" int tt_head_scores(const void* hidden, int64_t hidden_stride, const v
   hipStream_t st = static_cast<hipStream_t>(stream);
   float* given = static_cast<float*>(workspace);
   Part* parts = reinterpret_cast<Part*>(static_cast<uint8_t*>(workspace) + up(rows * 4, 256));
+  int32_t n_parts = 0;
   auto go = [&](auto zero) {
     using T = decltype(zero);
-    const HeadArgs<T> a{{static_cast<const T*>(weight), weight_stride, vocab},
-                        {static_cast<const T*>(hidden), hidden_stride, rows},
-                        width, scale, targets, parts, given, 0, 0};
-    return vectors(a.weight, width) && vectors(a.hidden, width) ? forward_by_rows<T, true>(a, st)
-                                                                : forward_by_rows<T, false>(a, st);
+    HeadArgs<T> a{{static_cast<const T*>(weight), weight_stride, vocab},
+                  {static_cast<const T*>(hidden), hidden_stride, rows},
+                  width, scale, targets, parts, given, 0, 0};
+    const int s = vectors(a.weight, width) && vectors(a.hidden, width) ? forward_by_rows<T, true>(a, st)
+                                                                       : forward_by_rows<T, false>(a, st);
+    n_parts = a.m_tiles;
+    return s;
   };
   const int s = type == TT_BF16 ? go(bf16_t{}) : go(f16_t{});
   if (s != TT_OK) return s;
   return launch(head_join_kernel, dim3((uint32_t)div_up(rows, 4)), dim3(256), st, static_cast<const Part*>(parts),
-                static_cast<const float*>(given), (int32_t)div_up(vocab, forward_tile_rows(rows)), rows, vocab, scale,
-                targets, logprobs, stats, entropy) == hipSuccess
+                static_cast<const float*>(given), n_parts, rows, vocab, scale, targets, logprobs, stats, entropy) == hipSuccess
              ? TT_OK
              : TT_ERR_HIP;
 }
