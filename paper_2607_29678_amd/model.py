@@ -23,25 +23,30 @@ _F32, _I32, _I64, _U8 = _lib.TT_F32, "i32", "i64", "u8"
 _codes = {}  # dtype -> its code (the types' names are long to make)
 
 
+_known = _codes.get
+
+
 def _code(dtype):
-    try:
-        return _codes[dtype]
-    except KeyError:
-        return _codes.setdefault(dtype, _NAMES.get(str(dtype)))
+    code = _known(dtype)
+    return _codes.setdefault(dtype, _NAMES.get(str(dtype))) if code is None else code
 
 
 def _flat(t, name, code, shape, device):
-    """Address of a contiguous tensor of this type and shape on this device; None for None."""
+    """Address of a contiguous tensor of this type and shape on this device; 0 for None."""
     if t is None:
-        return None
-    if t.shape != shape or _code(t.dtype) != code or t.get_device() != device or device < 0 or not t.is_contiguous():
+        return 0
+    if t.shape == shape and _known(t.dtype) == code and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    if t.shape != shape or _code(t.dtype) != code or t.get_device() != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s device tensor of shape %s, on device %d with the others, not %s %s on %s"
-                         % (name, {v: k for k, v in _NAMES.items()}[code], shape, device, t.dtype, tuple(t.shape), t.device))
+                         % (name, {v: k for k, v in _NAMES.items()}[code], tuple(shape), device, t.dtype, tuple(t.shape),
+                            t.device))
     return t.data_ptr()
 
 
 def _matrix(t, name, device, dtype=None, shape=None):
-    """(address, row stride) of a device matrix whose rows are contiguous and do not overlap."""
+    """(address, row stride) of a device matrix whose rows are contiguous and do not overlap.  (Every
+    call has one on the first tensor's device, so a host tensor, whose device is -1, stops here.)"""
     if t.dim() != 2 or t.get_device() != device or device < 0 or (dtype is not None and t.dtype != dtype) or \
             (shape is not None and t.shape != shape):
         raise ValueError("%s must be a device matrix%s%s, on device %d with the others, not %s %s on %s"
@@ -110,15 +115,15 @@ def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets,
         raise ValueError("tables must be an int32 matrix of %d rows, not %s %s" % (n, tables.dtype, tuple(tables.shape)))
     if len(each) != 1 or len(room) != 1 or len(free) != 1:
         raise ValueError("cached, slots and free_pages must have one dimension")
+    flat = _flat
     step = _STEP.pack(
-        n, page_size, width, stride, room[0], free[0], _flat(cached, "cached", _I32, each, d) or 0,
-        _flat(fresh, "fresh", _I32, each, d) or 0, _flat(held, "held", _I32, each, d) or 0,
-        _flat(ids, "ids", _I32, room, d) or 0, _flat(free_pages, "free_pages", _I32, free, d) or 0,
-        _flat(free_count, "free_count", _I64, (1,), d) or 0, table or 0, _flat(offsets, "offsets", _I32, (n + 1,), d) or 0,
-        _flat(lengths, "lengths", _I32, each, d) or 0, _flat(pages, "pages", _I32, each, d) or 0,
-        _flat(slots, "slots", _I64, room, d) or 0, _flat(positions, "positions", _I32, room, d) or 0,
-        _flat(requests, "requests", _I32, room, d) or 0, _flat(targets, "targets", _I32, room, d) or 0,
-        _flat(result, "result", _I64, (2,), d) or 0)
+        n, page_size, width, stride, room[0], free[0], flat(cached, "cached", _I32, each, d),
+        flat(fresh, "fresh", _I32, each, d), flat(held, "held", _I32, each, d), flat(ids, "ids", _I32, room, d),
+        flat(free_pages, "free_pages", _I32, free, d), flat(free_count, "free_count", _I64, (1,), d), table,
+        flat(offsets, "offsets", _I32, (n + 1,), d), flat(lengths, "lengths", _I32, each, d),
+        flat(pages, "pages", _I32, each, d), flat(slots, "slots", _I64, room, d), flat(positions, "positions", _I32, room, d),
+        flat(requests, "requests", _I32, room, d), flat(targets, "targets", _I32, room, d),
+        flat(result, "result", _I64, (2,), d))
     _lib.check(_lib.load().tt_step_plan(step, stream), "tt_step_plan")
 
 
