@@ -68,7 +68,7 @@ def check(torch, c, **kw):
     return got
 
 
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 511, 513, 4095, 4096, 4097, 9001])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 511, 513, 2047, 2048, 2049, 4095, 4096, 4097, 9001])
 @pytest.mark.parametrize("kind", ["decode", "mixed"])
 def test_requests(gpu, n, kind):
     rng = np.random.default_rng(n)
@@ -94,6 +94,39 @@ def test_requests_without_tokens(gpu, zeros):
 def test_long_requests(gpu):
     rng = np.random.default_rng(6)
     check(gpu, make(rng, 5, 64, "mixed", most_fresh=60_000, most_cached=100_000, zeros=0.0), use_ids=False)
+
+
+@pytest.mark.parametrize("n", [3, 700, 2049])
+def test_arrays_at_any_alignment(gpu, n):
+    from paper_2607_29678_amd import step_plan
+
+    torch = gpu
+    c = make(np.random.default_rng(n), n, 16, "mixed", room_over=3)
+    want_tables = c["tables"].copy()
+    want = ref.plan(c["cached"], c["fresh"], None, 16, want_tables, c["free"], c["count"], c["ids"], c["room"])
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda")  # noqa: E731
+
+    def off(k, t=torch.int32):  # one entry past an aligned address, with a guard behind
+        return torch.full((k + 2,), -99, dtype=t, device="cuda")
+
+    full = dict(offsets=off(n + 1), lengths=off(n), pages=off(n), slots=off(c["room"], torch.int64), positions=off(c["room"]),
+                requests=off(c["room"]), targets=off(c["room"]), result=off(2, torch.int64))
+    o = {k: v[1:-1] for k, v in full.items()}
+    tables = dev(c["tables"])
+    step_plan(dev(c["cached"]), dev(c["fresh"]), tables, dev(c["free"]), dev(np.array([c["count"]], dtype=np.int64)), 16,
+              o["offsets"], o["lengths"], o["pages"], o["slots"], o["positions"], o["requests"], o["result"],
+              ids=dev(c["ids"]), targets=o["targets"])
+    torch.cuda.synchronize()
+    for k in o:
+        assert o[k].cpu().tolist() == want[k], k
+        assert int(full[k][0]) == -99 and int(full[k][-1]) == -99
+    assert np.array_equal(tables.cpu().numpy(), want_tables)
+
+
+@pytest.mark.parametrize("room_over", [0, 1, 2, 3, 4, 5000])
+def test_room_past_the_tokens(gpu, room_over):
+    for n in (5, 2500):
+        check(gpu, make(np.random.default_rng(room_over), n, 16, "mixed", room_over=room_over))
 
 
 def test_no_requests(gpu):
