@@ -756,7 +756,16 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
     if (t < a.hidden.rows)
       grads[j] = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, t, a.vocab, a.scale);
   }
-  const float c = a.scale * LOG2E, factor = a.factor ? a.factor[0] : 1.f;
+  const float c = a.scale * LOG2E;
+  if (a.factor) {  // (a power of two)
+    const float factor = a.factor[0];
+#pragma unroll
+    for (int j = 0; j < Tl::TN; j++) {
+      grads[j].a *= factor;
+      grads[j].b *= factor;
+      grads[j].g *= factor;
+    }
+  }
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
   const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;
@@ -771,24 +780,26 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
       int last = left - Tl::row_of(0, 0);
       if (!WHOLE) asm volatile("" : "+v"(last));  // (opaque: comparisons are not made ahead and kept)
       __builtin_amdgcn_sched_barrier(0);
-      auto four = [&](int i, int q, auto with_given) {
+      auto four = [&](int i, int q, auto with_given, auto some_zero) {
+        using zeros = decltype(some_zero);
         typename Tl::V4 out;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
           const int place = 32 * i + 8 * q + r;
           float y = grad_of(Tl::value(acc, i, j, 4 * q + r), c, g);
           if (decltype(with_given)::value && place == given) y += g.g;
-          out[r] = (T)(!g.zero && (WHOLE || place < last) ? y * factor : 0.f);
+          out[r] = (T)((zeros::value && g.zero) || (!WHOLE && place >= last) ? 0.f : y);
         }
         keep_four<Tl>(sh, i, j, q, out);
       };
-      const bool any = __ballot(given >= 0);
+      // rows without a gradient, and given tokens, are in few tiles
+      const bool any = __ballot(given >= 0 || g.zero);
 #pragma unroll
       for (int i = 0; i < Tl::TM; i++) {
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-          if (any) four(i, q, std::true_type{});
-          else four(i, q, std::false_type{});
+          if (any) four(i, q, std::true_type{}, std::true_type{});
+          else four(i, q, std::false_type{}, std::false_type{});
         }
         __builtin_amdgcn_sched_barrier(0);
       }

@@ -143,9 +143,10 @@ __device__ __forceinline__ RowGrad row_grad(const int32_t* targets, const float*
   if (r.target >= vocab) r.a = __builtin_nanf("");
   return r;
 }
+// (p is 0 long before d reaches -1e4, where d is held so that 0 times -inf does not arise)
 __device__ __forceinline__ float grad_of(float x, float c, const RowGrad& r) {
-  const float d = fmaf(x - r.m, c, -r.l2), p = __builtin_amdgcn_exp2f(d);
-  return fmaf(weigh(p, d), r.b, p * r.a);
+  const float d = fmaf(x - r.m, c, -r.l2);
+  return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, -1e4f), r.b, r.a);
 }
 
 inline bool score_type(int32_t type) { return type == TT_F32 || type == TT_BF16 || type == TT_F16; }
