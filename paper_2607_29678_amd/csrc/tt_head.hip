@@ -1128,7 +1128,7 @@ extern "C" int tt_head_scores(const void* hidden, int64_t hidden_stride, const v
                               int64_t workspace_bytes, void* stream) {
   const int64_t need = tt_head_scores_workspace(rows, vocab, width);
   if (need < 0 || (type != TT_BF16 && type != TT_F16) || hidden_stride < width || weight_stride < width ||
-      !good_scale(scale) || workspace_bytes < need)
+      !good_scale(scale) || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)
     return TT_ERR_BAD_ARG;
   if (rows == 0) return TT_OK;
   if (!hidden || !weight || !workspace) return TT_ERR_NULL_ARG;
@@ -1157,6 +1157,7 @@ extern "C" int tt_head_scores(const void* hidden, int64_t hidden_stride, const v
 
 extern "C" int64_t tt_head_scores_grad_workspace(int64_t rows, int64_t vocab, int64_t width, int32_t ample) {
   if (!head_sizes(rows, vocab, width)) return TT_ERR_BAD_ARG;
+  if (width > MOST_PIECE) return TT_ERR_TOO_LARGE;
   if (rows == 0) return 0;
   return grad_plan(rows, width, ample ? up(vocab < MOST_PIECE ? vocab : MOST_PIECE, PIECE) : PIECE, true).bytes;
 }
@@ -1168,14 +1169,15 @@ extern "C" int tt_head_scores_grad(const void* hidden, int64_t hidden_stride, co
                                    int64_t grad_hidden_stride, void* grad_weight, int64_t grad_weight_stride,
                                    void* workspace, int64_t workspace_bytes, void* stream) {
   const int64_t need = tt_head_scores_grad_workspace(rows, vocab, width, 0);
-  if (need < 0 || (type != TT_BF16 && type != TT_F16) || hidden_stride < width || weight_stride < width ||
+  if (need < 0) return (int)need;
+  if ((type != TT_BF16 && type != TT_F16) || hidden_stride < width || weight_stride < width ||
       (grad_hidden && grad_hidden_stride < width) || (grad_weight && grad_weight_stride < width) || !good_scale(scale) ||
-      workspace_bytes < need)
+      workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)
     return TT_ERR_BAD_ARG;
   if (!grad_hidden && !grad_weight) return TT_OK;
   if (!weight || (rows > 0 && (!hidden || !stats || !workspace || (grad_entropy && !entropy)))) return TT_ERR_NULL_ARG;
-  // launches of at most 2^32 threads, rows within a buffer
-  if (width > MOST_PIECE || div_up(vocab, 128) * (div_up(rows, 128) + div_up(width, 128)) > (int64_t)UINT32_MAX / 256 ||
+  // launches of at most 2^32 threads
+  if (div_up(vocab, 128) * (div_up(rows, 128) + div_up(width, 128)) > (int64_t)UINT32_MAX / 256 ||
       div_up(rows, 128) * div_up(width, 256) * 256 > (int64_t)UINT32_MAX / 256)
     return TT_ERR_TOO_LARGE;
   auto go = [&](auto zero) {

@@ -583,7 +583,9 @@ extern "C" int tt_token_scores(const void* logits, int32_t type, int64_t rows, i
                                int32_t* alt_ids, float* alt_logprobs, void* workspace, int64_t workspace_bytes,
                                void* stream) {
   const int64_t need = tt_token_scores_workspace(rows, vocab, n_alt);
-  if (need < 0 || !score_type(type) || stride < vocab || !good_scale(scale) || workspace_bytes < need) return TT_ERR_BAD_ARG;
+  if (need < 0 || !score_type(type) || stride < vocab || !good_scale(scale) || workspace_bytes < need ||
+      reinterpret_cast<uintptr_t>(workspace) % 256)
+    return TT_ERR_BAD_ARG;
   if (rows > (int64_t)UINT32_MAX / SC_THREADS) return TT_ERR_TOO_LARGE;
   if (rows == 0) return TT_OK;
   if (!logits || (need && !workspace) || (n_alt && (!alt_ids || !alt_logprobs))) return TT_ERR_NULL_ARG;

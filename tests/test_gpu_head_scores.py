@@ -139,6 +139,42 @@ def test_same_results_each_time(gpu):
             assert all(torch.equal(first[k], again[k]) for k in first)
 
 
+@pytest.mark.parametrize("rows", [5, 300])
+def test_captured_head_on_new_inputs(gpu, rows):
+    """Scores and gradients captured once follow what is in their inputs when they are replayed."""
+    from paper_2607_29678_amd import head_scores, head_scores_grad, head_scores_grad_workspace, head_scores_workspace
+
+    vocab, width = 3000, 128
+    hidden, weight, t = make(rows, vocab, width, torch.bfloat16, 30)
+    f = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    lp, st, en = f(rows), f(rows, 2), f(rows)
+    a, b = grads(rows)
+    gh, gw = torch.zeros_like(hidden), torch.zeros_like(weight)
+    size = max(head_scores_workspace(rows, vocab, width), head_scores_grad_workspace(rows, vocab, width))
+    work = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def call():
+        s = torch.cuda.current_stream().cuda_stream
+        head_scores(hidden, weight, t, lp, st, en, workspace=work, stream=s)
+        head_scores_grad(hidden, weight, t, st, en, a, b, gh, gw, workspace=work, stream=s)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(4):
+        for dst, src in zip((hidden, weight, t), make(rows, vocab, width, torch.bfloat16, 40 + seed)):
+            dst.copy_(src)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in (lp, st, en, gh, gw)]
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, (lp, st, en, gh, gw)))
+        check(hidden, weight, t)
+
+
 def test_another_stream(gpu):
     s = torch.cuda.Stream()
     check(*make(70, 3000, 128, torch.bfloat16, 12), stream=s.cuda_stream)

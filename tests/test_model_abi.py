@@ -142,6 +142,18 @@ def test_head_grad_strides_and_pointers():
     assert _head(rows=0, hidden=None, work=None, size=0) == 0
 
 
+def test_workspace_alignment():
+    assert _scores(vocab=50_000, stride=50_000, work=P + 8) == BAD
+    assert _head(work=P + 128) == BAD
+    assert _head_grad(work=P + 16) == BAD
+
+
+def test_widths_past_a_buffer():
+    lib = _lib.load()
+    assert lib.tt_head_scores_grad_workspace(8, 100, (1 << 21) + 1, 1) == LARGE
+    assert _head_grad(width=(1 << 21) + 8, hs=1 << 22, ws=1 << 22, ghs=1 << 22, gws=1 << 22, size=1 << 62) == LARGE
+
+
 def test_workspaces():
     assert token_scores_workspace(5000, 100_257, 20) == 0
     assert token_scores_workspace(1, 100_257, 20) > 0
