@@ -16,23 +16,44 @@ namespace {
 constexpr int SC_THREADS = 256;
 constexpr int SC_VECS = 192;       // 16-byte vectors with a possible alternative that a wave keeps in LDS
 constexpr int SC_CANDS = 512;      // candidates that are ordered there
-constexpr int SC_SPLIT_COLS = 2048;  // fewest columns of a part of a row
-constexpr int SC_MAX_SPLITS = 64;  // parts of a row: one list per lane when they are joined
-constexpr int64_t SC_BLOCKS = 1024;  // blocks that fill the chip (4 per compute unit)
-
 // Many short rows: a wave takes a row, and the reductions at a row's end are one
 // wave's (8,192 rows of 8,449 in bf16: 29 us against 39 with a block a row, with
 // 20 alternatives 52 against 61; at 16,384 entries 47 against 49, at 32,000 alike).
 constexpr int64_t WAVE_ROWS = 2048, WAVE_VOCAB = 16384;
 
-// Parts of a row that several blocks take: one block takes a row whole where there are rows enough.
-int scores_splits(int64_t rows, int64_t vocab) {
-  if (rows <= 0 || rows >= SC_BLOCKS) return 1;
-  int64_t n = SC_BLOCKS / rows, most = vocab / SC_SPLIT_COLS;
-  if (n > most) n = most;
-  if (n > SC_MAX_SPLITS) n = SC_MAX_SPLITS;
-  return n < 1 ? 1 : (int)n;
+// Parts of a row that several blocks take.  A part has a block's start and end
+// again and the parts are joined by a second launch, some 4 us in all, so that
+// only long rows gain, and the longer they are the more rows there are to fill
+// the chip without; finding alternatives takes longer and gains earlier.  us whole
+// and in parts (bf16 unless said):
+//   rows x vocab     scores alone       with 8 alternatives
+//      8 x  32,000     6.2 /  6.0          11.9 /  9.7 (11 parts)
+//      8 x 100,257    12.5 /  6.8          22.5 / 11.7 (32)
+//     64 x 100,257    12.8 /  9.3          22.9 / 14.7 (16)
+//    200 x 100,257    15.6 / 15.0          23.7 / 20.5 (5; f32 37.0 / 23.8)
+//    400 x 100,257    19.5 / 23.6          28.8 / 28.5 (2; f32 43.8 / 36.5)
+//    501 x   8,449     6.6 /  8.9           9.1 / 13.7 (2)
+//    700 x 100,257    28.6 / 32.6          34.3 / 36.7 (2)
+// 64 parts cost more to join than they save (8 rows of 256,000: 18.1 against 12.6).
+constexpr int SC_MAX_SPLITS = 32;
+constexpr int64_t SC_SPLIT_COLS = 2800;   // fewest columns of a part
+constexpr int64_t SC_BLOCKS = 1024;       // blocks that fill the chip (4 per compute unit)
+int scores_splits(int64_t rows, int64_t vocab, int32_t n_alt) {
+  const int64_t full = rows < 100 ? 100 : rows;
+  if (rows <= 0 || rows > (n_alt ? 512 : 256) || vocab < (n_alt ? 24576 : 40960) * full / 100) return 1;
+  int64_t n = SC_BLOCKS / rows;
+  if (n > vocab / SC_SPLIT_COLS) n = vocab / SC_SPLIT_COLS;
+  return (int)(n > SC_MAX_SPLITS ? SC_MAX_SPLITS : n);
 }
+// Parts that a workspace has room for: a bound of the above that does not follow
+// its figures, so that callers' sizes stay right when those change.
+int64_t scores_room(int64_t rows, int64_t vocab) {
+  if (rows <= 0 || rows >= SC_BLOCKS) return 0;
+  int64_t n = SC_BLOCKS / rows < 64 ? SC_BLOCKS / rows : 64;
+  if (n > vocab / 2048) n = vocab / 2048;
+  return n > 1 ? rows * n : 0;
+}
+static_assert(SC_MAX_SPLITS <= 64 && SC_SPLIT_COLS >= 2048, "scores_room");
 
 // A part's statistics and its alternatives in descending order (0: none)
 struct PartHead {
@@ -574,8 +595,7 @@ using namespace tt;
 
 extern "C" int64_t tt_token_scores_workspace(int64_t rows, int64_t vocab, int32_t n_alt) {
   if (rows < 0 || vocab < 1 || vocab > INT32_MAX || n_alt < 0 || n_alt > TT_MAX_ALTERNATIVES) return TT_ERR_BAD_ARG;
-  const int splits = scores_splits(rows, vocab);
-  return splits > 1 ? rows * splits * part_bytes(n_alt) : 0;
+  return scores_room(rows, vocab) * part_bytes(n_alt);
 }
 
 extern "C" int tt_token_scores(const void* logits, int32_t type, int64_t rows, int64_t vocab, int64_t stride, float scale,
@@ -589,7 +609,7 @@ extern "C" int tt_token_scores(const void* logits, int32_t type, int64_t rows, i
   if (rows > (int64_t)UINT32_MAX / SC_THREADS) return TT_ERR_TOO_LARGE;
   if (rows == 0) return TT_OK;
   if (!logits || (need && !workspace) || (n_alt && (!alt_ids || !alt_logprobs))) return TT_ERR_NULL_ARG;
-  const int splits = scores_splits(rows, vocab);
+  const int splits = scores_splits(rows, vocab, n_alt);
   auto go = [&](auto zero) {
     using T = decltype(zero);
     return run_scores(ScoreArgs<T>{static_cast<const T*>(logits), rows, vocab, stride, scale, targets, logprobs, stats,

@@ -179,6 +179,38 @@ def test_many_short_rows(gpu, kind, vocab, shift):
         check(z, t, n_alt)
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("rows,vocab,shift", [(24, 41_003, 0), (24, 24_576, 3), (60, 60_001, 1), (200, 82_001, 0), (450, 111_001, 5)])
+def test_long_rows_in_parts(gpu, kind, rows, vocab, shift):
+    """Rows that several blocks share: masks of whole parts, ties across them, sorted rows, rows without a distribution."""
+    z, t = logits_of(rows, vocab, kind, vocab, 1, shift)
+    whole = z.clone()
+    low = torch.finfo(kind).min
+    z[0] = -INF
+    z[1] = low
+    z[2] = 1.5
+    z[3] = torch.sort(z[3].float()).values.to(kind)
+    z[4] = torch.sort(z[4].float(), descending=True).values.to(kind)
+    z[5, vocab // 2] = math.nan
+    z[6, vocab - 1] = INF
+    z[7, : vocab // 2] = -INF
+    z[8, vocab // 7:] = low
+    z[9, :-1] = -INF
+    z[10, 1:] = -INF
+    z[11] = 0.0
+    z[11, 1::2] = -0.0
+    z[12] = torch.round(z[12].float()).to(kind)
+    for r, (mask, left) in enumerate([(-INF, 3), (low, 3), (-INF, 1), (low, vocab // 2), (-INF, vocab // 2), (low, 70)], 13):
+        z[r] = mask
+        keep = torch.randperm(vocab, generator=torch.Generator().manual_seed(r))[:left].to("cuda")
+        z[r, keep] = whole[r, keep]
+    z[20, ::700] = 9.0
+    z[21, -64:] = 9.0
+    z[22, :100] = torch.linspace(5, 8, 100, device="cuda").to(kind)
+    for n_alt in (0, 1, 20, 64):
+        check(z, t, n_alt)
+
+
 def test_targets(gpu):
     z, t = logits_of(40, 1281, torch.float32, 14)
     t[3], t[4], t[5], t[6] = -1, -2**31, 1281, 2**31 - 1
