@@ -965,15 +965,35 @@ struct GradPlan {
   int64_t k_part, parts;  // parts of k in grad_hidden (of every piece alike, so that their sums can go on)
   int64_t factor, sums, g, hidden, weight, bytes;
 };
+// Parts of k, by what they cost: rounds of tiles, each as long as a part, and
+// the parts' sums, written and read again.  SUM is the time of one of these sums
+// in units of one entry of k of a 256 x 256 tile (30 ns).  grad_hidden alone, us:
+// 640 rows of 1,024 at a vocabulary of 50,257: 12 parts 187, the 21 that fill the
+// chip with wide tiles 214, one 684; 2,048 of 2,048 at 100,257: 4 parts 1,590, 8
+// 1,635, one 2,539; 1,500 of 4,096: 8 parts 2,307, 2 2,335, one 2,745.
+constexpr double SUM = 8.0 / 5e12 / 30e-9;
+int64_t parts_of_k(int64_t rows, int64_t width, int64_t piece) {
+  const int64_t m = div_up(width, 256), wide = m * div_up(rows, 256), slim = m * div_up(rows, 128);
+  int64_t most = div_up(piece, 1024), best = 1;  // at least 16 steps of k each
+  if (most > 64) most = 64;
+  double least = 0;
+  for (int64_t n = 1; n <= most; n++) {
+    const double w = (double)div_up(wide * n, CUS), s = (double)div_up(slim * n, CUS) * NARROW;
+    const double time = (w < s ? w : s) * (double)up(div_up(piece, n), 64) + (n > 1 ? SUM * (double)(n * rows * width) : 0);
+    if (n == 1 || time < least) {
+      least = time;
+      best = n;
+    }
+    if (wide * n >= 8 * CUS) break;  // the last round no longer counts
+  }
+  return best;
+}
 // pack: hidden and weight are copied to aligned rows
 GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
   GradPlan p;
   p.padded = up(rows, 64);
   p.wide = up(width, 8);
-  p.parts = CUS / (div_up(width, 256) * div_up(rows, 256));
-  const int64_t most = div_up(piece, 1024);  // at least 16 steps of k each
-  if (p.parts > most) p.parts = most;
-  if (p.parts < 1) p.parts = 1;
+  p.parts = parts_of_k(rows, width, piece);
   p.k_part = up(div_up(piece, p.parts), 64);
   p.parts = div_up(piece, p.k_part);
   int64_t at = 0;
@@ -1052,6 +1072,7 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
   const bool aligned = vectors(c.hidden, c.width) && vectors(c.weight, c.width);
   // the largest piece of the vocabulary that the workspace holds
   int64_t piece = PIECE, most = up(vocab < MOST_PIECE ? vocab : MOST_PIECE, PIECE);
+  if (grad_plan(rows, c.width, most, !aligned).bytes <= c.work_bytes) piece = most;
   while (piece < most) {
     const int64_t mid = up((piece + most) / 2, PIECE);
     if (grad_plan(rows, c.width, mid, !aligned).bytes <= c.work_bytes) piece = mid;
