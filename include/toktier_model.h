@@ -145,7 +145,8 @@ int tt_head_scores(const void* hidden, int64_t hidden_stride, const void* weight
  * gradient with respect to them is rounded to the type of hidden before it is
  * multiplied by weight and hidden (for TT_F16 after it was scaled by a power of
  * two that brings its largest possible value near the type's), and those
- * products are summed in 32 bits.
+ * products are summed in 32 bits.  For up to 256 rows what that rounding takes
+ * off is kept too and multiplied with the rest.
  *   grad_hidden = G weight, grad_weight = G^T hidden, G as in
  *   tt_token_scores_grad.
  * The workspace function gives the least size, which works through the

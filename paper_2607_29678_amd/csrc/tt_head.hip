@@ -380,6 +380,11 @@ struct HeadArgs {
   int32_t m_tiles, n_tiles;
 };
 
+// Bound by the matrix cores: 4,001 rows of 2,048 at 100,257 entries in bf16 take
+// 1.48 ms with the join, 1.11 PFLOP/s (the library's plain product of 4,096 rows
+// takes 1.46 and writes 0.8 GB of logits that would be read again).  Four
+// waves share a tile of 256 x 256, so that each keeps 128 x 128 sums in half of its
+// registers: the fewest LDS reads a product that fit.
 template <class Tl>
 __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_kernel(HeadArgs<typename Tl::Elem> a) {
   __shared__ typename Tl::Shared sh;
@@ -474,6 +479,8 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
 // Blocks begin at different k: rows are often a power of two apart, and blocks in
 // step would ask the same few memory channels.
 // Every lane keeps the statistics of its own entries of a column to the end.
+// 4 rows of 2,048 at 50,257 entries: 45-47 us, 206 MB of weights at 4.5 TB/s; of
+// 4,096 at 100,257, where start and end weigh less: 5.9 TB/s.
 template <class T, int BN_>
 struct Stream {
   using Elem = T;
@@ -690,12 +697,16 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, float mos
   out[1] = ldexpf(1.f, -e);
 }
 
-// Copies rows of any alignment into aligned ones with zeros behind them.
+// Copies rows of any alignment into aligned ones with zeros behind them.  Where
+// `second` is not 0, the rows stand again from row `second` on, zeros in between.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < in.rows * stride; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride, int64_t second) {
+  const int64_t rows = second ? second : in.rows;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * stride; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / stride, col = i - row * stride;
-    out[i] = col < width ? in.p[row * in.stride + col] : (T)0.f;
+    const T x = col < width && row < in.rows ? in.p[row * in.stride + col] : (T)0.f;
+    out[i] = x;
+    if (second && row < in.rows) out[i + second * stride] = x;
   }
 }
 
@@ -707,7 +718,7 @@ struct GradLogitsArgs {
   const int32_t* targets;
   const float *stats, *entropy, *grad_logprobs, *grad_entropy;
   const float* factor;  // NULL: 1
-  T* g;                 // [g_rows][g_stride], both multiples of 64
+  T* g;                 // [g_rows][g_stride], both multiples of 64; SPLIT: [2][g_rows][g_stride]
   int64_t g_stride, g_rows;
   int32_t m_tiles, n_tiles;
 };
@@ -737,8 +748,12 @@ __device__ __forceinline__ void for_rows(typename Tl::Shared& sh, F put) {
   }
 }
 
-// G, zero past the last row and the piece's last entry.
-template <class Tl>
+// G, zero past the last row and the piece's last entry.  SPLIT: G rounded, and
+// behind it what the rounding took off, rounded.  The three products of 2,048 rows
+// of 2,048 at 100,257 entries in bf16 take 2.36 ms, 1.07 PFLOP/s; this one, with
+// an exponential an entry behind it, 0.90 ms of them, grad_weight's 0.74 (1.13
+// PFLOP/s) and grad_hidden's 0.69 (1.22).
+template <class Tl, bool SPLIT>
 __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsArgs<typename Tl::Elem> a) {
   using T = typename Tl::Elem;
   __shared__ typename Tl::Shared sh;
@@ -764,12 +779,13 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
       grads[j].a *= factor;
       grads[j].b *= factor;
       grads[j].g *= factor;
+      grads[j].h *= factor;
     }
   }
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
   const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;
-  auto columns = [&](auto whole) {
+  auto columns = [&](auto whole, bool rest) {
     constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
     for (int j = 0; j < Tl::TN; j++) {
@@ -780,6 +796,7 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
       int last = left - Tl::row_of(0, 0);
       if (!WHOLE) asm volatile("" : "+v"(last));  // (opaque: comparisons are not made ahead and kept)
       __builtin_amdgcn_sched_barrier(0);
+      float at_given = 0.f;
       auto four = [&](int i, int q, auto with_given, auto some_zero) {
         using zeros = decltype(some_zero);
         typename Tl::V4 out;
@@ -787,13 +804,22 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
         for (int r = 0; r < 4; r++) {
           const int place = 32 * i + 8 * q + r;
           float y = grad_of(Tl::value(acc, i, j, 4 * q + r), c, g);
-          if (decltype(with_given)::value && place == given) y += g.g;
-          out[r] = (T)((zeros::value && g.zero) || (!WHOLE && place >= last) ? 0.f : y);
+          if (decltype(with_given)::value && place == given) y = at_given;
+          if ((zeros::value && g.zero) || (!WHOLE && place >= last)) y = 0.f;
+          out[r] = (T)(SPLIT && rest ? y - (float)(T)y : y);
         }
         keep_four<Tl>(sh, i, j, q, out);
       };
       // rows without a gradient, and given tokens, are in few tiles
       const bool any = __ballot(given >= 0 || g.zero);
+      if (any) {
+#pragma unroll
+        for (int i = 0; i < Tl::TM; i++)
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (32 * i + 8 * (r >> 2) + (r & 3) == given) at_given = Tl::value(acc, i, j, r);
+        at_given = grad_of_given(at_given, c, g);
+      }
 #pragma unroll
       for (int i = 0; i < Tl::TM; i++) {
 #pragma unroll
@@ -805,12 +831,16 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
       }
     }
   };
-  if (left == Tl::BM) columns(std::true_type{});
-  else columns(std::false_type{});
-  for_rows<Tl>(sh, [&](int row, int m, typename Tl::V8 x) {
-    if (n0 + row < a.g_rows && m0 + m < a.g_stride)
-      *reinterpret_cast<typename Tl::V8*>(a.g + (n0 + row) * a.g_stride + m0 + m) = x;
-  });
+  for (int plane = 0; plane < (SPLIT ? 2 : 1); plane++) {
+    if (plane) __syncthreads();
+    if (left == Tl::BM) columns(std::true_type{}, plane);
+    else columns(std::false_type{}, plane);
+    T* to = a.g + plane * a.g_rows * a.g_stride;
+    for_rows<Tl>(sh, [&](int row, int m, typename Tl::V8 x) {
+      if (n0 + row < a.g_rows && m0 + m < a.g_stride)
+        *reinterpret_cast<typename Tl::V8*>(to + (n0 + row) * a.g_stride + m0 + m) = x;
+    });
+  }
 }
 
 template <class T>
@@ -889,15 +919,21 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void product_kernel(ProductArgs<typ
   });
 }
 
-// out[row][col] = factor * the sum of the parts, for the first `cols` of their rows of `width`
+// out[row][col] = factor * the sum of the parts, for the first `cols` of their rows
+// of `width`; a part has `part_rows` rows, those from `second` on (0: none) more
+// of the same sums.
 template <class T>
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t rows, int64_t width,
-                                                        int64_t cols, const float* factor, T* out, int64_t stride) {
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t part_rows, int64_t second,
+                                                        int64_t rows, int64_t width, int64_t cols, const float* factor,
+                                                        T* out, int64_t stride) {
   const float f = factor ? factor[1] : 1.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
     float y = 0.f;
     const int64_t row = i / cols, col = i - row * cols;
-    for (int p = 0; p < parts; p++) y += sums[(p * rows + row) * width + col];
+    for (int p = 0; p < parts; p++) {
+      y += sums[(p * part_rows + row) * width + col];
+      if (second) y += sums[(p * part_rows + second + row) * width + col];
+    }
     out[row * stride + col] = (T)(y * f);
   }
 }
@@ -958,9 +994,17 @@ int forward_by_rows(HeadArgs<T>& a, hipStream_t st) {
   return run_forward<Tile<T, 256, 256, 2, 2, true>>(a, st);
 }
 
+// Up to so many rows G is kept in two parts, rounded and what that took off, and
+// the products sum both.  With G rounded alone the results are off by 1.4 times
+// their own rounding, as the errors of many entries average out; those of the
+// given tokens of a few rows do not (2.5 times for one row, 1.6 for 128).
+constexpr int64_t SPLIT_ROWS = 256;
+
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
 struct GradPlan {
+  bool split;             // G in two parts, the second `padded` rows behind the first
   int64_t padded;         // rows, up to a multiple of 64
+  int64_t g_rows;         // rows of G that count, those of both parts
   int64_t wide;           // width, up to a multiple of 8
   int64_t k_part, parts;  // parts of k in grad_hidden (of every piece alike, so that their sums can go on)
   int64_t factor, sums, g, hidden, weight, bytes;
@@ -991,9 +1035,11 @@ int64_t parts_of_k(int64_t rows, int64_t width, int64_t piece) {
 // pack: hidden and weight are copied to aligned rows
 GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
   GradPlan p;
+  p.split = rows <= SPLIT_ROWS;
   p.padded = up(rows, 64);
+  p.g_rows = p.split ? p.padded + rows : rows;
   p.wide = up(width, 8);
-  p.parts = parts_of_k(rows, width, piece);
+  p.parts = parts_of_k(p.g_rows, width, piece);
   p.k_part = up(div_up(piece, p.parts), 64);
   p.parts = div_up(piece, p.k_part);
   int64_t at = 0;
@@ -1003,9 +1049,9 @@ GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
     return was;
   };
   p.factor = take(8);
-  p.sums = take(4 * p.parts * rows * p.wide);
-  p.g = take(2 * p.padded * piece);
-  p.hidden = take(pack ? 2 * rows * p.wide : 0);
+  p.sums = take(4 * p.parts * p.g_rows * p.wide);
+  p.g = take((p.split ? 4 : 2) * p.padded * piece);
+  p.hidden = take(p.split ? 2 * p.g_rows * p.wide : pack ? 2 * rows * p.wide : 0);
   p.weight = take(pack ? 2 * piece * p.wide : 0);
   p.bytes = at;
   return p;
@@ -1025,9 +1071,10 @@ struct GradCall {
 };
 
 template <class T>
-hipError_t pack(const Operand<T>& in, int64_t width, T* out, int64_t stride, hipStream_t st) {
+hipError_t pack(const Operand<T>& in, int64_t width, T* out, int64_t stride, hipStream_t st, int64_t second = 0) {
   const int64_t blocks = div_up(in.rows * stride, 1024);
-  return launch(pack_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st, in, width, out, stride);
+  return launch(pack_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st, in, width, out, stride,
+                second);
 }
 
 template <class Tl>
@@ -1053,11 +1100,11 @@ hipError_t grad_hidden_product(const ProductArgs<T>& a, hipStream_t st) {
   return narrow(a.a.rows, a.b.rows, div_up(a.k, a.k_part)) ? product<ByWeight<T, 128>>(a, st)
                                                           : product<ByWeight<T, 256>>(a, st);
 }
-template <class Tl>
+template <class Tl, bool SPLIT = false>
 hipError_t grad_logits(GradLogitsArgs<typename Tl::Elem> a, hipStream_t st) {
   a.m_tiles = (int32_t)div_up(a.weight.rows, Tl::BM);
   a.n_tiles = (int32_t)div_up(a.hidden.rows, Tl::BN);
-  return launch(grad_logits_kernel<Tl>, dim3((uint32_t)((int64_t)a.m_tiles * a.n_tiles)), dim3(Tl::THREADS), st, a);
+  return launch(grad_logits_kernel<Tl, SPLIT>, dim3((uint32_t)((int64_t)a.m_tiles * a.n_tiles)), dim3(Tl::THREADS), st, a);
 }
 
 template <class T>
@@ -1091,12 +1138,12 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     factor = f;
   }
   Operand<T> hidden = c.hidden;
-  if (!aligned) {
+  if (!aligned || p.split) {
     T* to = reinterpret_cast<T*>(c.work + p.hidden);
-    if (bad(pack(c.hidden, c.width, to, p.wide, st))) return TT_ERR_HIP;
+    if (bad(pack(c.hidden, c.width, to, p.wide, st, p.split ? p.padded : 0))) return TT_ERR_HIP;
     hidden = {to, p.wide, rows};
   }
-  const bool direct = p.parts == 1 && piece >= vocab;  // grad_hidden needs no sums in between
+  const bool direct = p.parts == 1 && piece >= vocab && !p.split;  // grad_hidden needs no sums in between
   for (int64_t first = 0; first < vocab; first += piece) {
     const int64_t n = vocab - first < piece ? vocab - first : piece, g_stride = up(n, 64);
     Operand<T> weight{c.weight.p + first * c.weight.stride, c.weight.stride, n};
@@ -1107,16 +1154,17 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     }
     const GradLogitsArgs<T> ga{weight,    hidden,          width,          first,  vocab, c.scale,  c.targets, c.stats,
                                c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.padded,  0, 0};
-    if (bad(narrow(n, rows, 1) ? grad_logits<Tile<T, 256, 128, 2, 2, true>>(ga, st)
-                               : grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st)))
+    if (bad(p.split              ? grad_logits<Tile<T, 256, 128, 2, 2, true>, true>(ga, st)
+            : narrow(n, rows, 1) ? grad_logits<Tile<T, 256, 128, 2, 2, true>>(ga, st)
+                                 : grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st)))
       return TT_ERR_HIP;
     if (c.grad_weight) {
-      const ProductArgs<T> pa{{hidden.p, hidden.stride, width}, {g, g_stride, n}, rows, rows, 0, 0, factor,
+      const ProductArgs<T> pa{{hidden.p, hidden.stride, width}, {g, g_stride, n}, p.g_rows, p.g_rows, 0, 0, factor,
                               c.grad_weight + first * c.grad_weight_stride, c.grad_weight_stride, c.width, nullptr, false};
       if (bad(grad_weight_product(pa, st))) return TT_ERR_HIP;
     }
     if (c.grad_hidden) {
-      const ProductArgs<T> pa{{weight.p, weight.stride, width}, {g, g_stride, rows}, n, direct ? n : p.k_part, 0, 0,
+      const ProductArgs<T> pa{{weight.p, weight.stride, width}, {g, g_stride, p.g_rows}, n, direct ? n : p.k_part, 0, 0,
                               direct ? factor : nullptr, direct ? c.grad_hidden : nullptr, c.grad_hidden_stride, c.width,
                               sums, first > 0};
       if (bad(grad_hidden_product(pa, st))) return TT_ERR_HIP;
@@ -1126,8 +1174,8 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     const int64_t blocks = div_up(rows * c.width, 256);
     const int32_t used = (int32_t)div_up(vocab < piece ? vocab : piece, p.k_part);  // parts of the first piece
     if (bad(launch(sum_parts_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st,
-                   static_cast<const float*>(sums), used, rows, width, c.width, factor, c.grad_hidden,
-                   c.grad_hidden_stride)))
+                   static_cast<const float*>(sums), used, p.g_rows, p.split ? p.padded : 0, rows, width, c.width, factor,
+                   c.grad_hidden, c.grad_hidden_stride)))
       return TT_ERR_HIP;
   }
   return TT_OK;

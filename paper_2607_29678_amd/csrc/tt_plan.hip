@@ -9,6 +9,11 @@
 // second launch, or a wait between blocks, would cost more than the repeated
 // sums up to the few thousand requests that a step has.
 //
+// What bounds it is latency: a chain of two loads, the sums and a search in LDS.
+// 96 requests of one token take 7.0 us, 301 of
+// 16,381 tokens 8.1, 64 of 420,000 tokens 8.8: 24 bytes written and 4 read a
+// token, 11.8 MB, at 1.3 TB/s.
+//
 // Page numbers of new pages are read from the stack of free pages, not from
 // the table that some other block may or may not have written yet.
 #include "../../include/toktier_model.h"

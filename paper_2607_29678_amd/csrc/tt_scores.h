@@ -118,10 +118,12 @@ __device__ __forceinline__ float given_log_prob(int32_t target, int64_t vocab, f
   return target < vocab ? log_prob(x, r, scale) : __builtin_nanf("");
 }
 
-// The gradient of a row with respect to its logits, G_j = a p_j + b p_j d_j
-// (+ at the given token: g), with p_j = 2^d_j and d_j = (x_j - m) c - log2 s.
+// The gradient of a row with respect to its logits, G_j = a p_j + b p_j d_j with
+// p_j = 2^d_j and d_j = (x_j - m) c - log2 s.  At the given token a p_j + g would
+// cancel where p_j is near 1 (a sure token: 1 - p_j of 3e-4 would keep 11 bits),
+// so there it is h p_j + b p_j d_j - g (p_j - 1): h is the entropy's share of a.
 struct RowGrad {
-  float m, l2, a, b, g;
+  float m, l2, a, b, g, h;
   int32_t target;
   bool zero;
 };
@@ -139,6 +141,7 @@ __device__ __forceinline__ RowGrad row_grad(const int32_t* targets, const float*
   r.a = -scale * (gl + ge * h);
   r.b = -scale * ge * LN2;
   r.g = scale * gl;
+  r.h = -scale * ge * h;
   r.zero = (gl == 0.f && ge == 0.f) || log_s == NEG_INF;
   if (r.target >= vocab) r.a = __builtin_nanf("");
   return r;
@@ -147,6 +150,10 @@ __device__ __forceinline__ RowGrad row_grad(const int32_t* targets, const float*
 __device__ __forceinline__ float grad_of(float x, float c, const RowGrad& r) {
   const float d = fmaf(x - r.m, c, -r.l2);
   return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, -1e4f), r.b, r.a);
+}
+__device__ __forceinline__ float grad_of_given(float x, float c, const RowGrad& r) {
+  const float d = fmaf(x - r.m, c, -r.l2);
+  return fmaf(__builtin_amdgcn_exp2f(d), fmaf(fmaxf(d, -1e4f), r.b, r.h), -r.g * expm1f(d * LN2));
 }
 
 inline bool score_type(int32_t type) { return type == TT_F32 || type == TT_BF16 || type == TT_F16; }

@@ -262,7 +262,10 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
   __syncthreads();
 }
 
-// One part of one row per block.
+// One part of one row per block (or wave).  Bound by reading the logits:
+// 2,048 rows of 100,257 in bf16 with 20 alternatives take 82 us, 5.0 TB/s (a
+// large copy moves 5.0 here), 8 rows with 5 alternatives in 17 parts 7 us and
+// 4-5 to join them: latency.
 template <class T, bool ALT, int THREADS>
 __global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
   __shared__ std::conditional_t<ALT, ScoreShared<THREADS>, SumShared<THREADS>> sh;
@@ -537,29 +540,29 @@ __global__ __launch_bounds__(THREADS) void scores_grad_kernel(GradArgs<T> a) {
     if (v + k * THREADS < vecs) x[k] = load_vec(in + sp.head + (int64_t)(v + k * THREADS) * N);
   const RowGrad g = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, row, a.vocab, a.scale);
   const float c = a.scale * LOG2E;
-  auto one = [&](float x, bool given) {
-    if (g.zero) return (T)0.f;
-    const float z = grad_of(x, c, g);
-    return (T)(given ? z + g.g : z);
-  };
+  auto one = [&](float x) { return (T)(g.zero ? 0.f : grad_of(x, c, g)); };
+  auto edge = [&](float x, bool given) { return given && !g.zero ? (T)grad_of_given(x, c, g) : one(x); };
 #pragma unroll
   for (int k = 0; k < U; k++) {
     const int w = v + k * THREADS;
     if (w >= vecs) continue;
     Vec<T> z;
     const int64_t at = g.target - (sp.head + (int64_t)w * N);  // place of the given token in this vector
+#pragma unroll
+    for (int i = 0; i < N; i++) z.v[i] = one((float)x[k].v[i]);
     if (at >= 0 && at < N) {
+      float given = 0.f;
 #pragma unroll
-      for (int i = 0; i < N; i++) z.v[i] = one((float)x[k].v[i], i == (int)at);
-    } else {
+      for (int i = 0; i < N; i++) given = i == (int)at ? (float)x[k].v[i] : given;
+      const T y = edge(given, true);
 #pragma unroll
-      for (int i = 0; i < N; i++) z.v[i] = one((float)x[k].v[i], false);
+      for (int i = 0; i < N; i++) z.v[i] = i == (int)at ? y : z.v[i];
     }
     store_vec_once(out + sp.head + (int64_t)w * N, z);
   }
-  if (chunk == 0 && tid < sp.head) out[tid] = one((float)in[tid], tid == g.target);
+  if (chunk == 0 && tid < sp.head) out[tid] = edge((float)in[tid], tid == g.target);
   if (chunk + 1 == (uint32_t)a.chunks && sp.tail + tid < a.vocab)
-    out[sp.tail + tid] = one((float)in[sp.tail + tid], sp.tail + tid == g.target);
+    out[sp.tail + tid] = edge((float)in[sp.tail + tid], sp.tail + tid == g.target);
 }
 
 template <class T>
