@@ -697,16 +697,15 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, float mos
   out[1] = ldexpf(1.f, -e);
 }
 
-// Copies rows of any alignment into aligned ones with zeros behind them.  Where
-// `second` is not 0, the rows stand again from row `second` on, zeros in between.
+// Copies rows of any alignment into aligned ones with zeros behind them, and all
+// rows again behind those where they are wanted twice.
 template <class T>
-__global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride, int64_t second) {
-  const int64_t rows = second ? second : in.rows;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * stride; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride, bool twice) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < in.rows * stride; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / stride, col = i - row * stride;
-    const T x = col < width && row < in.rows ? in.p[row * in.stride + col] : (T)0.f;
+    const T x = col < width ? in.p[row * in.stride + col] : (T)0.f;
     out[i] = x;
-    if (second && row < in.rows) out[i + second * stride] = x;
+    if (twice) out[i + in.rows * stride] = x;
   }
 }
 
@@ -718,7 +717,7 @@ struct GradLogitsArgs {
   const int32_t* targets;
   const float *stats, *entropy, *grad_logprobs, *grad_entropy;
   const float* factor;  // NULL: 1
-  T* g;                 // [g_rows][g_stride], both multiples of 64; SPLIT: [2][g_rows][g_stride]
+  T* g;                 // [g_rows][g_stride], both multiples of 64; SPLIT: [2][rows][g_stride]
   int64_t g_stride, g_rows;
   int32_t m_tiles, n_tiles;
 };
@@ -784,11 +783,12 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
   }
   f32x16 acc[Tl::TM][Tl::TN];
   Tl::multiply(a.weight, a.hidden, m0, n0, 0, a.width, sh, acc);
-  const int left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;
+  const int lane = threadIdx.x & 63, left = a.weight.rows - m0 < Tl::BM ? (int)(a.weight.rows - m0) : Tl::BM;
   auto columns = [&](auto whole, bool rest) {
     constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
     for (int j = 0; j < Tl::TN; j++) {
+      if (SPLIT && n0 + Tl::col_of(j) - (lane & 31) >= a.hidden.rows) continue;  // (the same for the wave)
       const RowGrad& g = grads[j];
       // an entry's place is 32 i + 8 (r / 4) + r % 4 from the lane's first one
       const int64_t at = g.target - a.first - m0 - Tl::row_of(0, 0);
@@ -919,20 +919,20 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void product_kernel(ProductArgs<typ
   });
 }
 
-// out[row][col] = factor * the sum of the parts, for the first `cols` of their rows
-// of `width`; a part has `part_rows` rows, those from `second` on (0: none) more
-// of the same sums.
+// out[row][col] = factor * the sum of the parts, for the first `cols` of their rows of `width`
 template <class T>
-__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t part_rows, int64_t second,
-                                                        int64_t rows, int64_t width, int64_t cols, const float* factor,
-                                                        T* out, int64_t stride) {
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float* sums, int32_t parts, int64_t rows, int64_t width,
+                                                        int64_t cols, const float* factor, T* out, int64_t stride) {
   const float f = factor ? factor[1] : 1.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
     float y = 0.f;
     const int64_t row = i / cols, col = i - row * cols;
-    for (int p = 0; p < parts; p++) {
-      y += sums[(p * part_rows + row) * width + col];
-      if (second) y += sums[(p * part_rows + second + row) * width + col];
+    for (int p0 = 0; p0 < parts; p0 += 8) {  // (eight parts under way: with few rows there is nothing else to wait on)
+      float x[8];
+#pragma unroll
+      for (int p = 0; p < 8; p++) x[p] = p0 + p < parts ? sums[((p0 + p) * rows + row) * width + col] : 0.f;
+#pragma unroll
+      for (int p = 0; p < 8; p++) y += x[p];
     }
     out[row * stride + col] = (T)(y * f);
   }
@@ -997,12 +997,15 @@ int forward_by_rows(HeadArgs<T>& a, hipStream_t st) {
 // Up to so many rows G is kept in two parts, rounded and what that took off, and
 // the products sum both.  With G rounded alone the results are off by 1.4 times
 // their own rounding, as the errors of many entries average out; those of the
-// given tokens of a few rows do not (2.5 times for one row, 1.6 for 128).
+// given tokens of a few rows do not (2.5 times for one row, 1.6 for 128).  us with
+// G rounded alone and in two parts, bf16: one row of 1,024 at a vocabulary of
+// 50,257 97 / 98, 64 105 / 124, 256 154 / 220; 256 of 2,048 at 100,257 489 /
+// 702.  More rows would pay up to two thirds for what averages out.
 constexpr int64_t SPLIT_ROWS = 256;
 
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
 struct GradPlan {
-  bool split;             // G in two parts, the second `padded` rows behind the first
+  bool split;             // G in two parts, one after the other
   int64_t padded;         // rows, up to a multiple of 64
   int64_t g_rows;         // rows of G that count, those of both parts
   int64_t wide;           // width, up to a multiple of 8
@@ -1037,7 +1040,7 @@ GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
   GradPlan p;
   p.split = rows <= SPLIT_ROWS;
   p.padded = up(rows, 64);
-  p.g_rows = p.split ? p.padded + rows : rows;
+  p.g_rows = p.split ? 2 * rows : rows;
   p.wide = up(width, 8);
   p.parts = parts_of_k(p.g_rows, width, piece);
   p.k_part = up(div_up(piece, p.parts), 64);
@@ -1050,7 +1053,7 @@ GradPlan grad_plan(int64_t rows, int64_t width, int64_t piece, bool pack) {
   };
   p.factor = take(8);
   p.sums = take(4 * p.parts * p.g_rows * p.wide);
-  p.g = take((p.split ? 4 : 2) * p.padded * piece);
+  p.g = take(2 * (p.split ? p.g_rows : p.padded) * piece);
   p.hidden = take(p.split ? 2 * p.g_rows * p.wide : pack ? 2 * rows * p.wide : 0);
   p.weight = take(pack ? 2 * piece * p.wide : 0);
   p.bytes = at;
@@ -1071,10 +1074,10 @@ struct GradCall {
 };
 
 template <class T>
-hipError_t pack(const Operand<T>& in, int64_t width, T* out, int64_t stride, hipStream_t st, int64_t second = 0) {
+hipError_t pack(const Operand<T>& in, int64_t width, T* out, int64_t stride, hipStream_t st, bool twice = false) {
   const int64_t blocks = div_up(in.rows * stride, 1024);
   return launch(pack_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st, in, width, out, stride,
-                second);
+                twice);
 }
 
 template <class Tl>
@@ -1140,7 +1143,7 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
   Operand<T> hidden = c.hidden;
   if (!aligned || p.split) {
     T* to = reinterpret_cast<T*>(c.work + p.hidden);
-    if (bad(pack(c.hidden, c.width, to, p.wide, st, p.split ? p.padded : 0))) return TT_ERR_HIP;
+    if (bad(pack(c.hidden, c.width, to, p.wide, st, p.split))) return TT_ERR_HIP;
     hidden = {to, p.wide, rows};
   }
   const bool direct = p.parts == 1 && piece >= vocab && !p.split;  // grad_hidden needs no sums in between
@@ -1153,7 +1156,7 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
       weight = {to, p.wide, n};
     }
     const GradLogitsArgs<T> ga{weight,    hidden,          width,          first,  vocab, c.scale,  c.targets, c.stats,
-                               c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.padded,  0, 0};
+                               c.entropy, c.grad_logprobs, c.grad_entropy, factor, g,     g_stride, p.split ? rows : p.padded, 0, 0};
     if (bad(p.split              ? grad_logits<Tile<T, 256, 128, 2, 2, true>, true>(ga, st)
             : narrow(n, rows, 1) ? grad_logits<Tile<T, 256, 128, 2, 2, true>>(ga, st)
                                  : grad_logits<Tile<T, 256, 256, 2, 2, true>>(ga, st)))
@@ -1174,8 +1177,8 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     const int64_t blocks = div_up(rows * c.width, 256);
     const int32_t used = (int32_t)div_up(vocab < piece ? vocab : piece, p.k_part);  // parts of the first piece
     if (bad(launch(sum_parts_kernel<T>, dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), dim3(256), st,
-                   static_cast<const float*>(sums), used, p.g_rows, p.split ? p.padded : 0, rows, width, c.width, factor,
-                   c.grad_hidden, c.grad_hidden_stride)))
+                   static_cast<const float*>(sums), used * (p.split ? 2 : 1), rows, width, c.width, factor, c.grad_hidden,
+                   c.grad_hidden_stride)))
       return TT_ERR_HIP;
   }
   return TT_OK;
