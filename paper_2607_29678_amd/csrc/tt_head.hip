@@ -672,14 +672,21 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
 
 // A power of two that brings the largest possible entry of G near 2^13 (16-bit
 // floats hold up to 65,504, and lose small entries below 2^-14), and its inverse.
-__global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, float most_entropy, float scale,
+// Only gradients that row_grad() passes on count: what stands at a row without a
+// token, or in a row whose G is 0 or no number, must not take the others' bits.
+__global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, int64_t vocab, float most_entropy, float scale,
+                                                         const int32_t* targets, const float* stats,
                                                          const float* grad_logprobs, const float* grad_entropy,
                                                          float* out) {
   __shared__ float part[4];
   float m = 0.f;
   for (int64_t i = threadIdx.x; i < rows; i += 256) {
-    const float g = (grad_logprobs ? fabsf(grad_logprobs[i]) : 0.f) + (grad_entropy ? fabsf(grad_entropy[i]) * most_entropy : 0.f);
-    m = fmaxf(m, g * scale);
+    const int32_t t = targets ? targets[i] : -1;
+    const float log_s = stats[2 * i + 1];
+    const float g = (grad_logprobs && t >= 0 ? fabsf(grad_logprobs[i]) : 0.f) +
+                    (grad_entropy ? fabsf(grad_entropy[i]) * most_entropy : 0.f);
+    // (log s: -inf where there is no distribution, or NaN)
+    if (t < vocab && log_s > NEG_INF && g * scale < __builtin_inff()) m = fmaxf(m, g * scale);
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
@@ -688,7 +695,7 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, float mos
   if (threadIdx.x) return;
   m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
   int e = 0;
-  if (m > 0.f && m < __builtin_inff()) {
+  if (m > 0.f) {
     frexpf(m, &e);  // m < 2^e
     e = 13 - e;
     e = e > 100 ? 100 : e < -100 ? -100 : e;
@@ -1136,7 +1143,8 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
   if (std::is_same<T, f16_t>::value) {
     float* f = reinterpret_cast<float*>(c.work + p.factor);
     const float entropy = logf((float)vocab) + 0.5f;  // |p (log p + H)| <= 1/e + log(vocab)
-    if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, entropy, c.scale, c.grad_logprobs, c.grad_entropy, f)))
+    if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, vocab, entropy, c.scale, c.targets, c.stats, c.grad_logprobs,
+                   c.grad_entropy, f)))
       return TT_ERR_HIP;
     factor = f;
   }
