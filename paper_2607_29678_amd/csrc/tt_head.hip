@@ -438,15 +438,18 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
             if (32 * i + 8 * (r >> 2) + (r & 3) == given) x = Tl::value(acc, i, j, r);
         if (mine) a.given[t] = x;
       }
+      const float less = smaller(m, __shfl_xor(m, 32));
       m = larger(m, __shfl_xor(m, 32));
       const Reference ref = reference(m, c);
       Stats st = {m, 0.f, 0.f};
+      float left_out = NEG_INF;  // (ends as the lane's largest entry)
       if (!WHOLE) asm volatile("" : "+v"(last));
       auto sums = [&](auto plain) {
 #pragma unroll
         for (int i = 0; i < Tl::TM; i++) {
 #pragma unroll
-          for (int r = 0; r < 16; r++) add_entry<decltype(plain)::value>(st, entry(i, r), ref, c);
+          for (int r = 0; r < 16; r += 2)
+            add_two<decltype(plain)::value>(st, left_out, entry(i, r), entry(i, r + 1), ref, c);
           __builtin_amdgcn_sched_barrier(0);  // (the accumulators do not fit the other registers all at once)
         }
       };
@@ -454,6 +457,7 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
       else sums(std::false_type{});
       st.s += __shfl_xor(st.s, 32);
       st.u += __shfl_xor(st.u, 32);
+      add_entry<false>(st, less, ref, c);  // (of the two lanes' largest entries only the larger one is left out)
       if (lane < 32) joined[wm * Tl::BN + col] = {m, st.s, st.u, 0.f};
     }
   };
@@ -608,10 +612,11 @@ __global__ __launch_bounds__(128, 1) void head_stream_kernel(HeadArgs<typename S
         if (at >= last) acc[j][r] = NEG_INF;
         m = larger(m, acc[j][r]);
       }
+      float left_out = st[j].m;
       lower(st[j], m, c);
       const Reference ref = reference(m, c);
 #pragma unroll
-      for (int r = 0; r < 16; r++) add_entry<false>(st[j], acc[j][r], ref, c);
+      for (int r = 0; r < 16; r += 2) add_two<false>(st[j], left_out, acc[j][r], acc[j][r + 1], ref, c);
     }
   }
   loads_done_but<0>();
@@ -648,16 +653,20 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
     float m = st.m;
 #pragma unroll
     for (int k = 0; k < U; k++) m = larger(m, q[k].m);
+    float left_out = st.m;
     lower(st, m, c);
+    const Reference ref = reference(m, c);
 #pragma unroll
     for (int k = 0; k < U; k++) {
       Stats o = {q[k].m, q[k].s, q[k].u};
       lower(o, m, c);
       st.s += o.s;
       st.u += o.u;
+      add_entry<false>(st, smaller(left_out, q[k].m), ref, c);
+      left_out = larger(left_out, q[k].m);
     }
   }
-  st = wave_join(st, c);
+  st = wave_join(st, st.m, c);
   if (lane) return;
   const RowScores r = row_scores(st, c);
   if (logprobs) logprobs[row] = given_log_prob(t, vocab, x_given, r, scale);

@@ -16,26 +16,28 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
 
-// The larger of two, NaN if either is: a row's maximum carries its NaNs.
+// The larger (smaller) of two, NaN if either is: a row's maximum carries its NaNs.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 
-// Statistics of a part of a row, in powers of two: m the largest logit, s the
-// sum of e_j = 2^d_j and u the sum of e_j d_j, d_j = x_j c - R with c =
-// scale / log 2 and R the rounded product m c.  How far R is off m c is made up
-// for wherever sums of different m meet (rounded_off), so that one fused
-// multiply-add an entry gives d_j.  Where m c is too large for that (masks of
-// the type's lowest value overflow), d_j = (x_j - m) c.  d_j is held at -126 or
-// more: 2^-126 is nothing next to the largest entry's 1, and 0 times -inf does
-// not arise.
+// Statistics of a part of a row, in powers of two: m the largest logit, and over
+// all entries but one of those that m is of, s the sum of e_j = 2^d_j and u the
+// sum of e_j d_j.  That one entry is left out so that what the others come to
+// keeps its bits where the row is nearly sure of it (next to a 1, a sum of 1e-5
+// would keep 7 of its 24 bits).
+// d_j = x_j c - R with c = scale / log 2 and R the rounded product m c.  How far
+// R is off m c is made up for wherever sums of different m meet (rounded_off), so
+// that one fused multiply-add an entry gives d_j.  Where m c is too large for that
+// (masks of the type's lowest value overflow), d_j = (x_j - m) c.
 struct Stats {
   float m, s, u;
 };
 constexpr float PLAIN_MOST = 1048576.f;
-constexpr float LEAST_EXPONENT = -126.f;
+constexpr float LEAST_EXPONENT = -126.f;  // 2^d is 0 or next to it below
 
 __device__ __forceinline__ Stats empty_stats() { return {NEG_INF, 0.f, 0.f}; }
 
-// d_j = max((x_j - base) c + off, -126); base is 0 for all but huge m
+// d_j = (x_j - base) c + off; base is 0 for all but huge m
 struct Reference {
   float base, off;
 };
@@ -48,18 +50,28 @@ __device__ __forceinline__ Reference reference(float m, float c) {
 __device__ __forceinline__ float rounded_off(float m, float c) {
   return m != NEG_INF && is_plain(m, c) ? -fmaf(m, c, -(m * c)) : 0.f;
 }
-// PLAIN: base is known to be 0
+// PLAIN: base is known to be 0.  (-inf adds 0: d is held for the product alone)
 template <bool PLAIN>
 __device__ __forceinline__ void add_entry(Stats& st, float x, const Reference& r, float c) {
-  const float d = fmaxf(fmaf(PLAIN ? x : x - r.base, c, r.off), LEAST_EXPONENT), e = __builtin_amdgcn_exp2f(d);
+  const float d = fmaf(PLAIN ? x : x - r.base, c, r.off), e = __builtin_amdgcn_exp2f(d);
   st.s += e;
-  st.u = fmaf(e, d, st.u);
+  st.u = fmaf(e, fmaxf(d, LEAST_EXPONENT), st.u);
+}
+// Two entries and the largest before them: the largest of the three goes on in
+// `top`, the other two are added.
+template <bool PLAIN>
+__device__ __forceinline__ void add_two(Stats& st, float& top, float x, float y, const Reference& r, float c) {
+  const float low = smaller(smaller(top, x), y), mid = __builtin_amdgcn_fmed3f(top, x, y);
+  top = larger(larger(top, x), y);
+  add_entry<PLAIN>(st, low, r, c);
+  add_entry<PLAIN>(st, mid, r, c);
 }
 
 // e d for e = 2^d: 0 where e is 0, also for d = -inf; NaN stays.
 __device__ __forceinline__ float weigh(float e, float d) { return e * fmaxf(d, -1e30f); }
 
-// a's sums moved to the larger maximum m.
+// a's sums moved to the larger maximum m.  The entry that a left out is not
+// among them: it is the caller's to add, or to go on leaving out.
 __device__ __forceinline__ void lower(Stats& a, float m, float c) {
   if (a.m == m) return;
   if (a.m == NEG_INF) {
@@ -73,18 +85,24 @@ __device__ __forceinline__ void lower(Stats& a, float m, float c) {
 }
 
 __device__ __forceinline__ Stats join(Stats a, Stats b, float c) {
-  const float m = larger(a.m, b.m);
+  const float m = larger(a.m, b.m), less = smaller(a.m, b.m);
   lower(a, m, c);
   lower(b, m, c);
-  return {m, a.s + b.s, a.u + b.u};
+  Stats all = {m, a.s + b.s, a.u + b.u};
+  add_entry<false>(all, less, reference(m, c), c);
+  return all;
 }
 
 // The wave's statistics in every lane: one move to the wave's maximum, then sums.
-__device__ __forceinline__ Stats wave_join(Stats a, float c) {
+// Each lane left out `held`, and some lane's is the wave's maximum.
+__device__ __forceinline__ Stats wave_join(Stats a, float held, float c) {
   float m = a.m;
 #pragma unroll
   for (int d = 32; d; d >>= 1) m = larger(m, __shfl_xor(m, d));
   lower(a, m, c);
+  // every lane but the first of those that hold the maximum adds what it left out
+  const uint64_t top = __ballot(held == m);
+  if ((top & (~top + 1)) != 1ull << (threadIdx.x & 63)) add_entry<false>(a, held, reference(m, c), c);
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
     a.s += __shfl_xor(a.s, d);
@@ -103,8 +121,10 @@ __device__ __forceinline__ RowScores row_scores(const Stats& a, float c) {
     const float nan = __builtin_nanf("");
     return {nan, nan, nan};
   }
-  const float l = __builtin_amdgcn_logf(a.s);  // base 2
-  return {a.m, LN2 * (l + rounded_off(a.m, c)), LN2 * (l - a.u / a.s)};
+  // the sums as of m c itself; the entry left out is a 1 whose exponent is 0
+  const float off = rounded_off(a.m, c), f = __builtin_amdgcn_exp2f(off), s = a.s * f, u = f * fmaf(off, a.s, a.u);
+  const float log_s = log1pf(s);
+  return {a.m, log_s, fmaf(-LN2, u / (1.f + s), log_s)};
 }
 
 // log p of logit x in a row with these results.

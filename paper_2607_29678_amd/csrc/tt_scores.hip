@@ -265,9 +265,11 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
 // One part of one row per block (or wave).  Bound by reading the logits:
 // 2,048 rows of 100,257 in bf16 with 20 alternatives take 82 us, 5.0 TB/s (a
 // large copy moves 5.0 here), 8 rows with 5 alternatives in 17 parts 7 us and
-// 4-5 to join them: latency.
+// 4-5 to join them: latency.  Without alternatives eight waves a SIMD keep more
+// loads under way (2,048 rows of 100,257: 70-73 us; 76 with the 71 registers that
+// the compiler takes of its own accord).
 template <class T, bool ALT, int THREADS>
-__global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
+__global__ __launch_bounds__(THREADS, ALT ? 1 : 8) void scores_kernel(ScoreArgs<T> a) {
   __shared__ std::conditional_t<ALT, ScoreShared<THREADS>, SumShared<THREADS>> sh;
   constexpr int N = Vec<T>::N, U = ALT ? 2 : 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -286,10 +288,13 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
   // the given token's logit (loaded ahead of the sums)
   const int32_t target = a.targets ? a.targets[row] : -1;
   const bool holds_given = target >= c0 && target < c1;
-  const float x_given = holds_given ? (float)p[target - c0] : 0.f;
+  float x_given = holds_given ? (float)p[target - c0] : 0.f;
 
+  // The row's largest entry stays out of the sums (Stats).  That is looked after
+  // only in the steps in which the wave's largest entry, `most`, rises, some log of
+  // their number: each lane then leaves out its largest so far.
   Stats st = empty_stats();
-  float bound = NEG_INF;
+  float held = NEG_INF, most = NEG_INF, bound = NEG_INF;
   // U vectors at a time share one move of the maximum.  The loop runs equally
   // often in every thread: it holds barriers.  The vectors of the next step are
   // under way while the last ones are summed; in the last step a thread repeats
@@ -330,16 +335,27 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
     }
     lower(st, m, c);
     const Reference ref = reference(m, c);
-    auto sums = [&](auto plain) {
+    auto sums = [&](auto plain, auto rises) {
 #pragma unroll
       for (int k = 0; k < U; k++) {
         if (!WHOLE && k * THREADS >= here) continue;
 #pragma unroll
-        for (int i = 0; i < N; i++) add_entry<decltype(plain)::value>(st, x[k][i], ref, c);
+        for (int i = 0; i < N; i += 2) {
+          if (decltype(rises)::value) {
+            add_two<decltype(plain)::value>(st, held, x[k][i], x[k][i + 1], ref, c);
+          } else {
+            add_entry<decltype(plain)::value>(st, x[k][i], ref, c);
+            add_entry<decltype(plain)::value>(st, x[k][i + 1], ref, c);
+          }
+        }
       }
     };
-    if (__ballot(!is_plain(m, c)) == 0) sums(std::true_type{});
-    else sums(std::false_type{});
+    const uint64_t above = __ballot(m > most);
+    for (uint64_t v = above; v; v = __ballot(m > most))
+      most = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), __builtin_ctzll(v)));
+    if (__ballot(!is_plain(m, c))) sums(std::false_type{}, std::true_type{});
+    else if (above) sums(std::true_type{}, std::true_type{});
+    else sums(std::true_type{}, std::false_type{});
     if constexpr (ALT) {
       if ((step & (step + 1)) == 0) bound = bound_of<0x10000u, THREADS>(st.m, a.n_alt, sh);  // after 1, 2, 4, 8 ... steps
 #pragma unroll
@@ -360,17 +376,19 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(ScoreArgs<T> a) {
     }
   };
   if (steps > 0) fetch(0);
+  x_given = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x_given)));  // (no vector register in the loop)
   for (int step = 0; step + 1 < steps; step++) take(step, std::true_type{});
   if (steps > 0) take(steps - 1, std::false_type{});
   auto edge = [&](int64_t j) {
-    const float x = (float)p[j], m = larger(st.m, x);
+    const float x = (float)p[j], m = larger(st.m, x), less = smaller(held, x);
     lower(st, m, c);
-    add_entry<false>(st, x, reference(m, c), c);
+    add_entry<false>(st, less, reference(m, c), c);
+    held = larger(held, x);
   };
   if (tid < sp.head) edge(tid);
   if (sp.tail + tid < sp.n) edge(sp.tail + tid);
   const float mine = st.m;
-  st = wave_join(st, c);
+  st = wave_join(st, held, c);
   if constexpr (THREADS > 64) {
     if (lane == 0) sh.st[wave] = st;
     __syncthreads();
@@ -456,7 +474,7 @@ __global__ __launch_bounds__(SC_THREADS) void scores_join_kernel(ScoreArgs<T> a)
     lists[i] = i < n ? reinterpret_cast<const uint64_t*>(in + part * part_bytes(k) + sizeof(PartHead))[i - part * k] : 0;
   }
   const float x_given = __shfl(head.given, t >= 0 && t < a.vocab ? (int)(t / a.per_part) : 0);
-  const Stats st = wave_join(head.st, c);  // (every wave for itself)
+  const Stats st = wave_join(head.st, head.st.m, c);  // (every wave for itself)
   const RowScores r = row_scores(st, c);
   const bool nan = r.log_s != r.log_s;
   if (tid == 0) {
