@@ -171,8 +171,13 @@ __device__ __forceinline__ float grad_of(float x, float c, const RowGrad& r) {
   const float d = fmaf(x - r.m, c, -r.l2);
   return __builtin_amdgcn_exp2f(d) * fmaf(fmaxf(d, -1e4f), r.b, r.a);
 }
+// A logit that is computed again (by tiles of another shape) differs from the
+// statistics' in its last bits, which next to a small log s are not small.  But
+// where log2 s is below 0.36 all others come to less than 0.29 of the largest
+// entry: one within a factor of 2^-0.7 of it is itself the largest, and d is -log2 s.
 __device__ __forceinline__ float grad_of_given(float x, float c, const RowGrad& r) {
-  const float d = fmaf(x - r.m, c, -r.l2);
+  const bool largest = r.l2 < 0.36f && (x - r.m) * c > -0.7f;
+  const float d = largest ? -r.l2 : fmaf(x - r.m, c, -r.l2);
   return fmaf(__builtin_amdgcn_exp2f(d), fmaf(fmaxf(d, -1e4f), r.b, r.h), -r.g * expm1f(d * LN2));
 }
 

@@ -175,3 +175,26 @@ def test_head_scores_of_sure_rows(gpu, rows, vocab, width, kind, lift):
     near(got["entropy"], e["entropy"], (2 * tol + 2 * off) * e["entropy"] + 2 * off * torch.expm1(e["log_s"]))
     given = torch.where(t < 0, torch.zeros_like(e["log_s"]), e["lp"].gather(1, t.clamp(min=0).long()[:, None])[:, 0])
     near(got["logprobs"], given, tol * given.abs())
+
+
+@pytest.mark.parametrize("kind", TYPES[1:])
+@pytest.mark.parametrize("lift", [6.0, 15.0, 18.0, 21.0])
+@pytest.mark.parametrize("rows,vocab,width", HEADS)
+def test_head_gradients_from_the_scores_own_statistics(gpu, rows, vocab, width, kind, lift):
+    hidden, weight, t = sure_head(rows, vocab, width, kind, lift)
+    t[1::7] = -1
+    z, off, e, got, room = head_scores(hidden, weight, t)
+    # gradients of the log probabilities, large enough that the results are ordinary 16-bit floats
+    a = torch.full((rows,), 4096.0, device="cuda")
+    gh, gw = torch.empty_like(hidden), torch.empty_like(weight)
+    tt.head_scores_grad(hidden, weight, t, got["stats"], None, a, None, gh, gw, workspace=room)
+    torch.cuda.synchronize()
+    h, w = hidden.double(), weight.double()
+    g, size = exact_grad(e, t, a.double(), torch.zeros_like(a).double())
+    unit, least = ref.ROUNDING[kind]
+    rel = 2 * relative_error(e["depth"], vocab) + 6 * off + 16 * ref.U32 + (unit if rows > 256 else 2.0**-16)
+    floor = least * 2  # what is below the smallest 16-bit float beside a gradient of 4096
+    want = g @ w
+    near(gh, want, size @ w.abs() * (rel + vocab * ref.U32) + floor * w.abs().sum(0) + unit * want.abs() + least)
+    want = g.t().contiguous() @ h
+    near(gw, want, size.t().contiguous() @ h.abs() * (rel + rows * ref.U32) + floor * h.abs().sum(0) + unit * want.abs() + least)
