@@ -55,14 +55,15 @@ __device__ __forceinline__ Buffer buffer_at(const void* p) {
 }
 // 16 bytes a lane from the buffer's byte `offset` to LDS, at `to` + 16 lane.
 // Written as assembly, since for the builtin the compiler makes every later
-// read of LDS wait for the load; there is no result register.  (m0 is the
-// compiler's to set before each use of its own; a write of it needs one wait
-// state before its use.)
+// read of LDS wait for the load; there is no result register.  It takes a wait
+// state from the write of m0 to its use, and five from a vector instruction's
+// write of a scalar register to a load's use of it, which the compiler does not
+// look after in here.
 // ONCE: what is read once does not stay in the caches.
 template <bool ONCE = false>
 __device__ __forceinline__ void load_to_lds(Buffer from, uint32_t offset, uint32_t to) {
-  if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(offset), "s"(from));
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from));
+  if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(offset), "s"(from) : "m0", "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(from) : "m0", "memory");
 }
 // Waits for all but the last N of this wave's loads and for its LDS reads, then
 // for the block's other waves.
@@ -321,8 +322,18 @@ struct Tile {
       }
     } while (++s < steps);
     loads_done_but<0>();
-    // (what reads the accumulators by assembly has to wait for the last products itself)
+    // What reads the accumulators by assembly has to wait for the last products
+    // itself: the accumulators go through the wait, so that no product is behind
+    // it and no read ahead of it.
+    auto pass = [&] {
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) asm volatile("" : "+a"(acc[i][j]));
+    };
+    pass();
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+    pass();
   }
 
   // One value of an accumulator, out of an accumulation register where the
