@@ -32,6 +32,10 @@
 extern "C" {
 #endif
 
+/* The current device of the calling thread, on which the calls below enqueue;
+ * TT_ERR_HIP if there is none. */
+int32_t tt_current_device(void);
+
 /* ---- plan of a step -------------------------------------------------------- */
 /* One step of a server with a paged cache: request r has cached[r] tokens in
  * the cache and brings fresh[r] new ones (either may be 0).  The new tokens of

@@ -63,6 +63,7 @@ SIGNATURES = {
 # the same for include/toktier_model.h
 _F = ctypes.c_float
 MODEL_SIGNATURES = {
+    "tt_current_device": (_I32, []),
     "tt_step_plan": (ctypes.c_int, [_P, _P]),
     "tt_token_scores_workspace": (_I64, [_I64, _I64, _I32]),
     "tt_token_scores": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _I32, _P, _P, _P, _I64, _P]),

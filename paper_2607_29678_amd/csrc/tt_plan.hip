@@ -284,6 +284,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void plan_kernel(tt_step s) {
 
 using namespace tt;
 
+extern "C" int32_t tt_current_device(void) {
+  int device = 0;
+  return hipGetDevice(&device) == hipSuccess ? device : TT_ERR_HIP;
+}
+
 extern "C" int tt_step_plan(const tt_step* step, void* stream) {
   if (!step) return TT_ERR_NULL_ARG;
   const tt_step& s = *step;

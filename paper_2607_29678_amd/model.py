@@ -7,9 +7,9 @@ gradients.
 
 Like the rest of the package the functions only check and marshal arguments; PyTorch is not
 imported.  Tensors are device tensors with the attributes of torch's; outputs are the caller's.  The
-calls enqueue on ``stream`` (a HIP stream handle as an int, None for the null stream), which has
-to belong to the tensors' device, and return at once.  The C calls trust the shapes they are told,
-so every shape, type and stride is checked here; a mismatch raises ``ValueError``.
+calls enqueue on ``stream`` (a HIP stream handle as an int, None for the null stream) of the current
+device, which has to be the tensors', and return at once.  The C calls trust the shapes they are told,
+so every shape, type, stride and device is checked here; a mismatch raises ``ValueError``.
 """
 
 import functools
@@ -31,6 +31,17 @@ def _code(dtype):
     return _codes.setdefault(dtype, _NAMES.get(str(dtype))) if code is None else code
 
 
+def _device(t, name):
+    """Device of a call's first tensor.  The launch goes to the current device, so that has to be it."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError("%s must be a device tensor, not on %s" % (name, t.device))
+    current = _lib.load().tt_current_device()
+    if device != current:
+        raise ValueError("%s is on device %d, but device %d is current" % (name, device, current))
+    return device
+
+
 def _flat(t, name, code, shape, device):
     """Address of a contiguous tensor of this type and shape on this device; 0 for None."""
     if t is None:
@@ -45,9 +56,8 @@ def _flat(t, name, code, shape, device):
 
 
 def _matrix(t, name, device, dtype=None, shape=None):
-    """(address, row stride) of a device matrix whose rows are contiguous and do not overlap.  (Every
-    call has one on the first tensor's device, so a host tensor, whose device is -1, stops here.)"""
-    if t.dim() != 2 or t.get_device() != device or device < 0 or (dtype is not None and t.dtype != dtype) or \
+    """(address, row stride) of a device matrix whose rows are contiguous and do not overlap."""
+    if t.dim() != 2 or t.get_device() != device or (dtype is not None and t.dtype != dtype) or \
             (shape is not None and t.shape != shape):
         raise ValueError("%s must be a device matrix%s%s, on device %d with the others, not %s %s on %s"
                          % (name, "" if dtype is None else " of %s" % dtype, "" if shape is None else " of shape %s" % (shape,),
@@ -107,7 +117,7 @@ def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets,
     token, as many as the step may hold; ``result`` (int64, two entries) receives the number of
     tokens and the free pages left, or a negative error code and the count as it was.
     """
-    d, each, room, free = cached.get_device(), cached.shape, slots.shape, free_pages.shape
+    d, each, room, free = _device(cached, "cached"), cached.shape, slots.shape, free_pages.shape
     n = each[0]
     table, stride = _matrix(tables, "tables", d)
     width = tables.shape[1]
@@ -140,7 +150,7 @@ def token_scores(logits, targets, logprobs=None, stats=None, entropy=None, alt_i
     (float32 [rows, 2]) and ``alt_ids`` (int32), ``alt_logprobs`` (float32) [rows, k] for the ``k``
     best alternatives; outputs that are None are not computed.
     """
-    d = logits.get_device()
+    d = _device(logits, "logits")
     p, stride = _matrix(logits, "logits", d)
     kind = _type_of(logits, "logits", (0, 1, 2))
     rows, vocab = logits.shape
@@ -159,7 +169,7 @@ def token_scores_grad(logits, targets, stats, entropy, grad_logprobs, grad_entro
     """``tt_token_scores_grad``: gradient with respect to the logits, into ``grad_logits`` (the
     logits' type and shape; may be the logits).  ``targets``, ``grad_logprobs`` and ``grad_entropy``
     may be None; ``entropy`` may be None with ``grad_entropy``."""
-    d = logits.get_device()
+    d = _device(logits, "logits")
     p, stride = _matrix(logits, "logits", d)
     kind = _type_of(logits, "logits", (0, 1, 2))
     rows, vocab = logits.shape
@@ -189,7 +199,7 @@ def _head(hidden, weight, device):
 def head_scores(hidden, weight, targets, logprobs=None, stats=None, entropy=None, scale=1.0, workspace=None, stream=None):
     """``tt_head_scores``: the scores of ``hidden @ weight.T`` (bfloat16 or float16) without storing it;
     arguments as those of ``token_scores``."""
-    d = hidden.get_device()
+    d = _device(hidden, "hidden")
     head = _head(hidden, weight, d)
     rows, vocab, width = head[5:]
     room, size = _room(workspace, _need("tt_head_scores_workspace", rows, vocab, width), d)
@@ -209,7 +219,7 @@ def head_scores_grad(hidden, weight, targets, stats, entropy, grad_logprobs, gra
                      scale=1.0, workspace=None, stream=None):
     """``tt_head_scores_grad``: gradients with respect to ``hidden`` and ``weight`` (either output may
     be None); the other arguments as those of ``token_scores_grad``."""
-    d = hidden.get_device()
+    d = _device(hidden, "hidden")
     head = _head(hidden, weight, d)
     rows, vocab, width = head[5:]
     gh = (None, width) if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", d, hidden.dtype, (rows, width))
