@@ -126,6 +126,8 @@ def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets,
     if len(each) != 1 or len(room) != 1 or len(free) != 1:
         raise ValueError("cached, slots and free_pages must have one dimension")
     flat = _flat
+    if not -0x80000000 <= page_size <= 0x7FFFFFFF:  # (0 and less the call itself refuses)
+        raise ValueError("page_size %r does not fit 32 bits" % (page_size,))
     step = _STEP.pack(
         n, page_size, width, stride, room[0], free[0], flat(cached, "cached", _I32, each, d),
         flat(fresh, "fresh", _I32, each, d), flat(held, "held", _I32, each, d), flat(ids, "ids", _I32, room, d),

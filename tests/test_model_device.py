@@ -1,4 +1,4 @@
-"""The binding of ``toktier_model.h`` with tensors on another device than the current one: no launch (CPU, stand-ins)."""
+"""What the binding of ``toktier_model.h`` refuses before a launch, without a GPU: other devices, sizes past 32 bits."""
 
 import pytest
 
@@ -91,3 +91,17 @@ def test_tensors_on_several_devices(library):
 def test_the_library_knows_its_device():
     want = torch.cuda.current_device() if torch.cuda.is_available() else _lib_error()
     assert _lib.load().tt_current_device() == want
+
+
+@pytest.mark.parametrize("page_size", [1 << 31, -(1 << 31) - 1, 1 << 40])
+def test_page_sizes_past_32_bits(library, page_size):
+    lib = library(0)
+    f = lambda *s, t=torch.int32: OnDevice(torch.zeros(s, dtype=t), 0)  # noqa: E731
+    args = [f(3), f(3), f(3, 5), f(9), f(1, t=torch.int64), page_size, f(4), f(3), f(3), f(8, t=torch.int64), f(8), f(8),
+            f(2, t=torch.int64)]
+    with pytest.raises(ValueError):
+        tt.step_plan(*args)
+    assert lib.calls == []
+    args[5] = (1 << 31) - 1
+    tt.step_plan(*args)
+    assert lib.calls == ["tt_step_plan"]
