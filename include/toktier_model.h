@@ -151,10 +151,12 @@ int tt_head_scores(const void* hidden, int64_t hidden_stride, const void* weight
 /* Gradients with respect to hidden and weight (either may be NULL: not
  * wanted), rounded once to their type.  The logits are computed again; the
  * gradient with respect to them is rounded to the type of hidden before it is
- * multiplied by weight and hidden (for TT_F16 after it was scaled by a power of
- * two that brings its largest possible value near the type's), and those
- * products are summed in 32 bits.  For up to 256 rows what that rounding takes
- * off is kept too and multiplied with the rest.
+ * multiplied by weight and hidden, and those products are summed in 32 bits.  It
+ * is scaled before that, so that a gradient that many rows share is not rounded;
+ * for TT_F16 the largest possible value of all rows comes to 2^12 to 2^13: entries
+ * below 2^-27 of it lose bits, below 2^-38 they are 0.  For up to 256 rows what the
+ * rounding takes off is kept too and multiplied with the rest: the results' error
+ * is then their own rounding, and with more rows some 1.4 times that in the norm.
  *   grad_hidden = G weight, grad_weight = G^T hidden, G as in
  *   tt_token_scores_grad.
  * The workspace function gives the least size, which works through the

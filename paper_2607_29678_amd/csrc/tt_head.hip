@@ -690,38 +690,53 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
 
 // ---- gradients -------------------------------------------------------------
 
-// A power of two that brings the largest possible entry of G near 2^13 (16-bit
-// floats hold up to 65,504, and lose small entries below 2^-14), and its inverse.
+// What G is multiplied by before it is rounded, and its inverse.  The largest
+// gradient of a log probability becomes a power of two: where all rows have the
+// same one (a mean over rows), its rounding would be in every entry of G alike and
+// not average out (2.2 times the results' own rounding at 1 / 510 in bf16).  And
+// the largest possible entry comes to 2^12 to 2^13, as 16-bit floats hold up to 65,504
+// and lose small entries below 2^-14.
 // Only gradients that row_grad() passes on count: what stands at a row without a
 // token, or in a row whose G is 0 or no number, must not take the others' bits.
 __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, int64_t vocab, float most_entropy, float scale,
                                                          const int32_t* targets, const float* stats,
                                                          const float* grad_logprobs, const float* grad_entropy,
                                                          float* out) {
-  __shared__ float part[4];
-  float m = 0.f;
+  __shared__ float part[2][4];
+  float m = 0.f, ml = 0.f;  // the largest possible entry, the largest gradient of a log probability
   for (int64_t i = threadIdx.x; i < rows; i += 256) {
     const int32_t t = targets ? targets[i] : -1;
     const float log_s = stats[2 * i + 1];
-    const float g = (grad_logprobs && t >= 0 ? fabsf(grad_logprobs[i]) : 0.f) +
-                    (grad_entropy ? fabsf(grad_entropy[i]) * most_entropy : 0.f);
+    const float gl = grad_logprobs && t >= 0 ? fabsf(grad_logprobs[i]) : 0.f;
+    const float g = gl + (grad_entropy ? fabsf(grad_entropy[i]) * most_entropy : 0.f);
     // (log s: -inf where there is no distribution, or NaN)
-    if (t < vocab && log_s > NEG_INF && g * scale < __builtin_inff()) m = fmaxf(m, g * scale);
+    if (t < vocab && log_s > NEG_INF && g * scale < __builtin_inff()) {
+      m = fmaxf(m, g * scale);
+      ml = fmaxf(ml, gl * scale);
+    }
   }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+  for (int d = 32; d; d >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, d));
+    ml = fmaxf(ml, __shfl_xor(ml, d));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    part[0][threadIdx.x >> 6] = m;
+    part[1][threadIdx.x >> 6] = ml;
+  }
   __syncthreads();
   if (threadIdx.x) return;
-  m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  int e = 0;
+  m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
+  ml = fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3]));
+  int e = 0, el = 0;
   if (m > 0.f) {
     frexpf(m, &e);  // m < 2^e
     e = 13 - e;
     e = e > 100 ? 100 : e < -100 ? -100 : e;
   }
-  out[0] = ldexpf(1.f, e);
-  out[1] = ldexpf(1.f, -e);
+  const float x = ml > 0.f ? 2.f * frexpf(ml, &el) : 1.f;  // in [1, 2)
+  out[0] = ldexpf(1.f / x, e);
+  out[1] = ldexpf(x, -e);
 }
 
 // Copies rows of any alignment into aligned ones with zeros behind them, and all
@@ -798,7 +813,7 @@ __global__ __launch_bounds__(Tl::THREADS, 1) void grad_logits_kernel(GradLogitsA
       grads[j] = row_grad(a.targets, a.stats, a.entropy, a.grad_logprobs, a.grad_entropy, t, a.vocab, a.scale);
   }
   const float c = a.scale * LOG2E;
-  if (a.factor) {  // (a power of two)
+  if (a.factor) {
     const float factor = a.factor[0];
 #pragma unroll
     for (int j = 0; j < Tl::TN; j++) {
@@ -1160,7 +1175,7 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
   T* g = reinterpret_cast<T*>(c.work + p.g);
   float* sums = reinterpret_cast<float*>(c.work + p.sums);
   const float* factor = nullptr;
-  if (std::is_same<T, f16_t>::value) {
+  if (std::is_same<T, f16_t>::value || !p.split) {
     float* f = reinterpret_cast<float*>(c.work + p.factor);
     const float entropy = logf((float)vocab) + 0.5f;  // |p (log p + H)| <= 1/e + log(vocab)
     if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, vocab, entropy, c.scale, c.targets, c.stats, c.grad_logprobs,
