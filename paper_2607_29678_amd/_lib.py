@@ -75,7 +75,6 @@ MODEL_SIGNATURES = {
                                            _P, _I64, _P, _I64, _P]),
 }
 TT_F32, TT_BF16, TT_F16 = 0, 1, 2
-TT_MAX_ALTERNATIVES = 64
 
 
 class Step(ctypes.Structure):

@@ -392,7 +392,7 @@ struct HeadArgs {
 };
 
 // Bound by the matrix cores: 4,001 rows of 2,048 at 100,257 entries in bf16 take
-// 1.48 ms with the join, 1.11 PFLOP/s (the library's plain product of 4,096 rows
+// 1.47-1.52 ms with the join, 1.08-1.12 PFLOP/s (the library's plain product of 4,096 rows
 // takes 1.46 and writes 0.8 GB of logits that would be read again).  Four
 // waves share a tile of 256 x 256, so that each keeps 128 x 128 sums in half of its
 // registers: the fewest LDS reads a product that fit.
@@ -495,7 +495,8 @@ __global__ __launch_bounds__(Tl::THREADS, Tl::DIRECT ? 1 : 2) void head_scores_k
 // step would ask the same few memory channels.
 // Every lane keeps the statistics of its own entries of a column to the end.
 // 4 rows of 2,048 at 50,257 entries: 45-47 us, 206 MB of weights at 4.5 TB/s; of
-// 4,096 at 100,257, where start and end weigh less: 5.9 TB/s.
+// 4,096 at 100,257, where start and end weigh less: 5.9 TB/s.  64 rows: 59 us
+// (65 rows by tiles of 256 x 128: 45).
 template <class T, int BN_>
 struct Stream {
   using Elem = T;
@@ -740,7 +741,8 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, int64_t v
 }
 
 // Copies rows of any alignment into aligned ones with zeros behind them, and all
-// rows again behind those where they are wanted twice.
+// rows again behind those where they are wanted twice.  Entry by entry: 50,257
+// rows of 1,024 take 95 us, 2.2 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(Operand<T> in, int64_t width, T* out, int64_t stride, bool twice) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < in.rows * stride; i += (int64_t)gridDim.x * 256) {
@@ -1031,6 +1033,8 @@ int forward_by_rows(HeadArgs<T>& a, hipStream_t st) {
   if (VEC && rows <= 32) return run_stream<Stream<T, 32>>(a, st);
   if (VEC && rows <= 64) return run_stream<Stream<T, 64>>(a, st);
   if (rows <= 64) return run_forward<Tile<T, FEW_TILE, 64, 2, 1, false>>(a, st);
+  // (entry by entry through registers.  At 2,048 x 50,257 with weights off their
+  // alignment: 4 rows 217 us, aligned 47; 300 rows 939 and 97; 2,048 rows 4,406 and 413)
   if (!VEC) return run_forward<Tile<T, 256, 128, 4, 2, false>>(a, st);
   if (narrow(a.weight.rows, rows, 1)) return run_forward<Tile<T, 256, 128, 2, 2, true>>(a, st);
   return run_forward<Tile<T, 256, 256, 2, 2, true>>(a, st);
@@ -1041,8 +1045,8 @@ int forward_by_rows(HeadArgs<T>& a, hipStream_t st) {
 // their own rounding, as the errors of many entries average out; those of the
 // given tokens of a few rows do not (2.5 times for one row, 1.6 for 128).  us with
 // G rounded alone and in two parts, bf16: one row of 1,024 at a vocabulary of
-// 50,257 97 / 98, 64 105 / 124, 256 154 / 220; 256 of 2,048 at 100,257 489 /
-// 702.  More rows would pay up to two thirds for what averages out.
+// 50,257 89 / 97, 64 98 / 126, 128 110 / 151, 256 159 / 227; 256 of 2,048 at
+// 100,257 514 / 731.  More rows would pay up to two thirds for what averages out.
 constexpr int64_t SPLIT_ROWS = 256;
 
 // Layout of the gradients' workspace for pieces of `piece` vocabulary entries.
@@ -1063,7 +1067,7 @@ struct GradPlan {
 constexpr double SUM = 8.0 / 5e12 / 30e-9;
 int64_t parts_of_k(int64_t rows, int64_t width, int64_t piece) {
   const int64_t m = div_up(width, 256), wide = m * div_up(rows, 256), slim = m * div_up(rows, 128);
-  int64_t most = div_up(piece, 1024), best = 1;  // at least 16 steps of k each
+  int64_t most = div_up(piece, 1024), best = 1;  // more than 512 entries of k each (nine steps)
   if (most > 64) most = 64;
   double least = 0;
   for (int64_t n = 1; n <= most; n++) {
@@ -1162,7 +1166,9 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
     return !c.grad_weight || !bad(grad_weight_product(pa, st)) ? TT_OK : TT_ERR_HIP;
   }
   const bool aligned = vectors(c.hidden, c.width) && vectors(c.weight, c.width);
-  // the largest piece of the vocabulary that the workspace holds
+  // The largest piece of the vocabulary that the workspace holds.  640 rows of 1,024
+  // at 50,257 in bf16: 277 us with the ample size and half way to it, 583 with a tenth of
+  // the way from the least one, 2,940 with the least (three launches for 256 entries).
   int64_t piece = PIECE, most = up(vocab < MOST_PIECE ? vocab : MOST_PIECE, PIECE);
   if (grad_plan(rows, c.width, most, !aligned).bytes <= c.work_bytes) piece = most;
   while (piece < most) {

@@ -17,8 +17,9 @@ constexpr int SC_THREADS = 256;
 constexpr int SC_VECS = 192;       // 16-byte vectors with a possible alternative that a wave keeps in LDS
 constexpr int SC_CANDS = 512;      // candidates that are ordered there
 // Many short rows: a wave takes a row, and the reductions at a row's end are one
-// wave's (8,192 rows of 8,449 in bf16: 29 us against 39 with a block a row, with
-// 20 alternatives 52 against 61; at 16,384 entries 47 against 49, at 32,000 alike).
+// wave's.  us with a wave and with a block a row, bf16, without and with 20
+// alternatives: 8,192 rows of 8,449 30 / 47 and 46 / 65, of 16,384 48 / 59 and
+// 68 / 80, 4,096 of 32,000 44 / 51 and 60 / 65 (the bound leaves that to blocks).
 constexpr int64_t WAVE_ROWS = 2048, WAVE_VOCAB = 16384;
 
 // Parts of a row that several blocks take.  A part has a block's start and end
@@ -27,13 +28,13 @@ constexpr int64_t WAVE_ROWS = 2048, WAVE_VOCAB = 16384;
 // the chip without; finding alternatives takes longer and gains earlier.  us whole
 // and in parts (bf16 unless said):
 //   rows x vocab     scores alone       with 8 alternatives
-//      8 x  32,000     6.2 /  6.0          11.9 /  9.7 (11 parts)
-//      8 x 100,257    12.5 /  6.8          22.5 / 11.7 (32)
-//     64 x 100,257    12.8 /  9.3          22.9 / 14.7 (16)
-//    200 x 100,257    15.6 / 15.0          23.7 / 20.5 (5; f32 37.0 / 23.8)
-//    400 x 100,257    19.5 / 23.6          28.8 / 28.5 (2; f32 43.8 / 36.5)
-//    501 x   8,449     6.6 /  8.9           9.1 / 13.7 (2)
-//    700 x 100,257    28.6 / 32.6          34.3 / 36.7 (2)
+//      8 x  32,000     7.5 /  8.0          13.3 / 11.4 (11 parts)
+//      8 x 100,257    13.9 /  7.9          24.3 / 12.4 (32)
+//     64 x 100,257    14.2 / 10.7          24.5 / 15.9 (16)
+//    200 x 100,257    15.6 / 17.1          25.4 / 20.6 (5; f32 37.3 / 23.4)
+//    400 x 100,257    21.7 / 25.8          31.6 / 31.0 (2; f32 44.4 / 36.9)
+//    501 x   8,449     7.7 / 12.0          10.6 / 15.4 (2)
+//    700 x 100,257    30.3 / 35.6          38.0 / 40.8 (2)
 // 64 parts cost more to join than they save (8 rows of 256,000: 18.1 against 12.6).
 constexpr int SC_MAX_SPLITS = 32;
 constexpr int64_t SC_SPLIT_COLS = 2800;   // fewest columns of a part
@@ -262,12 +263,12 @@ __device__ __forceinline__ void find_again(const Span<T>& sp, uint32_t first, in
   __syncthreads();
 }
 
-// One part of one row per block (or wave).  Bound by reading the logits:
-// 2,048 rows of 100,257 in bf16 with 20 alternatives take 82 us, 5.0 TB/s (a
-// large copy moves 5.0 here), 8 rows with 5 alternatives in 17 parts 7 us and
-// 4-5 to join them: latency.  Without alternatives eight waves a SIMD keep more
-// loads under way (2,048 rows of 100,257: 70-73 us; 76 with the 71 registers that
-// the compiler takes of its own accord).
+// One part of one row per block (or wave).  2,048 rows of 100,257 in bf16 take
+// 70-73 us, 5.7 TB/s, and in f32 135, 6.1: bound by reading the logits.  With 20
+// alternatives they take 82-87, 4.9 TB/s: a wave's candidates come on top.  8 rows
+// with 5 alternatives in 17 parts take 7 us and 4-5 to join them: latency.  Without
+// alternatives eight waves a SIMD keep more loads under way (76 us with the 71
+// registers that the compiler takes of its own accord).
 template <class T, bool ALT, int THREADS>
 __global__ __launch_bounds__(THREADS, ALT ? 1 : 8) void scores_kernel(ScoreArgs<T> a) {
   __shared__ std::conditional_t<ALT, ScoreShared<THREADS>, SumShared<THREADS>> sh;
