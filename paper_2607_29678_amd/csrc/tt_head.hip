@@ -699,21 +699,36 @@ __global__ __launch_bounds__(256) void head_join_kernel(const Part* parts, const
 // and lose small entries below 2^-14.
 // Only gradients that row_grad() passes on count: what stands at a row without a
 // token, or in a row whose G is 0 or no number, must not take the others' bits.
-__global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, int64_t vocab, float most_entropy, float scale,
-                                                         const int32_t* targets, const float* stats,
-                                                         const float* grad_logprobs, const float* grad_entropy,
-                                                         float* out) {
-  __shared__ float part[2][4];
+// One block, which has little to do but wait for its loads: those of four rows a
+// thread are under way at once (2,048 rows 5.3 us, 16,384 18.7).
+constexpr int SCALE_THREADS = 1024;
+__global__ __launch_bounds__(SCALE_THREADS) void grad_scale_kernel(int64_t rows, int64_t vocab, float most_entropy,
+                                                                   float scale, const int32_t* targets,
+                                                                   const float* stats, const float* grad_logprobs,
+                                                                   const float* grad_entropy, float* out) {
+  constexpr int U = 4, WAVES = SCALE_THREADS / 64;
+  __shared__ float part[2][WAVES];
+  const int tid = threadIdx.x;
   float m = 0.f, ml = 0.f;  // the largest possible entry, the largest gradient of a log probability
-  for (int64_t i = threadIdx.x; i < rows; i += 256) {
-    const int32_t t = targets ? targets[i] : -1;
-    const float log_s = stats[2 * i + 1];
-    const float gl = grad_logprobs && t >= 0 ? fabsf(grad_logprobs[i]) : 0.f;
-    const float g = gl + (grad_entropy ? fabsf(grad_entropy[i]) * most_entropy : 0.f);
-    // (log s: -inf where there is no distribution, or NaN)
-    if (t < vocab && log_s > NEG_INF && g * scale < __builtin_inff()) {
-      m = fmaxf(m, g * scale);
-      ml = fmaxf(ml, gl * scale);
+  for (int64_t first = tid; first < rows; first += U * SCALE_THREADS) {
+    int32_t t[U];
+    float log_s[U], gl[U], ge[U];
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      const int64_t i = first + k * SCALE_THREADS < rows ? first + k * SCALE_THREADS : first;
+      t[k] = targets ? targets[i] : -1;
+      log_s[k] = stats[2 * i + 1];
+      gl[k] = grad_logprobs ? grad_logprobs[i] : 0.f;
+      ge[k] = grad_entropy ? grad_entropy[i] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      const float l = t[k] >= 0 ? fabsf(gl[k]) * scale : 0.f, g = l + fabsf(ge[k]) * most_entropy * scale;
+      // (log s: -inf where there is no distribution, or NaN)
+      if (t[k] < vocab && log_s[k] > NEG_INF && g < __builtin_inff()) {
+        m = fmaxf(m, g);
+        ml = fmaxf(ml, l);
+      }
     }
   }
 #pragma unroll
@@ -721,14 +736,17 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(int64_t rows, int64_t v
     m = fmaxf(m, __shfl_xor(m, d));
     ml = fmaxf(ml, __shfl_xor(ml, d));
   }
-  if ((threadIdx.x & 63) == 0) {
-    part[0][threadIdx.x >> 6] = m;
-    part[1][threadIdx.x >> 6] = ml;
+  if ((tid & 63) == 0) {
+    part[0][tid >> 6] = m;
+    part[1][tid >> 6] = ml;
   }
   __syncthreads();
-  if (threadIdx.x) return;
-  m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
-  ml = fmaxf(fmaxf(part[1][0], part[1][1]), fmaxf(part[1][2], part[1][3]));
+  if (tid) return;
+#pragma unroll
+  for (int w = 1; w < WAVES; w++) {
+    m = fmaxf(m, part[0][w]);
+    ml = fmaxf(ml, part[1][w]);
+  }
   int e = 0, el = 0;
   if (m > 0.f) {
     frexpf(m, &e);  // m < 2^e
@@ -1184,7 +1202,7 @@ int run_gradients(const GradCall<T>& c, hipStream_t st) {
   if (std::is_same<T, f16_t>::value || !p.split) {
     float* f = reinterpret_cast<float*>(c.work + p.factor);
     const float entropy = logf((float)vocab) + 0.5f;  // |p (log p + H)| <= 1/e + log(vocab)
-    if (bad(launch(grad_scale_kernel, dim3(1), dim3(256), st, rows, vocab, entropy, c.scale, c.targets, c.stats, c.grad_logprobs,
+    if (bad(launch(grad_scale_kernel, dim3(1), dim3(SCALE_THREADS), st, rows, vocab, entropy, c.scale, c.targets, c.stats, c.grad_logprobs,
                    c.grad_entropy, f)))
       return TT_ERR_HIP;
     factor = f;
