@@ -112,8 +112,8 @@ enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 };
  * (ID -1), its whole gradient included.
  * log s comes from the sum of the other entries next to the largest one: where a
  * row is nearly sure of a token, log s, the token's log probability and the
- * entropy are good to some 2^-17 of their own small values, and with them the
- * token's gradient.
+ * entropy are good to some 2^-17 of their own small values (the error of logits
+ * from hidden states included), and with them the token's gradient.
  * Sums are kept in 32 bits; scale is a positive number (1 / temperature). */
 
 /* Workspace of tt_token_scores in bytes, or a negative error code. */
