@@ -1,8 +1,10 @@
 /*
  * toktier_model.h — C ABI of the operators that stand next to the tokenizer,
  * on both sides of a model: the plan of a step's tokens (what a model needs
- * besides the IDs of tt_encode_batch and of session appends) and the scores of
- * given tokens (what comes back from the model about them).
+ * besides the IDs of tt_encode_batch and of session appends), the cache of keys
+ * and values that the plan is of, the adjustment of logits before they are
+ * scored, and the scores of given tokens (what comes back from the model about
+ * them).
  *
  * Conventions
  *  - Those of toktier.h: int64_t sizes, int32_t token IDs, TT_OK or a negative
@@ -90,10 +92,124 @@ typedef struct {
  *  TT_ERR_OOM      fewer free pages than the step needs. */
 int tt_step_plan(const tt_step* step, void* stream);
 
-/* ---- scores of given tokens ------------------------------------------------ */
 /* Element types of the tensors. */
 enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 };
 
+/* ---- keys and values in a paged cache ---------------------------------------- */
+/* The cache that a step's plan is of: key (and value) vectors of dim elements for
+ * each of kv_heads heads in each of page_size slots of each page.  Both have the
+ * same strides, in elements; a slot's number is page * page_size + place in it,
+ * as in tt_step.  dim and the strides are multiples of 8, dim is at most
+ * TT_MAX_HEAD_DIM, and keys and values are aligned to 16 bytes. */
+#define TT_MAX_HEAD_DIM 256
+typedef struct {
+  int32_t type;                 /* TT_BF16 or TT_F16, of every tensor of a call              */
+  int32_t page_size;            /* slots of a page, at least 1                               */
+  int32_t kv_heads;
+  int32_t dim;
+  int64_t pages;                /* below 2^31                                                */
+  int64_t page_stride, slot_stride, head_stride;
+  void* keys;
+  void* values;
+} tt_cache;
+
+/* Keys and values of a step's tokens, [tokens][kv_heads * dim], go to their
+ * slots (those of tt_step; tokens whose slot is not one of the cache's, -1 behind
+ * the last one, are passed over), and on the way the first 2 * pairs elements of
+ * each key head are rotated by the token's position: pair i, the elements x, y at
+ *   i, pairs + i     or, where interleaved,     2 i, 2 i + 1
+ * becomes x cos a - y sin a, x sin a + y cos a with a = positions[t] *
+ * frequencies[i], the product held in 64 bits.  pairs may be 0 (no rotation;
+ * positions and frequencies may be NULL then).
+ * queries [tokens][q_heads * dim], if there are any (NULL: q_heads is 0), are
+ * rotated the same way into rotated, which may be queries (same stride); rows of
+ * tokens without a slot stay as they are.  Each result is computed in 32 bits and
+ * rounded once.  The slots of one call are different ones: where a slot stands
+ * twice, it holds elements of either token. */
+int tt_cache_append(const tt_cache* cache, int64_t tokens, const int64_t* slots, const int32_t* positions,
+                    const float* frequencies, int32_t pairs, int32_t interleaved, const void* keys, int64_t key_stride,
+                    const void* values, int64_t value_stride, int32_t q_heads, const void* queries,
+                    int64_t query_stride, void* rotated, int64_t rotated_stride, void* stream);
+
+/* Attention of a step's tokens over the cache.  Token t of request r (offsets as
+ * in tt_step) is at position p = lengths[r] - offsets[r + 1] + t and sees the
+ * request's tokens j <= p with j > p - window or j < sinks (window 0: all of
+ * them).  Head h of queries [tokens][q_heads * dim], a multiple of kv_heads, is
+ * with head h / (q_heads / kv_heads) of the cache:
+ *   x_j = scale * query . key_j,  out = sum_j exp(x_j) value_j / sum_j exp(x_j)
+ *   logsums[t][h] = log sum_j exp(x_j)          (NULL: not wanted)
+ * tables [n_requests][table_stride] hold table_width entries a request.  A token
+ * that sees nothing (its position is negative) gets 0 and a logsum of -inf; one
+ * that sees a token whose page is not one of the cache's, or is behind the
+ * table's entries, gets NaN.  What a token does not see does not matter, be it
+ * NaN or infinite.  Rows behind offsets[n_requests] stay as they are.
+ * Products and sums are held in 32 bits; exp(x_j - max), at most 1 up to a factor
+ * of 2^8, is rounded to the type before it is multiplied by the values, and the
+ * result is rounded once. */
+typedef struct {
+  int32_t n_requests;
+  int32_t table_width;
+  int64_t table_stride;
+  int64_t tokens;               /* rows of queries and out, below 2^31                       */
+  int32_t q_heads;
+  int32_t window;               /* 0: every token up to its own                              */
+  int32_t sinks;                /* first tokens that stay visible behind the window          */
+  float scale;
+  int64_t query_stride, out_stride;
+  const int32_t* tables;
+  const int32_t* offsets;       /* [n_requests + 1]                                          */
+  const int32_t* lengths;       /* [n_requests] tokens in the cache, the step's among them   */
+  const void* queries;
+  void* out;
+  float* logsums;               /* [tokens][q_heads]                                         */
+} tt_attention;
+int64_t tt_cache_attention_workspace(int64_t tokens, int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t dim);
+int tt_cache_attention(const tt_cache* cache, const tt_attention* step, void* workspace, int64_t workspace_bytes,
+                       void* stream);
+
+/* ---- adjusted logits --------------------------------------------------------- */
+/* What is done to logits [rows][vocab] before a token is chosen or scored.  With c
+ * how often token j stands in the row's history (lists one after the other, row r's
+ * from history_offsets[r] up to history_offsets[r + 1]):
+ *   y = x                                                    where c is 0
+ *   y = (x > 0 ? x / repetition : x * repetition) - presence - frequency * c   else
+ *   y + the row's bias of j       (of the last entry of its list that names j)
+ *   -inf where the row's mask does not allow j, whatever x is
+ * Arrays that are NULL are not applied: per row repetition (1), presence (0),
+ * frequency (0); history with its offsets; bias_ids and bias_values with their
+ * offsets; masks with mask_rows.  Mask m is row m of masks [n_masks][mask_stride],
+ * bit j % 32 of word j / 32 is 1 where j is allowed; mask_rows[r] is the mask of
+ * row r, negative for none, and a number that is no mask makes the row NaN.  IDs
+ * outside the vocabulary are passed over, and offsets are held within their lists.
+ * Rounded once, to the type of the logits. */
+typedef struct {
+  int32_t type;                 /* TT_F32, TT_BF16 or TT_F16                                 */
+  int32_t n_masks;
+  int64_t rows, vocab, stride;
+  int64_t n_history, n_biases, mask_stride;
+  const void* logits;
+  const int32_t* history;       /* [n_history]                                               */
+  const int64_t* history_offsets; /* [rows + 1]                                              */
+  const float* repetition;      /* [rows] positive                                           */
+  const float* presence;        /* [rows]                                                    */
+  const float* frequency;       /* [rows]                                                    */
+  const int32_t* bias_ids;      /* [n_biases]                                                */
+  const float* bias_values;     /* [n_biases]                                                */
+  const int64_t* bias_offsets;  /* [rows + 1]                                                */
+  const uint32_t* masks;
+  const int32_t* mask_rows;     /* [rows]                                                    */
+} tt_adjustment;
+/* out may be the logits (same stride). */
+int tt_adjust_logits(const tt_adjustment* a, void* out, int64_t out_stride, void* stream);
+/* Gradient with respect to the logits from that with respect to the result:
+ * grad_out where c is 0, else grad_out / repetition (x > 0) or grad_out *
+ * repetition; 0 where the mask does not allow the token (presence, frequency and
+ * biases are not looked at).  Both have the type of the logits; grad_logits may be
+ * grad_out (same stride), but not the logits. */
+int tt_adjust_logits_grad(const tt_adjustment* a, const void* grad_out, int64_t grad_out_stride, void* grad_logits,
+                          int64_t grad_logits_stride, void* stream);
+
+/* ---- scores of given tokens ------------------------------------------------ */
 /* The most alternatives of a row. */
 #define TT_MAX_ALTERNATIVES 64
 

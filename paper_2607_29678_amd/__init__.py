@@ -9,8 +9,9 @@ the library sources (``csrc/``), its build script and a thin ctypes binding.
 
 from .tokenizer import (CL100K, DEEPSEEK, GPT2, O200K, PATTERNS, Session, Tokenizer, splice_plan,  # noqa: F401
                         status_string, sync_boundaries)
-from .model import (head_scores, head_scores_grad, head_scores_grad_workspace, head_scores_workspace,  # noqa: F401
-                    step_plan, token_scores, token_scores_grad, token_scores_workspace)
+from .model import (adjust_logits, adjust_logits_grad, cache_append, cache_attention,  # noqa: F401
+                    cache_attention_workspace, head_scores, head_scores_grad, head_scores_grad_workspace,
+                    head_scores_workspace, step_plan, token_scores, token_scores_grad, token_scores_workspace)
 from ._lib import TokTierError  # noqa: F401
 
 

@@ -73,6 +73,11 @@ MODEL_SIGNATURES = {
     "tt_head_scores_grad_workspace": (_I64, [_I64, _I64, _I64, _I32]),
     "tt_head_scores_grad": (ctypes.c_int, [_P, _I64, _P, _I64, _I32, _I64, _I64, _I64, _F, _P, _P, _P, _P, _P, _P, _I64,
                                            _P, _I64, _P, _I64, _P]),
+    "tt_cache_append": (ctypes.c_int, [_P, _I64, _P, _P, _P, _I32, _I32, _P, _I64, _P, _I64, _I32, _P, _I64, _P, _I64, _P]),
+    "tt_cache_attention_workspace": (_I64, [_I64, _I32, _I32, _I32, _I32]),
+    "tt_cache_attention": (ctypes.c_int, [_P, _P, _P, _I64, _P]),
+    "tt_adjust_logits": (ctypes.c_int, [_P, _P, _I64, _P]),
+    "tt_adjust_logits_grad": (ctypes.c_int, [_P, _P, _I64, _P, _I64, _P]),
 }
 TT_F32, TT_BF16, TT_F16 = 0, 1, 2
 
@@ -84,6 +89,30 @@ class Step(ctypes.Structure):
                 ("max_tokens", _I64), ("n_free", _I64), ("cached", _P), ("fresh", _P), ("held", _P), ("ids", _P),
                 ("free_pages", _P), ("free_count", _P), ("tables", _P), ("offsets", _P), ("lengths", _P), ("pages", _P),
                 ("slots", _P), ("positions", _P), ("requests", _P), ("targets", _P), ("result", _P)]
+
+
+class Cache(ctypes.Structure):
+    """``tt_cache``: a paged cache of keys and values."""
+
+    _fields_ = [("type", _I32), ("page_size", _I32), ("kv_heads", _I32), ("dim", _I32), ("pages", _I64), ("page_stride", _I64),
+                ("slot_stride", _I64), ("head_stride", _I64), ("keys", _P), ("values", _P)]
+
+
+class Attention(ctypes.Structure):
+    """``tt_attention``: a step's queries over a paged cache."""
+
+    _fields_ = [("n_requests", _I32), ("table_width", _I32), ("table_stride", _I64), ("tokens", _I64), ("q_heads", _I32),
+                ("window", _I32), ("sinks", _I32), ("scale", _F), ("query_stride", _I64), ("out_stride", _I64), ("tables", _P),
+                ("offsets", _P), ("lengths", _P), ("queries", _P), ("out", _P), ("logsums", _P)]
+
+
+class Adjustment(ctypes.Structure):
+    """``tt_adjustment``: what is done to rows of logits."""
+
+    _fields_ = [("type", _I32), ("n_masks", _I32), ("rows", _I64), ("vocab", _I64), ("stride", _I64), ("n_history", _I64),
+                ("n_biases", _I64), ("mask_stride", _I64), ("logits", _P), ("history", _P), ("history_offsets", _P),
+                ("repetition", _P), ("presence", _P), ("frequency", _P), ("bias_ids", _P), ("bias_values", _P),
+                ("bias_offsets", _P), ("masks", _P), ("mask_rows", _P)]
 
 
 class Options(ctypes.Structure):

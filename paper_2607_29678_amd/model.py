@@ -1,6 +1,8 @@
 """Binding of ``include/toktier_model.h``: the operators next to the tokenizer, on both sides of a model.
 
-``step_plan`` lays the tokens of a step out in a paged cache; ``token_scores`` and ``head_scores``
+``step_plan`` lays the tokens of a step out in a paged cache, ``cache_append`` writes their keys and
+values there (rotated by their positions) and ``cache_attention`` reads them; ``adjust_logits`` applies
+penalties, biases and masks, with its gradient ``adjust_logits_grad``; ``token_scores`` and ``head_scores``
 give the log probabilities of given tokens with entropy (and alternatives), from stored logits or
 from hidden states and the head's weights; ``token_scores_grad`` and ``head_scores_grad`` are their
 gradients.
@@ -137,6 +139,191 @@ def step_plan(cached, fresh, tables, free_pages, free_count, page_size, offsets,
         flat(requests, "requests", _I32, room, d), flat(targets, "targets", _I32, room, d),
         flat(result, "result", _I64, (2,), d))
     _lib.check(_lib.load().tt_step_plan(step, stream), "tt_step_plan")
+
+
+# tt_cache, tt_attention and tt_adjustment, packed the same way
+_CACHE = struct.Struct("@iiiiqqqqPP")
+_ATTENTION = struct.Struct("@iiqqiiifqq6P")
+_ADJUSTMENT = struct.Struct("@iiqqqqqq11P")
+
+
+def _heads(t, name, device, dtype, tokens=None, heads=None, dim=None):
+    """(address, row stride) of a device tensor [tokens, heads, dim] whose rows are contiguous and do not overlap."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype != dtype or t.get_device() != device or (tokens is not None and shape[0] != tokens) or \
+            (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim):
+        raise ValueError("%s must be a %s tensor of [tokens%s, heads%s, dim%s] on device %d with the others, not %s %s on %s"
+                         % (name, dtype, "" if tokens is None else " = %d" % tokens, "" if heads is None else " = %d" % heads,
+                            "" if dim is None else " = %d" % dim, device, t.dtype, tuple(shape), t.device))
+    n, h, d = shape
+    row, head, step = t.stride()
+    if (d > 1 and step != 1) or (h > 1 and head != d):
+        raise ValueError("the rows of %s must be contiguous" % name)
+    if n <= 1:
+        row = max(row, h * d)
+    if row < h * d:
+        raise ValueError("the rows of %s overlap" % name)
+    return t.data_ptr(), row
+
+
+def _cache(keys, values):
+    """tt_cache of two tensors [pages, page_size, heads, dim] of the same strides; (packed, device)."""
+    d = _device(keys, "key_cache")
+    kind = _type_of(keys, "key_cache", (1, 2))
+    if keys.dim() != 4 or values.shape != keys.shape or values.dtype != keys.dtype or values.get_device() != d:
+        raise ValueError("key_cache and value_cache must be two tensors of [pages, page_size, heads, dim], not %s %s and %s %s on %s"
+                         % (keys.dtype, tuple(keys.shape), values.dtype, tuple(values.shape), values.device))
+    pages, page_size, heads, dim = keys.shape
+    strides = keys.stride()
+    if values.stride() != strides or (dim > 1 and strides[3] != 1):
+        raise ValueError("key_cache and value_cache must have the same strides, and contiguous vectors")
+    if page_size > 0x7FFFFFFF or heads > 0x7FFFFFFF or dim > 0x7FFFFFFF:
+        raise ValueError("a cache of shape %s is too large" % (tuple(keys.shape),))
+    # no two vectors of a cache share elements: from the narrowest stride up, each is at least what lies below it
+    below = dim
+    for stride, size in sorted(zip(strides[:3], keys.shape[:3])):
+        if size > 1:
+            if stride < below:
+                raise ValueError("vectors of the cache overlap")
+            below = stride * (size - 1) + below
+    stride = [0 if n <= 1 else s for s, n in zip(strides, keys.shape)]  # (one page, slot or head: its stride means nothing)
+    return _CACHE.pack(kind, page_size, heads, dim, pages, stride[0], stride[1], stride[2], keys.data_ptr(), values.data_ptr()), d
+
+
+def cache_append(keys, values, key_cache, value_cache, slots, positions=None, frequencies=None, interleaved=False, queries=None,
+                 rotated=None, stream=None):
+    """``tt_cache_append``: keys and values of a step's tokens into their slots of a paged cache.
+
+    ``keys`` and ``values`` are [tokens, heads, dim] (views of one projection's output are fine),
+    ``key_cache`` and ``value_cache`` [pages, page_size, heads, dim] with any order of their first three
+    dimensions, bfloat16 or float16.  ``slots`` (int64 [tokens]) are those of ``step_plan``; a token whose
+    slot is not in the cache is passed over.  With ``frequencies`` (float32 [pairs]) and ``positions``
+    (int32 [tokens]) the first 2 * pairs elements of each key are rotated on the way, as halves or as
+    ``interleaved`` neighbours, and ``queries`` [tokens, q_heads, dim] into ``rotated`` (may be ``queries``).
+    """
+    cache, d = _cache(key_cache, value_cache)
+    _, _, heads, dim = key_cache.shape
+    n, dtype = keys.shape[0], key_cache.dtype
+    k, k_stride = _heads(keys, "keys", d, dtype, n, heads, dim)
+    v, v_stride = _heads(values, "values", d, dtype, n, heads, dim)
+    if (queries is None) != (rotated is None):
+        raise ValueError("queries and rotated come together")
+    if queries is None:
+        q_heads, q, q_stride, r, r_stride = 0, None, 0, None, 0
+    else:
+        q, q_stride = _heads(queries, "queries", d, dtype, n, None, dim)
+        q_heads = queries.shape[1]
+        r, r_stride = _heads(rotated, "rotated", d, dtype, n, q_heads, dim)
+    pairs = 0
+    if frequencies is not None:
+        if positions is None:
+            raise ValueError("frequencies need positions")
+        if frequencies.dim() != 1:
+            raise ValueError("frequencies must have one dimension")
+        pairs = frequencies.shape[0]
+    _lib.check(_lib.load().tt_cache_append(
+        cache, n, _flat(slots, "slots", _I64, (n,), d), _flat(positions, "positions", _I32, (n,), d),
+        _flat(frequencies, "frequencies", _F32, (pairs,), d), pairs, 1 if interleaved else 0, k, k_stride, v, v_stride,
+        q_heads, q, q_stride, r, r_stride, stream), "tt_cache_append")
+
+
+def cache_attention_workspace(tokens, requests, q_heads, kv_heads, dim) -> int:
+    """``tt_cache_attention_workspace``: bytes of workspace that ``cache_attention`` needs."""
+    return _need("tt_cache_attention_workspace", tokens, requests, q_heads, kv_heads, dim)
+
+
+def cache_attention(queries, key_cache, value_cache, tables, offsets, lengths, out, logsums=None, scale=None, window=0, sinks=0,
+                    workspace=None, stream=None):
+    """``tt_cache_attention``: attention of a step's tokens over the paged cache of ``cache_append``.
+
+    ``queries`` and ``out`` are [tokens, q_heads, dim]; ``tables``, ``offsets`` and ``lengths`` are those of
+    ``step_plan`` (the tables with the step's pages).  A token sees its request's tokens up to itself, with
+    ``window`` the last ``window`` of them and the first ``sinks``.  ``logsums`` (float32 [tokens, q_heads])
+    receives the logarithms of the softmax's sums; ``scale`` is dim ** -0.5 by default.
+    """
+    cache, d = _cache(key_cache, value_cache)
+    _, _, heads, dim = key_cache.shape
+    dtype, n = key_cache.dtype, lengths.shape[0]
+    q, q_stride = _heads(queries, "queries", d, dtype, None, None, dim)
+    tokens, q_heads, _ = queries.shape
+    o, o_stride = _heads(out, "out", d, dtype, tokens, q_heads, dim)
+    table, t_stride = _matrix(tables, "tables", d)
+    if _code(tables.dtype) != _I32 or tables.shape[0] != n:
+        raise ValueError("tables must be an int32 matrix of %d rows, not %s %s" % (n, tables.dtype, tuple(tables.shape)))
+    if not (0 <= window <= 0x7FFFFFFF and 0 <= sinks <= 0x7FFFFFFF):
+        raise ValueError("window %r and sinks %r must be numbers of tokens below 2^31" % (window, sinks))
+    if max(tokens, n, q_heads, tables.shape[1]) > 0x7FFFFFFF:
+        raise ValueError("sizes past 32 bits")
+    if heads < 1 or q_heads < 1 or q_heads % heads:
+        raise ValueError("%d heads of queries are not a multiple of %d of keys" % (q_heads, heads))
+    flat = _flat
+    step = _ATTENTION.pack(
+        n, tables.shape[1], t_stride, tokens, q_heads, window, sinks, dim ** -0.5 if scale is None else scale, q_stride,
+        o_stride, table, flat(offsets, "offsets", _I32, (n + 1,), d), flat(lengths, "lengths", _I32, (n,), d), q, o,
+        flat(logsums, "logsums", _F32, (tokens, q_heads), d))
+    room, size = _room(workspace, _need("tt_cache_attention_workspace", tokens, n, q_heads, heads, dim), d)
+    _lib.check(_lib.load().tt_cache_attention(cache, step, room, size, stream), "tt_cache_attention")
+
+
+def _adjustment(logits, device, history, history_offsets, repetition, presence, frequency, bias_ids, bias_values, bias_offsets,
+                masks, mask_rows):
+    """tt_adjustment of these tensors."""
+    p, stride = _matrix(logits, "logits", device)
+    kind = _type_of(logits, "logits", (0, 1, 2))
+    rows, vocab = logits.shape
+    if (history is None) != (history_offsets is None) or (masks is None) != (mask_rows is None):
+        raise ValueError("history and history_offsets, masks and mask_rows come together")
+    if not (bias_ids is None) == (bias_values is None) == (bias_offsets is None):
+        raise ValueError("bias_ids, bias_values and bias_offsets come together")
+    if history is None and not (repetition is None and presence is None and frequency is None):
+        raise ValueError("penalties need a history")
+    n_history = n_biases = n_masks = mask = mask_stride = 0
+    if history is not None:
+        n_history = history.shape[0]
+    if bias_ids is not None:
+        n_biases = bias_ids.shape[0]
+    if masks is not None:
+        mask, mask_stride = _matrix(masks, "masks", device)
+        n_masks, words = masks.shape
+        if _code(masks.dtype) != _I32 or words < (vocab + 31) // 32 or n_masks > 0x7FFFFFFF:
+            raise ValueError("masks must be an int32 matrix of at least %d words a row, not %s %s"
+                             % ((vocab + 31) // 32, masks.dtype, tuple(masks.shape)))
+    one, ends = (rows,), (rows + 1,)
+    return _ADJUSTMENT.pack(
+        kind, n_masks, rows, vocab, stride, n_history, n_biases, mask_stride, p,
+        _flat(history, "history", _I32, (n_history,), device), _flat(history_offsets, "history_offsets", _I64, ends, device),
+        _flat(repetition, "repetition", _F32, one, device), _flat(presence, "presence", _F32, one, device),
+        _flat(frequency, "frequency", _F32, one, device), _flat(bias_ids, "bias_ids", _I32, (n_biases,), device),
+        _flat(bias_values, "bias_values", _F32, (n_biases,), device), _flat(bias_offsets, "bias_offsets", _I64, ends, device),
+        mask, _flat(mask_rows, "mask_rows", _I32, one, device))
+
+
+def adjust_logits(logits, out, history=None, history_offsets=None, repetition=None, presence=None, frequency=None, bias_ids=None,
+                  bias_values=None, bias_offsets=None, masks=None, mask_rows=None, stream=None):
+    """``tt_adjust_logits``: penalties for repeated tokens, biases and masks on logits [rows, vocab].
+
+    ``history`` (int32) holds the rows' tokens one row after the other, row r's between
+    ``history_offsets[r]`` and ``[r + 1]`` (int64 [rows + 1]); ``repetition``, ``presence`` and
+    ``frequency`` are float32 [rows].  ``bias_ids`` (int32) and ``bias_values`` (float32) are lists of the
+    same kind with ``bias_offsets``.  ``masks`` (int32 [masks, words]) holds a bit a token, 1 where it is
+    allowed, and ``mask_rows`` (int32 [rows]) each row's mask, negative for none.  ``out`` has the type
+    and shape of the logits, and may be the logits.
+    """
+    d = _device(logits, "logits")
+    a = _adjustment(logits, d, history, history_offsets, repetition, presence, frequency, bias_ids, bias_values, bias_offsets,
+                    masks, mask_rows)
+    _lib.check(_lib.load().tt_adjust_logits(a, *_matrix(out, "out", d, logits.dtype, logits.shape), stream), "tt_adjust_logits")
+
+
+def adjust_logits_grad(logits, grad_out, grad_logits, history=None, history_offsets=None, repetition=None, masks=None,
+                       mask_rows=None, stream=None):
+    """``tt_adjust_logits_grad``: gradient with respect to the logits, into ``grad_logits`` (may be
+    ``grad_out``), from that with respect to the adjusted logits; the other arguments are the call's."""
+    d = _device(logits, "logits")
+    a = _adjustment(logits, d, history, history_offsets, repetition, None, None, None, None, None, masks, mask_rows)
+    _lib.check(_lib.load().tt_adjust_logits_grad(
+        a, *_matrix(grad_out, "grad_out", d, logits.dtype, logits.shape),
+        *_matrix(grad_logits, "grad_logits", d, logits.dtype, logits.shape), stream), "tt_adjust_logits_grad")
 
 
 def token_scores_workspace(rows, vocab, n_alt=0) -> int:
