@@ -143,6 +143,8 @@ int tt_cache_append(const tt_cache* cache, int64_t tokens, const int64_t* slots,
  * that sees a token whose page is not one of the cache's, or is behind the
  * table's entries, gets NaN.  What a token does not see does not matter, be it
  * NaN or infinite.  Rows behind offsets[n_requests] stay as they are.
+ * How the sums of a step are shared out, and with it their rounding, depends on
+ * the offsets and lengths of the whole step.
  * Products and sums are held in 32 bits; exp(x_j - max), at most 1 up to a factor
  * of 2^8, is rounded to the type before it is multiplied by the values, and the
  * result is rounded once. */

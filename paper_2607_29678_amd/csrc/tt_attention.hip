@@ -1,88 +1,684 @@
 // tt_cache_attention: attention of a step's tokens over a paged cache, with an
 // optional sliding window and first tokens that stay visible.
+//
+// Work is cut into items: a tile of a request's tokens with the query heads that
+// share a key head (their products share the loads of keys and values), and every
+// item into units, tiles of keys that some of its tokens see.  All units of a step
+// stand in one line, and workers take equal parts of it: a step of long and short
+// requests, of single tokens and prompts, is even by construction, and a
+// graph's launches need no lengths on the host.  Every block finds its part by
+// summing the items' units for itself.  Where an item's units fall to several
+// workers, each leaves its sums in the workspace, and a second launch joins them.
+//
+// Products are of transposed tiles: S^T = K Q^T puts a query's scores into the
+// lanes of one column, so that the running maximum and sum are a lane's own and the
+// exponentials are, as they stand, the operand of O^T = V^T P^T.  Values are
+// transposed by the loads from LDS.
 #include "tt_cache.h"
 
 namespace tt {
 namespace {
 
+// n / d for 0 <= n < 2^31, as a product: with 2^s <= d < 2^(s + 1) and
+// m = floor(2^(32 + s) / d) + 1, m d exceeds 2^(32 + s) by at most d, and n times
+// that stays below 2^(32 + s).
+struct Quotient {
+  uint32_t d, m;
+  int s;
+  explicit Quotient(uint32_t by = 1) : d(by), m(0), s(0) {
+    while ((by >> s) > 1) s++;
+    if (by & (by - 1)) m = (uint32_t)(((uint64_t)1 << (32 + s)) / by) + 1;
+  }
+  __device__ __forceinline__ int of(int n) const { return (int)((m ? __umulhi((uint32_t)n, m) : (uint32_t)n) >> s); }
+};
+
+constexpr int ATT_THREADS = 256;
+constexpr int ATT_WAVES = 4;
+constexpr int STAGED = 1024;  // requests whose offsets and lengths are held in LDS for the search
+constexpr int EACH = 4;       // items counted by a thread at a time
+
+// What the small kernel (16 rows a wave, 32 keys a unit) and the large one (128 rows
+// a block, 64 keys a unit) make of a step.
+struct Plan {
+  int rows;        // of an item
+  int keys;        // of a unit
+  int workers;
+  int heads;       // query heads of an item
+  int tokens;      // of an item
+  int groups;      // items that the query heads of a key head take
+  int least;       // fewest units of a worker
+};
+
 struct AttentionArgs {
   tt_cache c;
   tt_attention s;
-  int64_t capacity;  // tokens that a request's table has room for
+  int capacity;  // tokens that a request's table has room for (at most 2^31 - 65)
+  Plan p;
+  Quotient by_page, by_tokens;
+  int per_kv;      // query heads of a key head
+  bool vectors;    // queries and out are aligned to 16 bytes
+  uint8_t* parts;  // workspace
 };
 
-// A wave for each token and head: 64 keys at a time, one a lane, a running
-// maximum and sum, then the values with a lane's dims.
-template <class T>
-__global__ __launch_bounds__(64) void attention_kernel(AttentionArgs a) {
-  __shared__ float query[TT_MAX_HEAD_DIM];
+// What a worker leaves for the join.
+struct Leaf {
+  int32_t first;  // its first piece goes on an item that began before: 0 no, 1 and the item goes on, 2 and the item ends
+  int32_t last;   // its last piece begins an item that goes on behind it
+  int32_t row0, tokens, head;  // that item's first row of queries, its tokens and its head unit
+  int32_t pad[3];
+};
+
+__host__ __device__ inline int64_t piece_floats(int rows, int dim) { return (int64_t)rows * (dim + 2); }
+__host__ __device__ inline int64_t leaves_bytes(int workers) { return ((int64_t)workers * (int64_t)sizeof(Leaf) + 255) & ~255; }
+__device__ __forceinline__ float* piece_of(const AttentionArgs& a, int worker, int which) {
+  return reinterpret_cast<float*>(a.parts + leaves_bytes(a.p.workers)) + (2 * (int64_t)worker + which) * piece_floats(a.p.rows, a.c.dim);
+}
+
+// One request's place in the step, and an item of it.
+struct Item {
+  int row0, tokens;        // rows of queries
+  int low;                 // position of the first token
+  int front, begin, last;  // some token sees key j if j <= last and (j < front or j >= begin)
+  int front_units, begin_unit, units;
+};
+
+__device__ __forceinline__ int clamped(int64_t x, int64_t least, int64_t most) { return (int)(x < least ? least : x > most ? most : x); }
+__device__ __forceinline__ int offset_of(const tt_attention& s, int r) { return clamped(s.offsets[r], 0, s.tokens); }
+
+// Slot `slot` of the step's items: request r's begin at slot offsets[r] / tokens + r,
+// which leaves each one room enough.  (Slots without tokens have no units.)
+__device__ __forceinline__ Item item_of(const AttentionArgs& a, int slot, int r, int off0, int off1, int raw1, int length) {
+  Item t;
+  const int64_t at = (int64_t)slot - (a.by_tokens.of(off0) + (int64_t)r);
+  const int64_t row0 = off0 + at * a.p.tokens;
+  t.row0 = (int)row0;
+  t.tokens = 0;
+  t.units = 0;
+  if (at < 0 || row0 >= off1) return t;
+  t.tokens = off1 - row0 < a.p.tokens ? (int)(off1 - row0) : a.p.tokens;
+  const int64_t low = (int64_t)length - raw1 + row0, high = low + t.tokens - 1;
+  t.low = clamped(low, INT32_MIN / 2, INT32_MAX);
+  t.last = clamped(high, -1, a.capacity);
+  t.begin = a.s.window ? clamped(low - a.s.window + 1, 0, a.capacity) : 0;
+  t.front = a.s.sinks < t.begin ? a.s.sinks : t.begin;
+  const int keys = a.p.keys;
+  t.front_units = (t.front + keys - 1) / keys;
+  t.begin_unit = t.begin / keys;
+  if (t.begin_unit < t.front_units) t.begin_unit = t.front_units;
+  t.units = t.last < 0 ? 1 : t.front_units + t.last / keys - t.begin_unit + 1;
+  if (t.units < t.front_units) t.units = t.front_units;
+  if (t.units < 1) t.units = 1;
+  return t;
+}
+
+struct Search {
+  int32_t offsets[STAGED + 1], lengths[STAGED];
+  int64_t sums[ATT_WAVES];
+};
+// Where a worker begins
+struct Start {
+  int slot, request, head, unit;
+  int64_t count;  // units
+};
+
+// Finds the parts of the block's COUNT workers (first, first + 1, ...).
+template <int COUNT>
+__device__ __forceinline__ void find_starts(const AttentionArgs& a, int first, Search& sh, Start* starts) {
   const tt_attention& s = a.s;
-  const int lane = threadIdx.x, dim = a.c.dim;
-  const int64_t t = blockIdx.x / (uint32_t)s.q_heads;
-  const int h = (int)(blockIdx.x % (uint32_t)s.q_heads), kv = h / (s.q_heads / a.c.kv_heads);
-  // the last request whose first token is at or before t
-  int lo = 0, hi = s.n_requests;
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (s.offsets[mid + 1] > t) hi = mid;
-    else lo = mid + 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = s.n_requests;
+  const bool staged = n <= STAGED;
+  if (staged) {
+    for (int i = tid; i <= n; i += ATT_THREADS) sh.offsets[i] = s.offsets[i];
+    for (int i = tid; i < n; i += ATT_THREADS) sh.lengths[i] = s.lengths[i];
   }
-  if (lo >= s.n_requests || s.offsets[lo] > t) return;
-  const int64_t p = (int64_t)s.lengths[lo] - s.offsets[lo + 1] + t;
-  const int64_t last = p < a.capacity ? p : a.capacity;
-  int64_t begin = s.window ? p - s.window + 1 : 0;
-  begin = begin < 0 ? 0 : begin > a.capacity ? a.capacity : begin;
-  const T* q = static_cast<const T*>(s.queries) + t * s.query_stride + h * dim;
-  for (int d = lane; d < dim; d += 64) query[d] = (float)q[d];
+  if (tid < COUNT) starts[tid] = {0, 0, 0, 0, 0};
   __syncthreads();
-  float m = NEG_INF, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const float c = s.scale * LOG2E;
-  const int32_t* table = s.tables + lo * s.table_stride;
-  auto run = [&](int64_t j0, int64_t end) {
-    for (; j0 < end; j0 += 64) {
-      const int64_t j = j0 + lane;
-      const T* value = nullptr;
-      float x = NEG_INF;
-      if (j < end) {
-        const int64_t entry = j / a.c.page_size;
-        const int32_t page = entry < s.table_width ? table[entry] : -1;
-        if (page < 0 || page >= a.c.pages) {
-          x = __builtin_nanf("");
-        } else {
-          const int64_t at = page * a.c.page_stride + (j - entry * a.c.page_size) * a.c.slot_stride + kv * a.c.head_stride;
-          const T* key = static_cast<const T*>(a.c.keys) + at;
-          value = static_cast<const T*>(a.c.values) + at;
-          x = 0.f;
-          for (int d = 0; d < dim; d++) x = fmaf(query[d], (float)key[d], x);
-        }
-      }
-      float top = larger(m, x);
-      for (int d = 32; d; d >>= 1) top = larger(top, __shfl_xor(top, d));
-      const float base = top == NEG_INF ? 0.f : top;
-      const float f = __builtin_amdgcn_exp2f((m - base) * c);
-      const float e = __builtin_amdgcn_exp2f((x - base) * c);
-      float all = e;
-      for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
-      sum = fmaf(sum, f, all);
-      m = top;
-      for (int i = 0; i < 4; i++) acc[i] *= f;
-      const int n = (int)(end - j0 < 64 ? end - j0 : 64);
-      for (int k = 0; k < n; k++) {
-        const float pk = __shfl(e, k);
-        const T* v = reinterpret_cast<const T*>(__shfl((unsigned long long)value, k));
-        for (int i = 0; i < 4; i++)
-          if (v && lane + 64 * i < dim) acc[i] = fmaf(pk, (float)v[lane + 64 * i], acc[i]);
+  auto raw = [&](int r) { return staged ? sh.offsets[r] : s.offsets[r]; };
+  auto offset = [&](int r) { return clamped(raw(r), 0, s.tokens); };
+  const int64_t slots = (int64_t)a.by_tokens.of(offset(n)) + n;
+  // units of EACH slots from slot0 on; the request of the first one
+  auto count = [&](int64_t slot0, int64_t* units, int* requests) {
+    int lo = 0, hi = n;  // requests [0, lo) begin at or before slot0
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if ((int64_t)a.by_tokens.of(offset(mid)) + mid <= slot0) lo = mid + 1;
+      else hi = mid;
+    }
+    int r = lo > 0 ? lo - 1 : 0;
+    int64_t sum = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+      const int64_t slot = slot0 + e;
+      while (r + 1 < n && (int64_t)a.by_tokens.of(offset(r + 1)) + r + 1 <= slot) r++;
+      units[e] = slot < slots ? item_of(a, (int)slot, r, offset(r), offset(r + 1), raw(r + 1), staged ? sh.lengths[r] : s.lengths[r]).units : 0;
+      requests[e] = r;
+      sum += units[e];
+    }
+    return sum;
+  };
+  // sums of the threads before this one, and of all
+  auto scan = [&](int64_t mine, int64_t& before) {
+    int64_t x = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) sh.sums[wave] = x;
+    __syncthreads();
+    before = x - mine;
+    int64_t all = 0;
+#pragma unroll
+    for (int w = 0; w < ATT_WAVES; w++) {
+      if (w < wave) before += sh.sums[w];
+      all += sh.sums[w];
+    }
+    return all;
+  };
+  constexpr int64_t AT_ONCE = (int64_t)ATT_THREADS * EACH;
+  int64_t units[EACH], total = 0, before = 0;
+  int requests[EACH];
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += AT_ONCE)
+    total += scan(count(slot0 + tid * EACH, units, requests), before);
+  if (total == 0) return;
+  const int64_t all = total * a.c.kv_heads * a.p.groups;
+  int64_t part = (all + a.p.workers - 1) / a.p.workers;
+  if (part < a.p.least) part = a.p.least;
+  int64_t base = 0;
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += AT_ONCE) {
+    int64_t here = total;
+    if (slots > AT_ONCE) here = scan(count(slot0 + tid * EACH, units, requests), before);
+#pragma unroll
+    for (int w = 0; w < COUNT; w++) {
+      const int64_t from = (first + w) * part;
+      if (from >= all) continue;
+      const int64_t head = from / total;
+      int64_t x = from - head * total - base - before;
+#pragma unroll
+      for (int e = 0; e < EACH; e++) {
+        if (x >= 0 && x < units[e])
+          starts[w] = {(int)(slot0 + tid * EACH + e), requests[e], (int)head, (int)x, from + part < all ? part : all - from};
+        x -= units[e];
       }
     }
-  };
-  const int64_t front = s.sinks < begin ? s.sinks : begin;
-  run(0, front < last + 1 ? front : last + 1);
-  run(begin, last + 1);
-  T* out = static_cast<T*>(s.out) + t * s.out_stride + h * dim;
-  const bool none = m == NEG_INF;
-  for (int i = 0; i < 4; i++)
-    if (lane + 64 * i < dim) out[lane + 64 * i] = (T)(none ? 0.f : acc[i] / sum);
-  if (s.logsums && lane == 0) s.logsums[t * s.q_heads + h] = none ? NEG_INF : fmaf(m, s.scale, logf(sum));
+    base += here;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// A worker's walk through the items
+struct Walk {
+  int slot, request, head, unit, slots;
+  int64_t left;
+  Item item;
+  __device__ __forceinline__ void read(const AttentionArgs& a) {
+    const int raw1 = a.s.offsets[request + 1];
+    item = item_of(a, slot, request, offset_of(a.s, request), offset_of(a.s, request + 1), raw1, a.s.lengths[request]);
+    item.row0 = uniform(item.row0);
+    item.tokens = uniform(item.tokens);
+    item.low = uniform(item.low);
+    item.front = uniform(item.front);
+    item.begin = uniform(item.begin);
+    item.last = uniform(item.last);
+    item.front_units = uniform(item.front_units);
+    item.begin_unit = uniform(item.begin_unit);
+    item.units = uniform(item.units);
+  }
+  __device__ __forceinline__ Walk(const AttentionArgs& a, const Start& st)
+      : slot(uniform(st.slot)), request(uniform(st.request)), head(uniform(st.head)), unit(uniform(st.unit)),
+        slots(a.by_tokens.of(offset_of(a.s, a.s.n_requests)) + a.s.n_requests),
+        left(((int64_t)uniform((int)(st.count >> 32)) << 32) | (uint32_t)uniform((int)st.count)) {
+    if (left > 0) read(a);
+  }
+  // to the next item that has units (there is one: left > 0; offsets that are not
+  // in order may have none, and the walk ends there)
+  __device__ __forceinline__ void next(const AttentionArgs& a) {
+    unit = 0;
+    do {
+      slot++;
+      if (slot >= slots) {
+        slot = 0;
+        request = 0;
+        head++;
+      }
+      while (request + 1 < a.s.n_requests &&
+             (int64_t)a.by_tokens.of(offset_of(a.s, request + 1)) + request + 1 <= slot)
+        request++;
+      request = uniform(request);
+      read(a);
+    } while (item.units == 0 && head < a.c.kv_heads * a.p.groups);
+    if (item.units == 0) left = 0;
+  }
+};
+
+template <class T>
+__device__ __forceinline__ Vec8<T> zero8() {
+  Vec8<T> z;
+#pragma unroll
+  for (int i = 0; i < 8; i++) z[i] = (T)0.f;
+  return z;
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> nan8() {
+  Vec8<T> z;
+#pragma unroll
+  for (int i = 0; i < 8; i++) z[i] = (T)__builtin_nanf("");
+  return z;
+}
+// Elements that are not finite, as bits
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(const Vec8<T>& v) {
+  constexpr uint32_t TOP = std::is_same<T, bf16_t>::value ? 0x7F80u : 0x7C00u;
+  using U8 = __attribute__((ext_vector_type(8))) uint16_t;
+  const U8 u = __builtin_bit_cast(U8, v);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) bits |= ((u[i] & TOP) == TOP ? 1u : 0u) << i;
+  return bits;
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> load8(const T* p, bool vectors) {
+  if (vectors) return *reinterpret_cast<const Vec8<T>*>(p);
+  Vec8<T> z;
+#pragma unroll
+  for (int i = 0; i < 8; i++) z[i] = p[i];
+  return z;
+}
+template <class T>
+__device__ __forceinline__ void store4(T* p, const float* x, float f, bool vectors) {
+  using T4 = T __attribute__((ext_vector_type(4)));
+  T4 z;
+#pragma unroll
+  for (int i = 0; i < 4; i++) z[i] = (T)(x[i] * f);
+  if (vectors) {
+    *reinterpret_cast<T4*>(p) = z;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i++) p[i] = z[i];
+  }
+}
+
+using F4 = float __attribute__((ext_vector_type(4)));
+using F16 = float __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ F4 product16(Vec8<bf16_t> a, Vec8<bf16_t> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ F4 product16(Vec8<f16_t> a, Vec8<f16_t> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ F16 product32(Vec8<bf16_t> a, Vec8<bf16_t> b, F16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ F16 product32(Vec8<f16_t> a, Vec8<f16_t> b, F16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+// Four rows of 16 columns, transposed: of 16 lanes, lane i gives the address of
+// columns 4 (i % 4) to 4 (i % 4) + 3 of row i / 4 and receives column i.
+using S4 = short __attribute__((ext_vector_type(4)));
+template <class T>
+__device__ __forceinline__ S4 transposed(const T* p) {
+  using P = __attribute__((address_space(3))) S4*;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p));
+}
+template <class T>
+__device__ __forceinline__ Vec8<T> both(S4 a, S4 b) {
+  using S8 = short __attribute__((ext_vector_type(8)));
+  return __builtin_bit_cast(Vec8<T>, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Whether every token of the item sees every key of [k0, k0 + keys)
+__device__ __forceinline__ bool all_seen(const AttentionArgs& a, const Item& t, int k0) {
+  const int end = k0 + a.p.keys;
+  const int64_t begin = a.s.window ? (int64_t)t.low + t.tokens - a.s.window : 0;  // of the last token
+  return end <= t.last + 1 && end - 1 <= t.low && (k0 >= begin || end <= a.s.sinks);
+}
+__device__ __forceinline__ bool sees(const AttentionArgs& a, int position, int key) {
+  int64_t begin = a.s.window ? (int64_t)position - a.s.window + 1 : 0;
+  if (begin > a.capacity) begin = a.capacity;
+  return key <= position && key <= a.capacity && (key >= begin || key < a.s.sinks);
+}
+__device__ __forceinline__ bool needed(const Item& t, int key) { return key <= t.last && (key < t.front || key >= t.begin); }
+__device__ __forceinline__ int first_key(const AttentionArgs& a, const Item& t, int unit) {
+  return (unit < t.front_units ? unit : t.begin_unit + unit - t.front_units) * a.p.keys;
+}
+// Page of a key's token: -1 where there is none, -2 where no token of the item sees it
+__device__ __forceinline__ int page_of(const AttentionArgs& a, const Item& t, const int32_t* table, int key) {
+  if (!needed(t, key)) return -2;
+  const int entry = a.by_page.of(key);
+  const int page = entry < a.s.table_width ? table[entry] : -1;
+  return page >= 0 && page < a.c.pages ? page : -1;
+}
+__device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, int page, int key, int64_t head) {
+  const int entry = a.by_page.of(key);
+  return page * a.c.page_stride + (key - entry * (int)a.by_page.d) * a.c.slot_stride + head;
+}
+
+// A running maximum goes up only where it has to by more than this (in powers of two)
+constexpr float SLACK = 8.f;
+
+// ---- 16 rows a wave: single tokens -----------------------------------------------
+
+// A wave takes its units by itself: 32 keys and values go from memory to registers,
+// the keys straight into the product, the values through LDS that is the wave's own.
+// The next unit's are under way during the exponentials and the second product.
+template <class T, int KK>  // KK: 32 elements of a head
+__global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(AttentionArgs a) {
+  constexpr int DT = 2 * KK, PITCH = KK * 32 + 16;  // (rows 32 bytes apart in the banks)
+  __shared__ union {
+    Search search;
+    T values[ATT_WAVES][32][PITCH];
+  } sh;
+  __shared__ Start starts[ATT_WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
+  const int dim = a.c.dim;
+  const int worker = blockIdx.x * ATT_WAVES + wave;
+  find_starts<ATT_WAVES>(a, blockIdx.x * ATT_WAVES, sh.search, starts);
+  __syncthreads();
+  Walk w(a, starts[wave]);
+  __syncthreads();  // (the search's LDS is the values' from here on)
+  T(*values)[PITCH] = sh.values[wave];
+  Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
+  const float c = a.s.scale * LOG2E;
+  bool chunk[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; kk++) chunk[kk] = kk * 32 + quad * 8 < dim;
+
+  while (w.left > 0) {
+    const Item& t = w.item;
+    const int take = (int64_t)(t.units - w.unit) < w.left ? t.units - w.unit : (int)w.left;
+    const int kv = w.head / a.p.groups, h0 = (w.head - kv * a.p.groups) * a.p.heads;
+    const int heads = a.per_kv - h0 < a.p.heads ? a.per_kv - h0 : a.p.heads;
+    const int rows = t.tokens * a.p.heads;  // (rows of heads past the last one are not used)
+    const int my_token = col / a.p.heads, my_head = col - my_token * a.p.heads;
+    const bool live = col < rows && my_head < heads;
+    const int position = t.low + my_token;
+    const int64_t q_row = t.row0 + my_token, q_head = (int64_t)kv * a.per_kv + h0 + my_head;
+    Vec8<T> q[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) {
+      q[kk] = zero8<T>();
+      if (live && chunk[kk])
+        q[kk] = load8(static_cast<const T*>(a.s.queries) + q_row * a.s.query_stride + q_head * dim + kk * 32 + quad * 8, a.vectors);
+    }
+    const int32_t* table = a.s.tables + w.request * a.s.table_stride;
+    const int64_t head = (int64_t)kv * a.c.head_stride + quad * 8;
+    const T *K = static_cast<const T*>(a.c.keys), *V = static_cast<const T*>(a.c.values);
+    Vec8<T> k[2][KK], v[2][KK];
+    int pages[2];
+    auto fetch_pages = [&](int unit) {
+      const int k0 = first_key(a, t, unit);
+#pragma unroll
+      for (int i = 0; i < 2; i++) pages[i] = page_of(a, t, table, k0 + 16 * i + col);
+    };
+    auto fetch = [&](int unit) {
+      const int k0 = first_key(a, t, unit);
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const int64_t at = vector_at(a, pages[i], k0 + 16 * i + col, head);
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) {
+          if (pages[i] >= 0 && chunk[kk]) {
+            k[i][kk] = *reinterpret_cast<const Vec8<T>*>(K + at + kk * 32);
+            v[i][kk] = *reinterpret_cast<const Vec8<T>*>(V + at + kk * 32);
+          } else {
+            k[i][kk] = pages[i] == -1 ? nan8<T>() : zero8<T>();
+            v[i][kk] = zero8<T>();
+          }
+        }
+      }
+    };
+    F4 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++) o[d] = F4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_INF, sum = 0.f;
+    const int end = w.unit + take;
+    fetch_pages(w.unit);
+    fetch(w.unit);
+    if (w.unit + 1 < end) fetch_pages(w.unit + 1);
+    for (int unit = w.unit; unit < end; unit++) {
+      const int k0 = first_key(a, t, unit);
+      const bool edge = !all_seen(a, t, k0);
+      // values of keys that only some tokens see must not reach the others through 0 * NaN
+      uint64_t spoiled[2] = {0, 0};
+      if (edge && t.tokens > 1) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          uint32_t any = 0;
+#pragma unroll
+          for (int kk = 0; kk < KK; kk++) {
+            const uint32_t bad = not_finite(v[i][kk]);
+            any |= bad;
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (bad >> e & 1) v[i][kk][e] = (T)0.f;
+          }
+          uint64_t votes = __ballot(any != 0);
+          votes |= votes >> 32;
+          spoiled[i] = (votes | votes >> 16) & 0xFFFF;
+        }
+      }
+      int64_t at_now[2] = {0, 0};
+      if (spoiled[0] | spoiled[1]) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) at_now[i] = page_of(a, t, table, k0 + 16 * i + col);
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) *reinterpret_cast<Vec8<T>*>(&values[16 * i + col][kk * 32 + quad * 8]) = v[i][kk];
+      F4 s[2];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        s[i] = F4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KK; kk++) s[i] = product16(k[i][kk], q[kk], s[i]);
+      }
+      if (unit + 1 < end) {
+        fetch(unit + 1);
+        if (unit + 2 < end) fetch_pages(unit + 2);
+      }
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (!sees(a, position, k0 + 16 * i + quad * 4 + e)) s[i][e] = NEG_INF;
+      }
+      float top = NEG_INF;
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          s[i][e] *= c;
+          top = fmaxf(top, s[i][e]);
+        }
+      if (__ballot(top > m + SLACK)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        top = top > m + SLACK ? top : m;  // (a row's own choice: its result does not depend on its neighbours)
+        const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < DT; d++) o[d] *= f;
+      }
+      const float base = m == NEG_INF ? 0.f : m;
+      Vec8<T> p;
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float x = __builtin_amdgcn_exp2f(s[i][e] - base);
+          sum += x;
+          p[4 * i + e] = (T)x;
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int d = 0; d < DT; d++) {
+        const T* from = &values[quad * 4 + (col >> 2)][d * 16 + (col & 3) * 4];
+        o[d] = product16(both<T>(transposed(from), transposed(from + 16 * PITCH)), p, o[d]);
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (spoiled[0] | spoiled[1]) {
+        for (int j = 0; j < 32; j++) {
+          if (!(spoiled[j >> 4] >> (j & 15) & 1)) continue;
+          const int page = __shfl((int)at_now[j >> 4], j & 15);
+          if (page < 0) continue;
+          const T* value = V + vector_at(a, page, k0 + j, (int64_t)kv * a.c.head_stride);
+          if (!sees(a, position, k0 + j)) continue;
+          for (int d = 0; d < DT; d++)
+            for (int e = 0; e < 4; e++) {
+              const int at = d * 16 + quad * 4 + e;
+              const float x = at < dim ? (float)value[at] : 0.f;
+              if (!(fabsf(x) < __builtin_inff())) {
+#pragma unroll
+                for (int dd = 0; dd < DT; dd++)
+#pragma unroll
+                  for (int ee = 0; ee < 4; ee++)
+                    if (dd == d && ee == e) o[dd][ee] += x;
+              }
+            }
+        }
+      }
+    }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    const bool began = w.unit > 0, ends = end == t.units;
+    if (!began && ends) {
+      const bool none = m == NEG_INF && sum == 0.f;
+      if (live) {
+        const float f = none ? 0.f : 1.f / sum;
+        T* out = static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + quad * 4;
+#pragma unroll
+        for (int d = 0; d < DT; d++) {
+          const float x[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
+          if (d * 16 + quad * 4 < dim) store4(out + d * 16, x, f, a.vectors);
+        }
+        if (a.s.logsums && quad == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
+      }
+    } else {
+      float* piece = piece_of(a, worker, began ? 0 : 1);
+      if (live) {
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+          if (d * 16 + quad * 4 < dim) {
+            float* x = piece + (int64_t)col * dim + d * 16 + quad * 4;
+            *reinterpret_cast<F4*>(x) = o[d];
+          }
+        if (quad == 0) *reinterpret_cast<float2*>(piece + (int64_t)a.p.rows * dim + 2 * col) = float2{m, sum};
+      }
+      if (began) {
+        leaf.first = ends ? 2 : 1;
+      } else {
+        leaf.last = 1;
+        leaf.row0 = t.row0;
+        leaf.tokens = t.tokens;
+        leaf.head = w.head;
+      }
+    }
+    w.left -= take;
+    if (w.left > 0) w.next(a);
+  }
+  if (lane == 0) *(reinterpret_cast<Leaf*>(a.parts) + worker) = leaf;
+}
+
+// ---- joins the pieces of items that several workers have ----------------------------
+
+// A block for a worker whose last piece begins an item, and for some of its rows.
+// SMALL: one row, whose pieces are many: groups of lanes take every n-th piece.
+// Else a group takes a row.
+template <class T, bool SMALL>
+__global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int lanes) {
+  __shared__ F4 sums[ATT_THREADS];
+  __shared__ float2 heads[ATT_THREADS];
+  const int tid = threadIdx.x, worker = blockIdx.x, dim = a.c.dim;
+  const Leaf* leaves = reinterpret_cast<const Leaf*>(a.parts);
+  const Leaf leaf = leaves[worker];
+  if (!leaf.last) return;
+  const int groups = ATT_THREADS / lanes, group = tid / lanes, at = (tid - group * lanes) * 4;
+  const int row = SMALL ? blockIdx.y : blockIdx.y * groups + group;
+  const int kv = leaf.head / a.p.groups, h0 = (leaf.head - kv * a.p.groups) * a.p.heads;
+  const int token = row / a.p.heads, head = row - token * a.p.heads;
+  const bool live = token < leaf.tokens && head < a.per_kv - h0;
+  if (SMALL && !live) return;
+  // the worker whose first piece ends the item
+  int last = worker + 1;
+  for (; last < a.p.workers; last += 64) {
+    const int i = last + (tid & 63);
+    const uint64_t votes = __ballot(i < a.p.workers && leaves[i].first == 2);
+    if (votes) {
+      last += __builtin_ctzll(votes);
+      break;
+    }
+  }
+  if (last >= a.p.workers) last = a.p.workers - 1;
+  const int pieces = last - worker + 1;
+  float m = NEG_INF, sum = 0.f;
+  F4 o = {0.f, 0.f, 0.f, 0.f};
+  const bool mine = live && at < dim;
+  if (mine) {
+    for (int i = SMALL ? group : 0; i < pieces; i += SMALL ? groups : 1) {
+      const float* piece = piece_of(a, worker + i, i ? 0 : 1);
+      const float2 h = *reinterpret_cast<const float2*>(piece + (int64_t)a.p.rows * dim + 2 * row);
+      const F4 x = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
+      const float top = fmaxf(m, h.x);
+      const float f = m == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(m - top), g = h.x == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(h.x - top);
+      // (a piece that is all NaN has no maximum: its sums count as they are)
+      sum = sum * (m == NEG_INF && sum != sum ? 1.f : f) + h.y * (h.x == NEG_INF && h.y != h.y ? 1.f : g);
+      o = o * f + x * (h.x == NEG_INF && h.y != h.y ? 1.f : g);
+      m = top;
+    }
+  }
+  if (SMALL) {
+    sums[tid] = o;
+    heads[tid] = float2{m, sum};
+    __syncthreads();
+    if (group != 0 || !mine) return;
+    float top = m;
+    for (int g = 1; g < groups; g++) top = fmaxf(top, heads[g * lanes + tid].x);
+    o = F4{0.f, 0.f, 0.f, 0.f};
+    sum = 0.f;
+    for (int g = 0; g < groups; g++) {
+      const float2 h = heads[g * lanes + tid];
+      const float f = h.x == NEG_INF ? (h.y != h.y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(h.x - top);
+      sum += h.y * f;
+      o += sums[g * lanes + tid] * f;
+    }
+    m = top;
+  }
+  if (!mine) return;
+  const bool none = m == NEG_INF && sum == 0.f;
+  const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
+  const float x[4] = {o[0], o[1], o[2], o[3]};
+  store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);
+  if (a.s.logsums && at == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
+}
+
+// ---- the calls ----------------------------------------------------------------------
+
+constexpr int SMALL_WORKERS = 2048;
+
+Plan plan_of(int64_t tokens, int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t dim) {
+  const int per_kv = q_heads / kv_heads;
+  Plan p;
+  p.rows = 16;
+  p.keys = 32;
+  p.workers = dim > 128 ? SMALL_WORKERS / 2 : SMALL_WORKERS;
+  p.least = 4;
+  p.heads = per_kv < p.rows ? per_kv : p.rows;
+  p.groups = (per_kv + p.heads - 1) / p.heads;
+  p.tokens = p.rows / p.heads;
+  return p;
+}
+
+int64_t room_of(const Plan& p, int dim) { return leaves_bytes(p.workers) + 2 * (int64_t)p.workers * piece_floats(p.rows, dim) * 4; }
+
+template <class T>
+int run_attention(const AttentionArgs& a, hipStream_t st) {
+  const int kk = (a.c.dim + 31) / 32;
+  auto* kernel = kk <= 2 ? small_kernel<T, 2> : kk == 3 ? small_kernel<T, 3> : kk == 4 ? small_kernel<T, 4> : small_kernel<T, 8>;
+  if (launch(kernel, dim3(a.p.workers / ATT_WAVES), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
+  int lanes = 8;
+  while (lanes * 4 < a.c.dim) lanes *= 2;
+  const int rows = a.p.tokens * a.p.heads;
+  return launch(join_kernel<T, true>, dim3(a.p.workers, rows), dim3(ATT_THREADS), st, a, lanes) == hipSuccess ? TT_OK : TT_ERR_HIP;
 }
 
 }  // namespace
@@ -95,7 +691,7 @@ extern "C" int64_t tt_cache_attention_workspace(int64_t tokens, int32_t n_reques
   if (tokens < 0 || tokens > INT32_MAX || n_requests < 0 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || dim < 8 ||
       dim > TT_MAX_HEAD_DIM || dim % 8)
     return TT_ERR_BAD_ARG;
-  return 0;
+  return tokens == 0 || n_requests == 0 ? 0 : room_of(plan_of(tokens, n_requests, q_heads, kv_heads, dim), dim);
 }
 
 extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* step, void* workspace, int64_t workspace_bytes,
@@ -107,17 +703,26 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
   const int64_t need = tt_cache_attention_workspace(s.tokens, s.n_requests, s.q_heads, cache->kv_heads, cache->dim);
   const int64_t width = (int64_t)s.q_heads * cache->dim;
   if (need < 0 || s.table_width < 0 || s.table_stride < s.table_width || s.window < 0 || s.sinks < 0 || !good_scale(s.scale) ||
-      s.query_stride < width || s.out_stride < width || (s.out && s.out == s.queries) || workspace_bytes < need ||
+      s.query_stride < width || s.out_stride < width || (s.out && s.out == s.queries) || (workspace && workspace_bytes < need) ||
       reinterpret_cast<uintptr_t>(workspace) % 256)
     return TT_ERR_BAD_ARG;
   if (s.tokens == 0 || s.n_requests == 0) return TT_OK;
   if (bad) return bad;
-  if (!s.offsets || !s.lengths || (s.table_width > 0 && !s.tables) || !s.queries || !s.out || (need && !workspace))
-    return TT_ERR_NULL_ARG;
-  if (s.tokens > (int64_t)UINT32_MAX / 64 / s.q_heads) return TT_ERR_TOO_LARGE;
-  AttentionArgs a{*cache, s, (int64_t)s.table_width * cache->page_size};
-  return launch(cache->type == TT_BF16 ? attention_kernel<bf16_t> : attention_kernel<f16_t>,
-                dim3((uint32_t)(s.tokens * s.q_heads)), dim3(64), static_cast<hipStream_t>(stream), a) == hipSuccess
-             ? TT_OK
-             : TT_ERR_HIP;
+  if (!s.offsets || !s.lengths || (s.table_width > 0 && !s.tables) || !s.queries || !s.out || !workspace) return TT_ERR_NULL_ARG;
+  // slots of items are numbered in 32 bits
+  if (s.tokens + s.n_requests > INT32_MAX) return TT_ERR_TOO_LARGE;
+  auto in_vectors = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; };
+  const int64_t capacity = (int64_t)s.table_width * cache->page_size;
+  AttentionArgs a{*cache,
+                  s,
+                  (int)(capacity < INT32_MAX - 64 ? capacity : INT32_MAX - 64),
+                  plan_of(s.tokens, s.n_requests, s.q_heads, cache->kv_heads, cache->dim),
+                  Quotient((uint32_t)cache->page_size),
+                  Quotient(1),
+                  s.q_heads / cache->kv_heads,
+                  in_vectors(s.queries, s.query_stride) && in_vectors(s.out, s.out_stride),
+                  static_cast<uint8_t*>(workspace)};
+  a.by_tokens = Quotient((uint32_t)a.p.tokens);
+  return cache->type == TT_BF16 ? run_attention<bf16_t>(a, static_cast<hipStream_t>(stream))
+                                : run_attention<f16_t>(a, static_cast<hipStream_t>(stream));
 }

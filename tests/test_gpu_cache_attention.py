@@ -198,14 +198,14 @@ def test_pages_that_are_none(gpu):
 def test_lengths_past_the_table(gpu):
     for new in (1, 70):
         s = Step([(100, new), (30, new)], 4, 2, 64, 16, BF)
-        clean = run(s)[0]
-        s.lengths[0] = s.width * 16 + new  # every token's own place is behind the table
-        for length in (s.width * 16 + new, 2**31 - 1):
+        want, _, tol, _ = s.reference()
+        for length in (s.width * 16 + new, 2**31 - 1):  # every token's own place is behind the table
             s.lengths[0] = length
             for window in (0, 8):
                 out = run(s, window)[0]
                 assert bool(torch.isnan(out[:new]).all())
-            assert torch.equal(run(s)[0][new:], clean[new:])
+            # (a step's lengths say how its sums are shared out: the others' rounding changes with them)
+            close(run(s)[0][new:2 * new], want[new:], tol[new:])
 
 
 def test_tokens_before_the_first(gpu):
