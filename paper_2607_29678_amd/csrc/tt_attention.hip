@@ -333,6 +333,17 @@ __device__ __forceinline__ bool sees(const AttentionArgs& a, int position, int k
   if (begin > a.capacity) begin = a.capacity;
   return key <= position && key <= a.capacity && (key >= begin || key < a.s.sinks);
 }
+// Bit j: whether the token at `position` sees key k0 + j (j < keys <= 64)
+__device__ __forceinline__ uint64_t seen_bits(const AttentionArgs& a, int position, int k0, int keys) {
+  auto below = [&](int64_t n) {  // bits [0, n - k0)
+    const int x = clamped(n - k0, 0, keys);
+    return x >= 64 ? ~0ull : (1ull << x) - 1ull;
+  };
+  const int last = position < a.capacity ? position : a.capacity;
+  int64_t begin = a.s.window ? (int64_t)position - a.s.window + 1 : 0;
+  if (begin > a.capacity) begin = a.capacity;
+  return below((int64_t)last + 1) & (~below(begin) | below(a.s.sinks));
+}
 __device__ __forceinline__ bool needed(const Item& t, int key) { return key <= t.last && (key < t.front || key >= t.begin); }
 __device__ __forceinline__ int first_key(const AttentionArgs& a, const Item& t, int unit) {
   return (unit < t.front_units ? unit : t.begin_unit + unit - t.front_units) * a.p.keys;
@@ -352,6 +363,10 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, int page, i
 // A running maximum goes up only where it has to by more than this (in powers of two)
 constexpr float SLACK = 8.f;
 
+// Workers whose parts follow each other run on one XCD (blocks go to the XCDs in
+// turn): the keys of a head that neighbouring items share stay in its L2.
+__device__ __forceinline__ int worker_of(uint32_t block, uint32_t blocks) { return (int)(block % 8 * (blocks / 8) + block / 8); }
+
 // ---- 16 rows a wave: single tokens -----------------------------------------------
 
 // A wave takes its units by itself: 32 keys and values go from memory to registers,
@@ -367,8 +382,8 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
   __shared__ Start starts[ATT_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
   const int dim = a.c.dim;
-  const int worker = blockIdx.x * ATT_WAVES + wave;
-  find_starts<ATT_WAVES>(a, blockIdx.x * ATT_WAVES, sh.search, starts);
+  const int first = worker_of(blockIdx.x, gridDim.x) * ATT_WAVES, worker = first + wave;
+  find_starts<ATT_WAVES>(a, first, sh.search, starts);
   __syncthreads();
   Walk w(a, starts[wave]);
   __syncthreads();  // (the search's LDS is the values' from here on)
@@ -475,11 +490,11 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
         if (unit + 2 < end) fetch_pages(unit + 2);
       }
       if (edge) {
+        const uint32_t seen = (uint32_t)seen_bits(a, position, k0, 32) >> (quad * 4);
 #pragma unroll
         for (int i = 0; i < 2; i++)
 #pragma unroll
-          for (int e = 0; e < 4; e++)
-            if (!sees(a, position, k0 + 16 * i + quad * 4 + e)) s[i][e] = NEG_INF;
+          for (int e = 0; e < 4; e++) s[i][e] = seen & 1u << (16 * i + e) ? s[i][e] : NEG_INF;
       }
       float top = NEG_INF;
 #pragma unroll
@@ -523,17 +538,14 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
           if (page < 0) continue;
           const T* value = V + vector_at(a, page, k0 + j, (int64_t)kv * a.c.head_stride);
           if (!sees(a, position, k0 + j)) continue;
+#pragma unroll
           for (int d = 0; d < DT; d++)
+#pragma unroll
             for (int e = 0; e < 4; e++) {
               const int at = d * 16 + quad * 4 + e;
               const float x = at < dim ? (float)value[at] : 0.f;
-              if (!(fabsf(x) < __builtin_inff())) {
-#pragma unroll
-                for (int dd = 0; dd < DT; dd++)
-#pragma unroll
-                  for (int ee = 0; ee < 4; ee++)
-                    if (dd == d && ee == e) o[dd][ee] += x;
-              }
+              o[d][e] += fabsf(x) < __builtin_inff() ? 0.f : x;
+              if (e == 3) __builtin_amdgcn_sched_barrier(0);  // (few loads at a time: registers are for the products)
             }
         }
       }
@@ -577,6 +589,249 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
     if (w.left > 0) w.next(a);
   }
   if (lane == 0) *(reinterpret_cast<Leaf*>(a.parts) + worker) = leaf;
+}
+
+// ---- 128 rows a block: prompts ---------------------------------------------------
+
+// Four waves of 32 rows share tiles of 64 keys and values in LDS, two of each, so
+// that one barrier a unit is enough: the next unit's come from memory to registers
+// during a unit's products and are written where the last unit's were.
+template <class T, int DP>  // DP: elements of a head, with zeros behind its own
+__global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(AttentionArgs a) {
+  constexpr int KEYS = 64, KK = DP / 16, DT = DP / 32;
+  constexpr int K_PITCH = DP + 8;                                  // (16 rows 16 bytes apart in the banks)
+  constexpr int V_PITCH = DP == 96 ? DP : DP + 32;                 // (4 rows 64 bytes apart)
+  constexpr int PER_ROW = DP == 64 ? 8 : DP == 256 ? 32 : 16;      // threads that fetch a row
+  constexpr int PASS = ATT_THREADS / PER_ROW, PASSES = KEYS / PASS;
+  struct Tiles {
+    T keys[2][KEYS][K_PITCH];
+    T values[2][KEYS][V_PITCH];
+  };
+  __shared__ __align__(16) union {
+    Search search;
+    Tiles tiles;
+  } sh;
+  __shared__ Start starts[1];
+  __shared__ unsigned long long spoiled[3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
+  const int dim = a.c.dim, worker = worker_of(blockIdx.x, gridDim.x);
+  find_starts<1>(a, worker, sh.search, starts);
+  if (tid < 3) spoiled[tid] = 0;
+  __syncthreads();
+  Walk w(a, starts[0]);
+  __syncthreads();  // (the search's LDS is the tiles' from here on)
+  Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
+  const float c = a.s.scale * LOG2E;
+  const int chunk = tid % PER_ROW, row_in = tid / PER_ROW;
+  const bool loads = chunk * 8 < dim, stores = chunk * 8 < DP;
+  const T *K = static_cast<const T*>(a.c.keys), *V = static_cast<const T*>(a.c.values);
+  int turn = 0, third = 0;  // tiles, and word of spoiled keys, of the present unit
+
+  while (w.left > 0) {
+    const Item& t = w.item;
+    const int take = (int64_t)(t.units - w.unit) < w.left ? t.units - w.unit : (int)w.left;
+    const int kv = w.head / a.p.groups, h0 = (w.head - kv * a.p.groups) * a.p.heads;
+    const int heads = a.per_kv - h0 < a.p.heads ? a.per_kv - h0 : a.p.heads;
+    const int row = wave * 32 + col, rows = t.tokens * a.p.heads;
+    const int my_token = row / a.p.heads, my_head = row - my_token * a.p.heads;
+    const bool live = row < rows && my_head < heads;
+    const int position = t.low + my_token;
+    const int64_t q_row = t.row0 + my_token, q_head = (int64_t)kv * a.per_kv + h0 + my_head;
+    // the wave's tokens
+    const int wave_rows = rows - wave * 32 < 32 ? rows - wave * 32 : 32;
+    const int low = t.low + uniform(wave * 32 / a.p.heads), high = t.low + uniform((wave * 32 + wave_rows - 1) / a.p.heads);
+    Vec8<T> q[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; kk++) {
+      q[kk] = zero8<T>();
+      if (live && kk * 16 + half * 8 < dim)
+        q[kk] = load8(static_cast<const T*>(a.s.queries) + q_row * a.s.query_stride + q_head * dim + kk * 16 + half * 8, a.vectors);
+    }
+    const int32_t* table = a.s.tables + w.request * a.s.table_stride;
+    const int64_t head = (int64_t)kv * a.c.head_stride + chunk * 8;
+    Vec8<T> k[PASSES], v[PASSES];
+    int pages[PASSES];
+    auto fetch_pages = [&](int unit) {
+      const int k0 = first_key(a, t, unit);
+#pragma unroll
+      for (int i = 0; i < PASSES; i++) pages[i] = page_of(a, t, table, k0 + PASS * i + row_in);
+    };
+    auto fetch = [&](int unit) {
+      const int k0 = first_key(a, t, unit);
+#pragma unroll
+      for (int i = 0; i < PASSES; i++) {
+        const int64_t at = vector_at(a, pages[i], k0 + PASS * i + row_in, head);
+        if (pages[i] >= 0 && loads) {
+          k[i] = *reinterpret_cast<const Vec8<T>*>(K + at);
+          v[i] = *reinterpret_cast<const Vec8<T>*>(V + at);
+        } else {
+          k[i] = pages[i] == -1 && loads ? nan8<T>() : zero8<T>();
+          v[i] = zero8<T>();
+        }
+      }
+    };
+    // registers to the tiles of `to`; values of keys that only some tokens see must
+    // not reach the others through 0 * NaN
+    auto put = [&](int unit, int to, int word) {
+      if (t.tokens > 1 && !all_seen(a, t, first_key(a, t, unit))) {
+#pragma unroll
+        for (int i = 0; i < PASSES; i++) {
+          const uint32_t bad = not_finite(v[i]);
+          if (bad) {
+            atomicOr(&spoiled[word], 1ull << (PASS * i + row_in));
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (bad >> e & 1) v[i][e] = (T)0.f;
+          }
+        }
+      }
+      if (stores) {
+#pragma unroll
+        for (int i = 0; i < PASSES; i++) {
+          *reinterpret_cast<Vec8<T>*>(&sh.tiles.keys[to][PASS * i + row_in][chunk * 8]) = k[i];
+          *reinterpret_cast<Vec8<T>*>(&sh.tiles.values[to][PASS * i + row_in][chunk * 8]) = v[i];
+        }
+      }
+    };
+    F16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) o[d][e] = 0.f;
+    float m = NEG_INF, sum = 0.f;
+    const int end = w.unit + take;
+    fetch_pages(w.unit);
+    fetch(w.unit);
+    if (w.unit + 1 < end) fetch_pages(w.unit + 1);
+    put(w.unit, turn, third);
+    for (int unit = w.unit; unit < end; unit++) {
+      const int after = third == 2 ? 0 : third + 1;
+      __syncthreads();
+      if (tid == 0) spoiled[after == 2 ? 0 : after + 1] = 0;  // (read in the last unit, written in the next one)
+      if (unit + 1 < end) {
+        fetch(unit + 1);
+        if (unit + 2 < end) fetch_pages(unit + 2);
+      }
+      const int k0 = first_key(a, t, unit);
+      const int64_t begin_low = a.s.window ? (int64_t)low - a.s.window + 1 : 0, begin_high = a.s.window ? (int64_t)high - a.s.window + 1 : 0;
+      const bool any = wave_rows > 0 && k0 <= high && (k0 + KEYS > begin_low || k0 < a.s.sinks || begin_low > a.capacity);
+      if (any) {
+        const T(*keys)[K_PITCH] = sh.tiles.keys[turn];
+        const T(*values)[V_PITCH] = sh.tiles.values[turn];
+        F16 s[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+#pragma unroll
+          for (int e = 0; e < 16; e++) s[i][e] = 0.f;
+#pragma unroll
+          for (int kk = 0; kk < KK; kk++)
+            s[i] = product32(*reinterpret_cast<const Vec8<T>*>(&keys[32 * i + col][kk * 16 + half * 8]), q[kk], s[i]);
+        }
+        const bool whole = k0 + KEYS <= t.last + 1 && k0 + KEYS - 1 <= low && (k0 >= begin_high || k0 + KEYS <= a.s.sinks);
+        if (!whole) {
+          const uint64_t seen = seen_bits(a, position, k0, KEYS) >> (4 * half);
+#pragma unroll
+          for (int i = 0; i < 2; i++) {
+            const uint32_t word = (uint32_t)(seen >> (32 * i));
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[i][e] = word & 1u << (8 * (e / 4) + e % 4) ? s[i][e] : NEG_INF;
+          }
+        }
+        float top = NEG_INF;
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+#pragma unroll
+          for (int e = 0; e < 16; e++) top = fmaxf(top, s[i][e]);
+        top *= c;
+        if (__ballot(top > m + SLACK)) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          top = top > m + SLACK ? top : m;  // (a row's own choice: its result does not depend on its neighbours)
+          const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
+          m = top;
+          sum *= f;
+#pragma unroll
+          for (int d = 0; d < DT; d++) o[d] *= f;
+        }
+        const float base = m == NEG_INF ? 0.f : m;
+        Vec8<T> p[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], c, -base));
+            sum += x;
+            p[i][e] = (T)x;
+          }
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            const T* from = &values[16 * i + 4 * half + ((lane & 15) >> 2)][d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4];
+            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * V_PITCH)), p[i], o[d]);
+          }
+        uint64_t bad = spoiled[third];
+        bad = ((uint64_t)uniform((int)(bad >> 32)) << 32) | (uint32_t)uniform((int)bad);
+        for (; bad; bad &= bad - 1) {
+          const int key = k0 + __builtin_ctzll(bad);
+          const int page = page_of(a, t, table, key);
+          if (page < 0 || !sees(a, position, key)) continue;
+          const T* value = V + vector_at(a, page, key, (int64_t)kv * a.c.head_stride) + 4 * half;
+#pragma unroll
+          for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+              const int at = d * 32 + 8 * (e / 4) + e % 4;
+              const float x = at + 4 * half < dim ? (float)value[at] : 0.f;
+              o[d][e] += fabsf(x) < __builtin_inff() ? 0.f : x;
+              if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (few loads at a time: registers are for the products)
+            }
+        }
+      }
+      if (unit + 1 < end) put(unit + 1, turn ^ 1, after);
+      turn ^= 1;
+      third = after;
+    }
+    sum += __shfl_xor(sum, 32);
+    const bool began = w.unit > 0, ends = end == t.units;
+    if (!began && ends) {
+      const bool none = m == NEG_INF && sum == 0.f;
+      if (live) {
+        const float f = none ? 0.f : 1.f / sum;
+        T* out = static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + half * 4;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float x[4] = {o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+            if (d * 32 + 2 * e + half * 4 < dim) store4(out + d * 32 + 2 * e, x, f, a.vectors);
+          }
+        if (a.s.logsums && half == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
+      }
+    } else {
+      float* piece = piece_of(a, worker, began ? 0 : 1);
+      if (live) {
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const int at = d * 32 + 2 * e + half * 4;
+            if (at < dim) *reinterpret_cast<F4*>(piece + (int64_t)row * dim + at) = F4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+          }
+        if (half == 0) *reinterpret_cast<float2*>(piece + (int64_t)a.p.rows * dim + 2 * row) = float2{m, sum};
+      }
+      if (began) {
+        leaf.first = ends ? 2 : 1;
+      } else {
+        leaf.last = 1;
+        leaf.row0 = t.row0;
+        leaf.tokens = t.tokens;
+        leaf.head = w.head;
+      }
+    }
+    w.left -= take;
+    if (w.left > 0) w.next(a);
+  }
+  if (tid == 0) *(reinterpret_cast<Leaf*>(a.parts) + worker) = leaf;
 }
 
 // ---- joins the pieces of items that several workers have ----------------------------
@@ -653,14 +908,15 @@ __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int 
 
 // ---- the calls ----------------------------------------------------------------------
 
-constexpr int SMALL_WORKERS = 2048;
+constexpr int SMALL_WORKERS = 2048, LARGE_WORKERS = 512;
 
 Plan plan_of(int64_t tokens, int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   const int per_kv = q_heads / kv_heads;
   Plan p;
-  p.rows = 16;
-  p.keys = 32;
-  p.workers = dim > 128 ? SMALL_WORKERS / 2 : SMALL_WORKERS;
+  const bool small = tokens * per_kv <= 16 * (int64_t)n_requests;
+  p.rows = small ? 16 : 128;
+  p.keys = small ? 32 : 64;
+  p.workers = (small ? SMALL_WORKERS : LARGE_WORKERS) / (dim > 128 ? 2 : 1);
   p.least = 4;
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
@@ -672,13 +928,22 @@ int64_t room_of(const Plan& p, int dim) { return leaves_bytes(p.workers) + 2 * (
 
 template <class T>
 int run_attention(const AttentionArgs& a, hipStream_t st) {
-  const int kk = (a.c.dim + 31) / 32;
-  auto* kernel = kk <= 2 ? small_kernel<T, 2> : kk == 3 ? small_kernel<T, 3> : kk == 4 ? small_kernel<T, 4> : small_kernel<T, 8>;
-  if (launch(kernel, dim3(a.p.workers / ATT_WAVES), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
-  int lanes = 8;
+  const int kk = (a.c.dim + 31) / 32, rows = a.p.tokens * a.p.heads;
+  int lanes = 8;  // of a row in the join
   while (lanes * 4 < a.c.dim) lanes *= 2;
-  const int rows = a.p.tokens * a.p.heads;
-  return launch(join_kernel<T, true>, dim3(a.p.workers, rows), dim3(ATT_THREADS), st, a, lanes) == hipSuccess ? TT_OK : TT_ERR_HIP;
+  const bool small = a.p.rows == 16;
+  if (small) {
+    auto* kernel = kk <= 2 ? small_kernel<T, 2> : kk == 3 ? small_kernel<T, 3> : kk == 4 ? small_kernel<T, 4> : small_kernel<T, 8>;
+    if (launch(kernel, dim3(a.p.workers / ATT_WAVES), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
+  } else {
+    auto* kernel = kk <= 2 ? large_kernel<T, 64> : kk == 3 ? large_kernel<T, 96> : kk == 4 ? large_kernel<T, 128> : large_kernel<T, 256>;
+    if (launch(kernel, dim3(a.p.workers), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
+  }
+  const int each = small ? 1 : ATT_THREADS / lanes;  // rows of a block
+  return launch(small ? join_kernel<T, true> : join_kernel<T, false>, dim3(a.p.workers, (rows + each - 1) / each), dim3(ATT_THREADS), st,
+                a, lanes) == hipSuccess
+             ? TT_OK
+             : TT_ERR_HIP;
 }
 
 }  // namespace
