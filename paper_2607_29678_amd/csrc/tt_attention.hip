@@ -382,7 +382,7 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
   __shared__ Start starts[ATT_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
   const int dim = a.c.dim;
-  const int first = worker_of(blockIdx.x, gridDim.x) * ATT_WAVES, worker = first + wave;
+  const int first = blockIdx.x * ATT_WAVES, worker = first + wave;
   find_starts<ATT_WAVES>(a, first, sh.search, starts);
   __syncthreads();
   Walk w(a, starts[wave]);
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
   __shared__ Start starts[1];
   __shared__ unsigned long long spoiled[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int dim = a.c.dim, worker = worker_of(blockIdx.x, gridDim.x);
+  const int dim = a.c.dim, worker = blockIdx.x;
   find_starts<1>(a, worker, sh.search, starts);
   if (tid < 3) spoiled[tid] = 0;
   __syncthreads();

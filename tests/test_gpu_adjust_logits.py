@@ -142,6 +142,24 @@ def test_in_place(gpu, dtype):
     check_grad(Case(4, 9_001, dtype, masks=3), in_place=True)
 
 
+@pytest.mark.parametrize("dtype", [F, BF, H])
+@pytest.mark.parametrize("over", range(-9, 10))
+def test_ends_of_runs(gpu, dtype, over):
+    """Lists that name the columns around 4,096 and 8,192, where a block's run of columns ends, and a row's first and last ones."""
+    for vocab in (4_096 + over, 8_192 + over):
+        c = Case(4, vocab, dtype, biases=2, masks=1, pitch=1)
+        ids = list(range(4_080, min(vocab, 4_110))) + list(range(vocab - 20, vocab)) + list(range(10))
+        c.history = [ids] * 4
+        c.args["history"], c.args["history_offsets"] = flat(c.history, torch.int32)
+        c.biases = [[(j, float(j % 7)) for j in ids[::2]]] * 4
+        c.args["bias_ids"], c.args["bias_offsets"] = flat(c.biases, torch.int32, lambda x: x[0])
+        c.args["bias_values"], _ = flat(c.biases, torch.float32, lambda x: x[1])
+        for lead in range(2):  # outputs of other alignments
+            store = torch.zeros(lead + 4 * (vocab + 3), dtype=dtype, device="cuda")
+            check(c, store[lead:].view(4, -1)[:, :vocab])
+        check_grad(c)
+
+
 def test_long_histories(gpu):
     """A token that stands more than 2^16 times, and a list longer than its neighbours."""
     c = Case(3, 700, F, history=5)
