@@ -35,10 +35,11 @@ struct Quotient {
 constexpr int ATT_THREADS = 256;
 constexpr int ATT_WAVES = 4;
 constexpr int STAGED = 1024;  // requests whose offsets and lengths are held in LDS for the search
+constexpr int SMALL_ROWS = 16;
 constexpr int EACH = 4;       // items counted by a thread at a time
 
-// What the small kernel (16 rows a wave, 32 keys a unit) and the large one (128 rows
-// a block, 64 keys a unit) make of a step.
+// What the small path (16 rows a wave, 32 keys a unit) and the large one (128 rows a
+// block, 64 keys a unit) make of a step.
 struct Plan {
   int rows;        // of an item
   int keys;        // of a unit
@@ -47,14 +48,15 @@ struct Plan {
   int tokens;      // of an item
   int groups;      // items that the query heads of a key head take
   int least;       // fewest units of a worker
+  Quotient by_tokens;
 };
 
 struct AttentionArgs {
   tt_cache c;
   tt_attention s;
   int capacity;  // tokens that a request's table has room for (at most 2^31 - 65)
-  Plan p;
-  Quotient by_page, by_tokens;
+  Plan small, large;
+  Quotient by_page;
   int per_kv;      // query heads of a key head
   bool vectors;    // queries and out are aligned to 16 bytes
   uint8_t* parts;  // workspace
@@ -68,10 +70,12 @@ struct Leaf {
   int32_t pad[3];
 };
 
+// The workspace: which path ran (256 bytes), a leaf for each worker, two pieces for each
 __host__ __device__ inline int64_t piece_floats(int rows, int dim) { return (int64_t)rows * (dim + 2); }
-__host__ __device__ inline int64_t leaves_bytes(int workers) { return ((int64_t)workers * (int64_t)sizeof(Leaf) + 255) & ~255; }
-__device__ __forceinline__ float* piece_of(const AttentionArgs& a, int worker, int which) {
-  return reinterpret_cast<float*>(a.parts + leaves_bytes(a.p.workers)) + (2 * (int64_t)worker + which) * piece_floats(a.p.rows, a.c.dim);
+__host__ __device__ inline int64_t leaves_bytes(int workers) { return 256 + (((int64_t)workers * (int64_t)sizeof(Leaf) + 255) & ~255); }
+__device__ __forceinline__ Leaf* leaves_of(const AttentionArgs& a) { return reinterpret_cast<Leaf*>(a.parts + 256); }
+__device__ __forceinline__ float* piece_of(const AttentionArgs& a, const Plan& p, int worker, int which) {
+  return reinterpret_cast<float*>(a.parts + leaves_bytes(p.workers)) + (2 * (int64_t)worker + which) * piece_floats(p.rows, a.c.dim);
 }
 
 // One request's place in the step, and an item of it.
@@ -87,21 +91,21 @@ __device__ __forceinline__ int offset_of(const tt_attention& s, int r) { return 
 
 // Slot `slot` of the step's items: request r's begin at slot offsets[r] / tokens + r,
 // which leaves each one room enough.  (Slots without tokens have no units.)
-__device__ __forceinline__ Item item_of(const AttentionArgs& a, int slot, int r, int off0, int off1, int raw1, int length) {
+__device__ __forceinline__ Item item_of(const AttentionArgs& a, const Plan& p, int slot, int r, int off0, int off1, int raw1, int length) {
   Item t;
-  const int64_t at = (int64_t)slot - (a.by_tokens.of(off0) + (int64_t)r);
-  const int64_t row0 = off0 + at * a.p.tokens;
+  const int64_t at = (int64_t)slot - (p.by_tokens.of(off0) + (int64_t)r);
+  const int64_t row0 = off0 + at * p.tokens;
   t.row0 = (int)row0;
   t.tokens = 0;
   t.units = 0;
   if (at < 0 || row0 >= off1) return t;
-  t.tokens = off1 - row0 < a.p.tokens ? (int)(off1 - row0) : a.p.tokens;
+  t.tokens = off1 - row0 < p.tokens ? (int)(off1 - row0) : p.tokens;
   const int64_t low = (int64_t)length - raw1 + row0, high = low + t.tokens - 1;
   t.low = clamped(low, INT32_MIN / 2, INT32_MAX);
   t.last = clamped(high, -1, a.capacity);
   t.begin = a.s.window ? clamped(low - a.s.window + 1, 0, a.capacity) : 0;
   t.front = a.s.sinks < t.begin ? a.s.sinks : t.begin;
-  const int keys = a.p.keys;
+  const int keys = p.keys;
   t.front_units = (t.front + keys - 1) / keys;
   t.begin_unit = t.begin / keys;
   if (t.begin_unit < t.front_units) t.begin_unit = t.front_units;
@@ -114,34 +118,70 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, int slot, int r,
 struct Search {
   int32_t offsets[STAGED + 1], lengths[STAGED];
   int64_t sums[ATT_WAVES];
+  int live[ATT_WAVES];
 };
 // Where a worker begins
 struct Start {
   int slot, request, head, unit;
   int64_t count;  // units
+  Item item;
 };
+
+// Offsets and lengths to LDS (of as many requests as it holds), and whether the
+// step's requests have few rows a key head, so that the small path takes it.
+__device__ __forceinline__ bool few_rows(const AttentionArgs& a, Search& sh) {
+  const tt_attention& s = a.s;
+  const int tid = threadIdx.x, n = s.n_requests;
+  const bool staged = n <= STAGED;
+  int live = 0;
+  for (int i = tid; i <= n; i += ATT_THREADS) {
+    const int x = s.offsets[i], length = i < n ? s.lengths[i] : 0;
+    live += i < n && s.offsets[i + 1] > x;
+    if (staged) {
+      sh.offsets[i] = x;
+      if (i < n) sh.lengths[i] = length;
+    }
+  }
+  const int tokens = clamped(s.offsets[n], 0, s.tokens);
+#pragma unroll
+  for (int d = 32; d; d >>= 1) live += __shfl_xor(live, d);
+  if ((tid & 63) == 0) sh.live[tid >> 6] = live;
+  __syncthreads();
+  live = 0;
+#pragma unroll
+  for (int w = 0; w < ATT_WAVES; w++) live += sh.live[w];
+  return (int64_t)tokens * a.per_kv <= (int64_t)live * SMALL_ROWS;
+}
+
+// n / d; 64-bit divisions take hundreds of instructions
+__device__ __forceinline__ int64_t divided(int64_t n, int64_t d) {
+  return n <= INT32_MAX && d <= INT32_MAX ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
+}
 
 // Finds the parts of the block's COUNT workers (first, first + 1, ...).
 template <int COUNT>
-__device__ __forceinline__ void find_starts(const AttentionArgs& a, int first, Search& sh, Start* starts) {
+__device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& p, int first, Search& sh, Start* starts) {
   const tt_attention& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = s.n_requests;
   const bool staged = n <= STAGED;
-  if (staged) {
-    for (int i = tid; i <= n; i += ATT_THREADS) sh.offsets[i] = s.offsets[i];
-    for (int i = tid; i < n; i += ATT_THREADS) sh.lengths[i] = s.lengths[i];
-  }
-  if (tid < COUNT) starts[tid] = {0, 0, 0, 0, 0};
-  __syncthreads();
+  if (tid < COUNT) starts[tid].count = 0;
   auto raw = [&](int r) { return staged ? sh.offsets[r] : s.offsets[r]; };
   auto offset = [&](int r) { return clamped(raw(r), 0, s.tokens); };
-  const int64_t slots = (int64_t)a.by_tokens.of(offset(n)) + n;
-  // units of EACH slots from slot0 on; the request of the first one
-  auto count = [&](int64_t slot0, int64_t* units, int* requests) {
+  auto begin = [&](int r) { return (int64_t)p.by_tokens.of(offset(r)) + r; };
+  const int64_t slots = begin(n);
+  // threads take one slot each, or EACH
+  const int each = slots <= ATT_THREADS ? 1 : EACH;
+  const int64_t at_once = (int64_t)ATT_THREADS * each;
+  auto item = [&](int64_t slot, int r) {
+    return item_of(a, p, (int)slot, r, offset(r), offset(r + 1), raw(r + 1), staged ? sh.lengths[r] : s.lengths[r]);
+  };
+  // units of the thread's slots from slot0 on; their requests
+  auto count = [&](int64_t slot0, int* units, int* requests) {
+    if (slot0 >= slots) return (int64_t)0;
     int lo = 0, hi = n;  // requests [0, lo) begin at or before slot0
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if ((int64_t)a.by_tokens.of(offset(mid)) + mid <= slot0) lo = mid + 1;
+      if (begin(mid) <= slot0) lo = mid + 1;
       else hi = mid;
     }
     int r = lo > 0 ? lo - 1 : 0;
@@ -149,8 +189,10 @@ __device__ __forceinline__ void find_starts(const AttentionArgs& a, int first, S
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
       const int64_t slot = slot0 + e;
-      while (r + 1 < n && (int64_t)a.by_tokens.of(offset(r + 1)) + r + 1 <= slot) r++;
-      units[e] = slot < slots ? item_of(a, (int)slot, r, offset(r), offset(r + 1), raw(r + 1), staged ? sh.lengths[r] : s.lengths[r]).units : 0;
+      units[e] = 0;
+      if (e >= each || slot >= slots) continue;
+      while (r + 1 < n && begin(r + 1) <= slot) r++;
+      units[e] = item(slot, r).units;
       requests[e] = r;
       sum += units[e];
     }
@@ -176,29 +218,29 @@ __device__ __forceinline__ void find_starts(const AttentionArgs& a, int first, S
     }
     return all;
   };
-  constexpr int64_t AT_ONCE = (int64_t)ATT_THREADS * EACH;
-  int64_t units[EACH], total = 0, before = 0;
-  int requests[EACH];
-  for (int64_t slot0 = 0; slot0 < slots; slot0 += AT_ONCE)
-    total += scan(count(slot0 + tid * EACH, units, requests), before);
+  int64_t total = 0, before = 0, mine = 0;
+  int units[EACH], requests[EACH];
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) total += scan(mine = count(slot0 + tid * each, units, requests), before);
   if (total == 0) return;
-  const int64_t all = total * a.c.kv_heads * a.p.groups;
-  int64_t part = (all + a.p.workers - 1) / a.p.workers;
-  if (part < a.p.least) part = a.p.least;
+  const int64_t all = total * a.c.kv_heads * p.groups;
+  int64_t part = divided(all + p.workers - 1, p.workers);
+  if (part < p.least) part = p.least;
   int64_t base = 0;
-  for (int64_t slot0 = 0; slot0 < slots; slot0 += AT_ONCE) {
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) {
     int64_t here = total;
-    if (slots > AT_ONCE) here = scan(count(slot0 + tid * EACH, units, requests), before);
-#pragma unroll
+    if (slots > at_once) here = scan(mine = count(slot0 + tid * each, units, requests), before);
     for (int w = 0; w < COUNT; w++) {
       const int64_t from = (first + w) * part;
-      if (from >= all) continue;
-      const int64_t head = from / total;
+      if (from >= all) break;
+      const int64_t head = divided(from, total);
       int64_t x = from - head * total - base - before;
+      if (x < 0 || x >= mine) continue;
 #pragma unroll
       for (int e = 0; e < EACH; e++) {
-        if (x >= 0 && x < units[e])
-          starts[w] = {(int)(slot0 + tid * EACH + e), requests[e], (int)head, (int)x, from + part < all ? part : all - from};
+        if (x >= 0 && x < units[e]) {
+          const int64_t slot = slot0 + tid * each + e;
+          starts[w] = {(int)slot, requests[e], (int)head, (int)x, from + part < all ? part : all - from, item(slot, requests[e])};
+        }
         x -= units[e];
       }
     }
@@ -214,28 +256,23 @@ struct Walk {
   int slot, request, head, unit, slots;
   int64_t left;
   Item item;
-  __device__ __forceinline__ void read(const AttentionArgs& a) {
+  __device__ __forceinline__ void read(const AttentionArgs& a, const Plan& p) {
     const int raw1 = a.s.offsets[request + 1];
-    item = item_of(a, slot, request, offset_of(a.s, request), offset_of(a.s, request + 1), raw1, a.s.lengths[request]);
-    item.row0 = uniform(item.row0);
-    item.tokens = uniform(item.tokens);
-    item.low = uniform(item.low);
-    item.front = uniform(item.front);
-    item.begin = uniform(item.begin);
-    item.last = uniform(item.last);
-    item.front_units = uniform(item.front_units);
-    item.begin_unit = uniform(item.begin_unit);
-    item.units = uniform(item.units);
+    take(item_of(a, p, slot, request, offset_of(a.s, request), offset_of(a.s, request + 1), raw1, a.s.lengths[request]));
   }
-  __device__ __forceinline__ Walk(const AttentionArgs& a, const Start& st)
+  __device__ __forceinline__ void take(const Item& t) {
+    item = {uniform(t.row0),  uniform(t.tokens),      uniform(t.low),        uniform(t.front), uniform(t.begin),
+            uniform(t.last),  uniform(t.front_units), uniform(t.begin_unit), uniform(t.units)};
+  }
+  __device__ __forceinline__ Walk(const AttentionArgs& a, const Plan& p, const Start& st)
       : slot(uniform(st.slot)), request(uniform(st.request)), head(uniform(st.head)), unit(uniform(st.unit)),
-        slots(a.by_tokens.of(offset_of(a.s, a.s.n_requests)) + a.s.n_requests),
+        slots(uniform(p.by_tokens.of(offset_of(a.s, a.s.n_requests)) + a.s.n_requests)),
         left(((int64_t)uniform((int)(st.count >> 32)) << 32) | (uint32_t)uniform((int)st.count)) {
-    if (left > 0) read(a);
+    take(st.item);
   }
   // to the next item that has units (there is one: left > 0; offsets that are not
   // in order may have none, and the walk ends there)
-  __device__ __forceinline__ void next(const AttentionArgs& a) {
+  __device__ __forceinline__ void next(const AttentionArgs& a, const Plan& p) {
     unit = 0;
     do {
       slot++;
@@ -245,11 +282,11 @@ struct Walk {
         head++;
       }
       while (request + 1 < a.s.n_requests &&
-             (int64_t)a.by_tokens.of(offset_of(a.s, request + 1)) + request + 1 <= slot)
+             (int64_t)p.by_tokens.of(offset_of(a.s, request + 1)) + request + 1 <= slot)
         request++;
       request = uniform(request);
-      read(a);
-    } while (item.units == 0 && head < a.c.kv_heads * a.p.groups);
+      read(a, p);
+    } while (item.units == 0 && head < a.c.kv_heads * p.groups);
     if (item.units == 0) left = 0;
   }
 };
@@ -323,8 +360,8 @@ __device__ __forceinline__ Vec8<T> both(S4 a, S4 b) {
 }
 
 // Whether every token of the item sees every key of [k0, k0 + keys)
-__device__ __forceinline__ bool all_seen(const AttentionArgs& a, const Item& t, int k0) {
-  const int end = k0 + a.p.keys;
+__device__ __forceinline__ bool all_seen(const AttentionArgs& a, const Item& t, int k0, int keys) {
+  const int end = k0 + keys;
   const int64_t begin = a.s.window ? (int64_t)t.low + t.tokens - a.s.window : 0;  // of the last token
   return end <= t.last + 1 && end - 1 <= t.low && (k0 >= begin || end <= a.s.sinks);
 }
@@ -345,8 +382,8 @@ __device__ __forceinline__ uint64_t seen_bits(const AttentionArgs& a, int positi
   return below((int64_t)last + 1) & (~below(begin) | below(a.s.sinks));
 }
 __device__ __forceinline__ bool needed(const Item& t, int key) { return key <= t.last && (key < t.front || key >= t.begin); }
-__device__ __forceinline__ int first_key(const AttentionArgs& a, const Item& t, int unit) {
-  return (unit < t.front_units ? unit : t.begin_unit + unit - t.front_units) * a.p.keys;
+__device__ __forceinline__ int first_key(const Item& t, int unit, int keys) {
+  return (unit < t.front_units ? unit : t.begin_unit + unit - t.front_units) * keys;
 }
 // Page of a key's token: -1 where there is none, -2 where no token of the item sees it
 __device__ __forceinline__ int page_of(const AttentionArgs& a, const Item& t, const int32_t* table, int key) {
@@ -373,19 +410,19 @@ __device__ __forceinline__ int worker_of(uint32_t block, uint32_t blocks) { retu
 // the keys straight into the product, the values through LDS that is the wave's own.
 // The next unit's are under way during the exponentials and the second product.
 template <class T, int KK>  // KK: 32 elements of a head
-__global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(AttentionArgs a) {
-  constexpr int DT = 2 * KK, PITCH = KK * 32 + 16;  // (rows 32 bytes apart in the banks)
-  __shared__ union {
-    Search search;
-    T values[ATT_WAVES][32][PITCH];
-  } sh;
-  __shared__ Start starts[ATT_WAVES];
+struct SmallShared {
+  static constexpr int PITCH = KK * 32 + 16;  // (rows 32 bytes apart in the banks)
+  T values[ATT_WAVES][32][PITCH];
+};
+template <class T, int KK>
+__device__ __forceinline__ void small_path(const AttentionArgs& a, Search& search, SmallShared<T, KK>& sh, Start* starts) {
+  constexpr int DT = 2 * KK, KEYS = 32, PITCH = SmallShared<T, KK>::PITCH;
+  const Plan& p = a.small;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
   const int dim = a.c.dim;
   const int first = blockIdx.x * ATT_WAVES, worker = first + wave;
-  find_starts<ATT_WAVES>(a, first, sh.search, starts);
-  __syncthreads();
-  Walk w(a, starts[wave]);
+  find_starts<ATT_WAVES>(a, p, first, search, starts);
+  Walk w(a, p, starts[wave]);
   __syncthreads();  // (the search's LDS is the values' from here on)
   T(*values)[PITCH] = sh.values[wave];
   Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
@@ -397,10 +434,10 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
   while (w.left > 0) {
     const Item& t = w.item;
     const int take = (int64_t)(t.units - w.unit) < w.left ? t.units - w.unit : (int)w.left;
-    const int kv = w.head / a.p.groups, h0 = (w.head - kv * a.p.groups) * a.p.heads;
-    const int heads = a.per_kv - h0 < a.p.heads ? a.per_kv - h0 : a.p.heads;
-    const int rows = t.tokens * a.p.heads;  // (rows of heads past the last one are not used)
-    const int my_token = col / a.p.heads, my_head = col - my_token * a.p.heads;
+    const int kv = w.head / p.groups, h0 = (w.head - kv * p.groups) * p.heads;
+    const int heads = a.per_kv - h0 < p.heads ? a.per_kv - h0 : p.heads;
+    const int rows = t.tokens * p.heads;  // (rows of heads past the last one are not used)
+    const int my_token = col / p.heads, my_head = col - my_token * p.heads;
     const bool live = col < rows && my_head < heads;
     const int position = t.low + my_token;
     const int64_t q_row = t.row0 + my_token, q_head = (int64_t)kv * a.per_kv + h0 + my_head;
@@ -417,12 +454,12 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
     Vec8<T> k[2][KK], v[2][KK];
     int pages[2];
     auto fetch_pages = [&](int unit) {
-      const int k0 = first_key(a, t, unit);
+      const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
       for (int i = 0; i < 2; i++) pages[i] = page_of(a, t, table, k0 + 16 * i + col);
     };
     auto fetch = [&](int unit) {
-      const int k0 = first_key(a, t, unit);
+      const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
       for (int i = 0; i < 2; i++) {
         const int64_t at = vector_at(a, pages[i], k0 + 16 * i + col, head);
@@ -447,8 +484,8 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
     fetch(w.unit);
     if (w.unit + 1 < end) fetch_pages(w.unit + 1);
     for (int unit = w.unit; unit < end; unit++) {
-      const int k0 = first_key(a, t, unit);
-      const bool edge = !all_seen(a, t, k0);
+      const int k0 = first_key(t, unit, KEYS);
+      const bool edge = !all_seen(a, t, k0, KEYS);
       // values of keys that only some tokens see must not reach the others through 0 * NaN
       uint64_t spoiled[2] = {0, 0};
       if (edge && t.tokens > 1) {
@@ -490,7 +527,7 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
         if (unit + 2 < end) fetch_pages(unit + 2);
       }
       if (edge) {
-        const uint32_t seen = (uint32_t)seen_bits(a, position, k0, 32) >> (quad * 4);
+        const uint32_t seen = (uint32_t)seen_bits(a, position, k0, KEYS) >> (quad * 4);
 #pragma unroll
         for (int i = 0; i < 2; i++)
 #pragma unroll
@@ -515,20 +552,20 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
         for (int d = 0; d < DT; d++) o[d] *= f;
       }
       const float base = m == NEG_INF ? 0.f : m;
-      Vec8<T> p;
+      Vec8<T> weights;
 #pragma unroll
       for (int i = 0; i < 2; i++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const float x = __builtin_amdgcn_exp2f(s[i][e] - base);
           sum += x;
-          p[4 * i + e] = (T)x;
+          weights[4 * i + e] = (T)x;
         }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int d = 0; d < DT; d++) {
         const T* from = &values[quad * 4 + (col >> 2)][d * 16 + (col & 3) * 4];
-        o[d] = product16(both<T>(transposed(from), transposed(from + 16 * PITCH)), p, o[d]);
+        o[d] = product16(both<T>(transposed(from), transposed(from + 16 * PITCH)), weights, o[d]);
       }
       __builtin_amdgcn_wave_barrier();
       if (spoiled[0] | spoiled[1]) {
@@ -566,7 +603,7 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
         if (a.s.logsums && quad == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
       }
     } else {
-      float* piece = piece_of(a, worker, began ? 0 : 1);
+      float* piece = piece_of(a, p, worker, began ? 0 : 1);
       if (live) {
 #pragma unroll
         for (int d = 0; d < DT; d++)
@@ -574,7 +611,7 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
             float* x = piece + (int64_t)col * dim + d * 16 + quad * 4;
             *reinterpret_cast<F4*>(x) = o[d];
           }
-        if (quad == 0) *reinterpret_cast<float2*>(piece + (int64_t)a.p.rows * dim + 2 * col) = float2{m, sum};
+        if (quad == 0) *reinterpret_cast<float2*>(piece + (int64_t)p.rows * dim + 2 * col) = float2{m, sum};
       }
       if (began) {
         leaf.first = ends ? 2 : 1;
@@ -586,9 +623,9 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
       }
     }
     w.left -= take;
-    if (w.left > 0) w.next(a);
+    if (w.left > 0) w.next(a, p);
   }
-  if (lane == 0) *(reinterpret_cast<Leaf*>(a.parts) + worker) = leaf;
+  if (lane == 0) leaves_of(a)[worker] = leaf;
 }
 
 // ---- 128 rows a block: prompts ---------------------------------------------------
@@ -597,28 +634,25 @@ __global__ __launch_bounds__(ATT_THREADS, KK <= 4 ? 2 : 1) void small_kernel(Att
 // that one barrier a unit is enough: the next unit's come from memory to registers
 // during a unit's products and are written where the last unit's were.
 template <class T, int DP>  // DP: elements of a head, with zeros behind its own
-__global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(AttentionArgs a) {
-  constexpr int KEYS = 64, KK = DP / 16, DT = DP / 32;
-  constexpr int K_PITCH = DP + 8;                                  // (16 rows 16 bytes apart in the banks)
-  constexpr int V_PITCH = DP == 96 ? DP : DP + 32;                 // (4 rows 64 bytes apart)
+struct LargeShared {
+  static constexpr int KEYS = 64;
+  static constexpr int K_PITCH = DP + 8;                   // (16 rows 16 bytes apart in the banks)
+  static constexpr int V_PITCH = DP == 96 ? DP : DP + 32;  // (4 rows 64 bytes apart)
+  T keys[2][KEYS][K_PITCH];
+  T values[2][KEYS][V_PITCH];
+};
+template <class T, int DP>
+__device__ __forceinline__ void large_path(const AttentionArgs& a, Search& search, LargeShared<T, DP>& sh, Start* starts,
+                                           unsigned long long* spoiled) {
+  constexpr int KEYS = 64, KK = DP / 16, DT = DP / 32, K_PITCH = LargeShared<T, DP>::K_PITCH, V_PITCH = LargeShared<T, DP>::V_PITCH;
   constexpr int PER_ROW = DP == 64 ? 8 : DP == 256 ? 32 : 16;      // threads that fetch a row
   constexpr int PASS = ATT_THREADS / PER_ROW, PASSES = KEYS / PASS;
-  struct Tiles {
-    T keys[2][KEYS][K_PITCH];
-    T values[2][KEYS][V_PITCH];
-  };
-  __shared__ __align__(16) union {
-    Search search;
-    Tiles tiles;
-  } sh;
-  __shared__ Start starts[1];
-  __shared__ unsigned long long spoiled[3];
+  const Plan& p = a.large;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int dim = a.c.dim, worker = blockIdx.x;
-  find_starts<1>(a, worker, sh.search, starts);
+  const int dim = a.c.dim, worker = worker_of(blockIdx.x, gridDim.x);
+  find_starts<1>(a, p, worker, search, starts);
   if (tid < 3) spoiled[tid] = 0;
-  __syncthreads();
-  Walk w(a, starts[0]);
+  Walk w(a, p, starts[0]);
   __syncthreads();  // (the search's LDS is the tiles' from here on)
   Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
   const float c = a.s.scale * LOG2E;
@@ -630,16 +664,16 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
   while (w.left > 0) {
     const Item& t = w.item;
     const int take = (int64_t)(t.units - w.unit) < w.left ? t.units - w.unit : (int)w.left;
-    const int kv = w.head / a.p.groups, h0 = (w.head - kv * a.p.groups) * a.p.heads;
-    const int heads = a.per_kv - h0 < a.p.heads ? a.per_kv - h0 : a.p.heads;
-    const int row = wave * 32 + col, rows = t.tokens * a.p.heads;
-    const int my_token = row / a.p.heads, my_head = row - my_token * a.p.heads;
+    const int kv = w.head / p.groups, h0 = (w.head - kv * p.groups) * p.heads;
+    const int heads = a.per_kv - h0 < p.heads ? a.per_kv - h0 : p.heads;
+    const int row = wave * 32 + col, rows = t.tokens * p.heads;
+    const int my_token = row / p.heads, my_head = row - my_token * p.heads;
     const bool live = row < rows && my_head < heads;
     const int position = t.low + my_token;
     const int64_t q_row = t.row0 + my_token, q_head = (int64_t)kv * a.per_kv + h0 + my_head;
     // the wave's tokens
     const int wave_rows = rows - wave * 32 < 32 ? rows - wave * 32 : 32;
-    const int low = t.low + uniform(wave * 32 / a.p.heads), high = t.low + uniform((wave * 32 + wave_rows - 1) / a.p.heads);
+    const int low = t.low + uniform(wave * 32 / p.heads), high = t.low + uniform((wave * 32 + wave_rows - 1) / p.heads);
     Vec8<T> q[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; kk++) {
@@ -652,12 +686,12 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
     Vec8<T> k[PASSES], v[PASSES];
     int pages[PASSES];
     auto fetch_pages = [&](int unit) {
-      const int k0 = first_key(a, t, unit);
+      const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
       for (int i = 0; i < PASSES; i++) pages[i] = page_of(a, t, table, k0 + PASS * i + row_in);
     };
     auto fetch = [&](int unit) {
-      const int k0 = first_key(a, t, unit);
+      const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
       for (int i = 0; i < PASSES; i++) {
         const int64_t at = vector_at(a, pages[i], k0 + PASS * i + row_in, head);
@@ -673,7 +707,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
     // registers to the tiles of `to`; values of keys that only some tokens see must
     // not reach the others through 0 * NaN
     auto put = [&](int unit, int to, int word) {
-      if (t.tokens > 1 && !all_seen(a, t, first_key(a, t, unit))) {
+      if (t.tokens > 1 && !all_seen(a, t, first_key(t, unit, KEYS), KEYS)) {
 #pragma unroll
         for (int i = 0; i < PASSES; i++) {
           const uint32_t bad = not_finite(v[i]);
@@ -688,8 +722,8 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
       if (stores) {
 #pragma unroll
         for (int i = 0; i < PASSES; i++) {
-          *reinterpret_cast<Vec8<T>*>(&sh.tiles.keys[to][PASS * i + row_in][chunk * 8]) = k[i];
-          *reinterpret_cast<Vec8<T>*>(&sh.tiles.values[to][PASS * i + row_in][chunk * 8]) = v[i];
+          *reinterpret_cast<Vec8<T>*>(&sh.keys[to][PASS * i + row_in][chunk * 8]) = k[i];
+          *reinterpret_cast<Vec8<T>*>(&sh.values[to][PASS * i + row_in][chunk * 8]) = v[i];
         }
       }
     };
@@ -712,12 +746,12 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
         fetch(unit + 1);
         if (unit + 2 < end) fetch_pages(unit + 2);
       }
-      const int k0 = first_key(a, t, unit);
+      const int k0 = first_key(t, unit, KEYS);
       const int64_t begin_low = a.s.window ? (int64_t)low - a.s.window + 1 : 0, begin_high = a.s.window ? (int64_t)high - a.s.window + 1 : 0;
       const bool any = wave_rows > 0 && k0 <= high && (k0 + KEYS > begin_low || k0 < a.s.sinks || begin_low > a.capacity);
       if (any) {
-        const T(*keys)[K_PITCH] = sh.tiles.keys[turn];
-        const T(*values)[V_PITCH] = sh.tiles.values[turn];
+        const T(*keys)[K_PITCH] = sh.keys[turn];
+        const T(*values)[V_PITCH] = sh.values[turn];
         F16 s[2];
 #pragma unroll
         for (int i = 0; i < 2; i++) {
@@ -753,21 +787,21 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
           for (int d = 0; d < DT; d++) o[d] *= f;
         }
         const float base = m == NEG_INF ? 0.f : m;
-        Vec8<T> p[4];
+        Vec8<T> weights[4];
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
           for (int e = 0; e < 8; e++) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], c, -base));
             sum += x;
-            p[i][e] = (T)x;
+            weights[i][e] = (T)x;
           }
 #pragma unroll
         for (int d = 0; d < DT; d++)
 #pragma unroll
           for (int i = 0; i < 4; i++) {
             const T* from = &values[16 * i + 4 * half + ((lane & 15) >> 2)][d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4];
-            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * V_PITCH)), p[i], o[d]);
+            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * V_PITCH)), weights[i], o[d]);
           }
         uint64_t bad = spoiled[third];
         bad = ((uint64_t)uniform((int)(bad >> 32)) << 32) | (uint32_t)uniform((int)bad);
@@ -808,7 +842,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
         if (a.s.logsums && half == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
       }
     } else {
-      float* piece = piece_of(a, worker, began ? 0 : 1);
+      float* piece = piece_of(a, p, worker, began ? 0 : 1);
       if (live) {
 #pragma unroll
         for (int d = 0; d < DT; d++)
@@ -817,7 +851,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
             const int at = d * 32 + 2 * e + half * 4;
             if (at < dim) *reinterpret_cast<F4*>(piece + (int64_t)row * dim + at) = F4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
           }
-        if (half == 0) *reinterpret_cast<float2*>(piece + (int64_t)a.p.rows * dim + 2 * row) = float2{m, sum};
+        if (half == 0) *reinterpret_cast<float2*>(piece + (int64_t)p.rows * dim + 2 * row) = float2{m, sum};
       }
       if (began) {
         leaf.first = ends ? 2 : 1;
@@ -829,98 +863,121 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void large_kernel(A
       }
     }
     w.left -= take;
-    if (w.left > 0) w.next(a);
+    if (w.left > 0) w.next(a, p);
   }
-  if (tid == 0) *(reinterpret_cast<Leaf*>(a.parts) + worker) = leaf;
+  if (tid == 0) leaves_of(a)[worker] = leaf;
+}
+
+template <class T, int DP>
+__global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void attention_kernel(AttentionArgs a) {
+  __shared__ __align__(16) union {
+    Search search;
+    SmallShared<T, DP / 32> small;
+    LargeShared<T, DP> large;
+  } sh;
+  __shared__ Start starts[ATT_WAVES];
+  __shared__ unsigned long long spoiled[3];
+  const bool small = few_rows(a, sh.search);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int32_t*>(a.parts) = small;
+  if (small) small_path<T, DP / 32>(a, sh.search, sh.small, starts);
+  else large_path<T, DP>(a, sh.search, sh.large, starts, spoiled);
 }
 
 // ---- joins the pieces of items that several workers have ----------------------------
 
-// A block for a worker whose last piece begins an item, and for some of its rows.
-// SMALL: one row, whose pieces are many: groups of lanes take every n-th piece.
-// Else a group takes a row.
-template <class T, bool SMALL>
+// Blocks (w, 0 .. JOIN_BLOCKS - 1) for worker w, if its last piece begins an item: they
+// share its rows.  Groups of lanes take a row each, or, where an item has many pieces,
+// all of them one row, each every n-th piece.
+constexpr int JOIN_BLOCKS = 4;
+template <class T>
 __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int lanes) {
   __shared__ F4 sums[ATT_THREADS];
   __shared__ float2 heads[ATT_THREADS];
+  const bool small = *reinterpret_cast<const int32_t*>(a.parts) != 0;
+  const Plan& p = small ? a.small : a.large;
   const int tid = threadIdx.x, worker = blockIdx.x, dim = a.c.dim;
-  const Leaf* leaves = reinterpret_cast<const Leaf*>(a.parts);
+  if (worker >= p.workers) return;
+  const Leaf* leaves = leaves_of(a);
   const Leaf leaf = leaves[worker];
   if (!leaf.last) return;
-  const int groups = ATT_THREADS / lanes, group = tid / lanes, at = (tid - group * lanes) * 4;
-  const int row = SMALL ? blockIdx.y : blockIdx.y * groups + group;
-  const int kv = leaf.head / a.p.groups, h0 = (leaf.head - kv * a.p.groups) * a.p.heads;
-  const int token = row / a.p.heads, head = row - token * a.p.heads;
-  const bool live = token < leaf.tokens && head < a.per_kv - h0;
-  if (SMALL && !live) return;
   // the worker whose first piece ends the item
   int last = worker + 1;
-  for (; last < a.p.workers; last += 64) {
+  for (; last < p.workers; last += 64) {
     const int i = last + (tid & 63);
-    const uint64_t votes = __ballot(i < a.p.workers && leaves[i].first == 2);
+    const uint64_t votes = __ballot(i < p.workers && leaves[i].first == 2);
     if (votes) {
       last += __builtin_ctzll(votes);
       break;
     }
   }
-  if (last >= a.p.workers) last = a.p.workers - 1;
+  if (last >= p.workers) last = p.workers - 1;
   const int pieces = last - worker + 1;
-  float m = NEG_INF, sum = 0.f;
-  F4 o = {0.f, 0.f, 0.f, 0.f};
-  const bool mine = live && at < dim;
-  if (mine) {
-    for (int i = SMALL ? group : 0; i < pieces; i += SMALL ? groups : 1) {
-      const float* piece = piece_of(a, worker + i, i ? 0 : 1);
-      const float2 h = *reinterpret_cast<const float2*>(piece + (int64_t)a.p.rows * dim + 2 * row);
-      const F4 x = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
-      const float top = fmaxf(m, h.x);
-      const float f = m == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(m - top), g = h.x == NEG_INF ? 0.f : __builtin_amdgcn_exp2f(h.x - top);
-      // (a piece that is all NaN has no maximum: its sums count as they are)
-      sum = sum * (m == NEG_INF && sum != sum ? 1.f : f) + h.y * (h.x == NEG_INF && h.y != h.y ? 1.f : g);
-      o = o * f + x * (h.x == NEG_INF && h.y != h.y ? 1.f : g);
+  const int groups = ATT_THREADS / lanes, group = tid / lanes, at = (tid - group * lanes) * 4;
+  const int kv = leaf.head / p.groups, h0 = (leaf.head - kv * p.groups) * p.heads;
+  const bool many = pieces > 2 * groups;
+  const int rows = leaf.tokens * p.heads, share = many ? 1 : groups;  // rows at a time
+  for (int row0 = blockIdx.y * share; row0 < rows; row0 += JOIN_BLOCKS * share) {
+    const int row = many ? row0 : row0 + group;
+    const int token = row / p.heads, head = row - token * p.heads;
+    const bool mine = row < rows && head < a.per_kv - h0 && at < dim;
+    float m = NEG_INF, sum = 0.f;
+    F4 o = {0.f, 0.f, 0.f, 0.f};
+    // (a piece that is all NaN has no maximum: its sums count as they are)
+    auto weight = [](float x, float y, float top) { return x == NEG_INF ? (y != y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(x - top); };
+    if (mine) {
+#pragma unroll 4
+      for (int i = many ? group : 0; i < pieces; i += many ? groups : 1) {
+        const float* piece = piece_of(a, p, worker + i, i ? 0 : 1);
+        const float2 h = *reinterpret_cast<const float2*>(piece + (int64_t)p.rows * dim + 2 * row);
+        const F4 x = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
+        const float top = fmaxf(m, h.x), f = weight(m, sum, top), g = weight(h.x, h.y, top);
+        sum = sum * f + h.y * g;
+        o = o * f + x * g;
+        m = top;
+      }
+    }
+    if (many) {
+      __syncthreads();
+      sums[tid] = o;
+      heads[tid] = float2{m, sum};
+      __syncthreads();
+      if (group != 0 || !mine) continue;
+      float top = m;
+      for (int g = 1; g < groups; g++) top = fmaxf(top, heads[g * lanes + tid].x);
+      o = F4{0.f, 0.f, 0.f, 0.f};
+      sum = 0.f;
+      for (int g = 0; g < groups; g++) {
+        const float2 h = heads[g * lanes + tid];
+        const float f = weight(h.x, h.y, top);
+        sum += h.y * f;
+        o += sums[g * lanes + tid] * f;
+      }
       m = top;
     }
+    if (!mine) continue;
+    const bool none = m == NEG_INF && sum == 0.f;
+    const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
+    const float x[4] = {o[0], o[1], o[2], o[3]};
+    store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);
+    if (a.s.logsums && at == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
   }
-  if (SMALL) {
-    sums[tid] = o;
-    heads[tid] = float2{m, sum};
-    __syncthreads();
-    if (group != 0 || !mine) return;
-    float top = m;
-    for (int g = 1; g < groups; g++) top = fmaxf(top, heads[g * lanes + tid].x);
-    o = F4{0.f, 0.f, 0.f, 0.f};
-    sum = 0.f;
-    for (int g = 0; g < groups; g++) {
-      const float2 h = heads[g * lanes + tid];
-      const float f = h.x == NEG_INF ? (h.y != h.y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(h.x - top);
-      sum += h.y * f;
-      o += sums[g * lanes + tid] * f;
-    }
-    m = top;
-  }
-  if (!mine) return;
-  const bool none = m == NEG_INF && sum == 0.f;
-  const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
-  const float x[4] = {o[0], o[1], o[2], o[3]};
-  store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);
-  if (a.s.logsums && at == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
 }
 
 // ---- the calls ----------------------------------------------------------------------
 
-constexpr int SMALL_WORKERS = 2048, LARGE_WORKERS = 512;
+constexpr int BLOCKS = 512;  // two a compute unit; heads of more than 128 elements: one
 
-Plan plan_of(int64_t tokens, int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t dim) {
+Plan plan_of(bool small, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   const int per_kv = q_heads / kv_heads;
   Plan p;
-  const bool small = tokens * per_kv <= 16 * (int64_t)n_requests;
-  p.rows = small ? 16 : 128;
+  p.rows = small ? SMALL_ROWS : 128;
   p.keys = small ? 32 : 64;
-  p.workers = (small ? SMALL_WORKERS : LARGE_WORKERS) / (dim > 128 ? 2 : 1);
+  p.workers = BLOCKS / (dim > 128 ? 2 : 1) * (small ? ATT_WAVES : 1);
   p.least = 4;
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
   p.tokens = p.rows / p.heads;
+  p.by_tokens = Quotient((uint32_t)p.tokens);
   return p;
 }
 
@@ -928,22 +985,12 @@ int64_t room_of(const Plan& p, int dim) { return leaves_bytes(p.workers) + 2 * (
 
 template <class T>
 int run_attention(const AttentionArgs& a, hipStream_t st) {
-  const int kk = (a.c.dim + 31) / 32, rows = a.p.tokens * a.p.heads;
+  const int kk = (a.c.dim + 31) / 32;
   int lanes = 8;  // of a row in the join
   while (lanes * 4 < a.c.dim) lanes *= 2;
-  const bool small = a.p.rows == 16;
-  if (small) {
-    auto* kernel = kk <= 2 ? small_kernel<T, 2> : kk == 3 ? small_kernel<T, 3> : kk == 4 ? small_kernel<T, 4> : small_kernel<T, 8>;
-    if (launch(kernel, dim3(a.p.workers / ATT_WAVES), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
-  } else {
-    auto* kernel = kk <= 2 ? large_kernel<T, 64> : kk == 3 ? large_kernel<T, 96> : kk == 4 ? large_kernel<T, 128> : large_kernel<T, 256>;
-    if (launch(kernel, dim3(a.p.workers), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
-  }
-  const int each = small ? 1 : ATT_THREADS / lanes;  // rows of a block
-  return launch(small ? join_kernel<T, true> : join_kernel<T, false>, dim3(a.p.workers, (rows + each - 1) / each), dim3(ATT_THREADS), st,
-                a, lanes) == hipSuccess
-             ? TT_OK
-             : TT_ERR_HIP;
+  auto* kernel = kk <= 2 ? attention_kernel<T, 64> : kk == 3 ? attention_kernel<T, 96> : kk == 4 ? attention_kernel<T, 128> : attention_kernel<T, 256>;
+  if (launch(kernel, dim3(a.large.workers), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
+  return launch(join_kernel<T>, dim3(a.small.workers, JOIN_BLOCKS), dim3(ATT_THREADS), st, a, lanes) == hipSuccess ? TT_OK : TT_ERR_HIP;
 }
 
 }  // namespace
@@ -956,7 +1003,9 @@ extern "C" int64_t tt_cache_attention_workspace(int64_t tokens, int32_t n_reques
   if (tokens < 0 || tokens > INT32_MAX || n_requests < 0 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || dim < 8 ||
       dim > TT_MAX_HEAD_DIM || dim % 8)
     return TT_ERR_BAD_ARG;
-  return tokens == 0 || n_requests == 0 ? 0 : room_of(plan_of(tokens, n_requests, q_heads, kv_heads, dim), dim);
+  if (tokens == 0 || n_requests == 0) return 0;
+  const int64_t small = room_of(plan_of(true, q_heads, kv_heads, dim), dim), large = room_of(plan_of(false, q_heads, kv_heads, dim), dim);
+  return small > large ? small : large;
 }
 
 extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* step, void* workspace, int64_t workspace_bytes,
@@ -978,16 +1027,15 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
   if (s.tokens + s.n_requests > INT32_MAX) return TT_ERR_TOO_LARGE;
   auto in_vectors = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; };
   const int64_t capacity = (int64_t)s.table_width * cache->page_size;
-  AttentionArgs a{*cache,
+  const AttentionArgs a{*cache,
                   s,
                   (int)(capacity < INT32_MAX - 64 ? capacity : INT32_MAX - 64),
-                  plan_of(s.tokens, s.n_requests, s.q_heads, cache->kv_heads, cache->dim),
+                  plan_of(true, s.q_heads, cache->kv_heads, cache->dim),
+                  plan_of(false, s.q_heads, cache->kv_heads, cache->dim),
                   Quotient((uint32_t)cache->page_size),
-                  Quotient(1),
                   s.q_heads / cache->kv_heads,
                   in_vectors(s.queries, s.query_stride) && in_vectors(s.out, s.out_stride),
                   static_cast<uint8_t*>(workspace)};
-  a.by_tokens = Quotient((uint32_t)a.p.tokens);
   return cache->type == TT_BF16 ? run_attention<bf16_t>(a, static_cast<hipStream_t>(stream))
                                 : run_attention<f16_t>(a, static_cast<hipStream_t>(stream));
 }
