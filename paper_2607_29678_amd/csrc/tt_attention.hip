@@ -48,6 +48,11 @@ struct Plan {
   int tokens;      // of an item
   int groups;      // items that the query heads of a key head take
   int least;       // fewest units of a worker
+  // Head units each have workers / stride workers, who take equal parts of its units:
+  // worker w is with head unit w % stride, so that neighbours read neighbouring heads
+  // of the same tokens.  More head units than workers: stride is 1 and all units stand
+  // in one line, head after head.
+  int stride, parts;
   Quotient by_tokens;
 };
 
@@ -122,7 +127,7 @@ struct Search {
 };
 // Where a worker begins
 struct Start {
-  int slot, request, head, unit;
+  int slot, request, head, unit, slots;
   int64_t count;  // units
   Item item;
 };
@@ -222,24 +227,25 @@ __device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& 
   int units[EACH], requests[EACH];
   for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) total += scan(mine = count(slot0 + tid * each, units, requests), before);
   if (total == 0) return;
-  const int64_t all = total * a.c.kv_heads * p.groups;
-  int64_t part = divided(all + p.workers - 1, p.workers);
-  if (part < p.least) part = p.least;
+  const int64_t line = p.stride > 1 ? total : total * a.c.kv_heads * p.groups;
+  int64_t size = divided(line + p.parts - 1, p.parts);
+  if (size < p.least) size = p.least;
   int64_t base = 0;
   for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) {
     int64_t here = total;
     if (slots > at_once) here = scan(mine = count(slot0 + tid * each, units, requests), before);
     for (int w = 0; w < COUNT; w++) {
-      const int64_t from = (first + w) * part;
-      if (from >= all) break;
-      const int64_t head = divided(from, total);
-      int64_t x = from - head * total - base - before;
+      const int part = (first + w) / p.stride;
+      const int64_t from = part * size;
+      if (from >= line || part >= p.parts) break;
+      const int64_t over = p.stride > 1 ? 0 : divided(from, total), head = p.stride > 1 ? first + w - part * p.stride : over;
+      int64_t x = from - over * total - base - before;
       if (x < 0 || x >= mine) continue;
 #pragma unroll
       for (int e = 0; e < EACH; e++) {
         if (x >= 0 && x < units[e]) {
           const int64_t slot = slot0 + tid * each + e;
-          starts[w] = {(int)slot, requests[e], (int)head, (int)x, from + part < all ? part : all - from, item(slot, requests[e])};
+          starts[w] = {(int)slot, requests[e], (int)head, (int)x, (int)slots, from + size < line ? size : line - from, item(slot, requests[e])};
         }
         x -= units[e];
       }
@@ -264,9 +270,9 @@ struct Walk {
     item = {uniform(t.row0),  uniform(t.tokens),      uniform(t.low),        uniform(t.front), uniform(t.begin),
             uniform(t.last),  uniform(t.front_units), uniform(t.begin_unit), uniform(t.units)};
   }
-  __device__ __forceinline__ Walk(const AttentionArgs& a, const Plan& p, const Start& st)
+  __device__ __forceinline__ explicit Walk(const Start& st)
       : slot(uniform(st.slot)), request(uniform(st.request)), head(uniform(st.head)), unit(uniform(st.unit)),
-        slots(uniform(p.by_tokens.of(offset_of(a.s, a.s.n_requests)) + a.s.n_requests)),
+        slots(uniform(st.slots)),
         left(((int64_t)uniform((int)(st.count >> 32)) << 32) | (uint32_t)uniform((int)st.count)) {
     take(st.item);
   }
@@ -400,10 +406,6 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, int page, i
 // A running maximum goes up only where it has to by more than this (in powers of two)
 constexpr float SLACK = 8.f;
 
-// Workers whose parts follow each other run on one XCD (blocks go to the XCDs in
-// turn): the keys of a head that neighbouring items share stay in its L2.
-__device__ __forceinline__ int worker_of(uint32_t block, uint32_t blocks) { return (int)(block % 8 * (blocks / 8) + block / 8); }
-
 // ---- 16 rows a wave: single tokens -----------------------------------------------
 
 // A wave takes its units by itself: 32 keys and values go from memory to registers,
@@ -420,9 +422,10 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
   const Plan& p = a.small;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
   const int dim = a.c.dim;
-  const int first = blockIdx.x * ATT_WAVES, worker = first + wave;
+  // (pairs of neighbouring blocks on one XCD: blocks go to the XCDs in turn)
+  const int block = (int)((blockIdx.x & ~15u) | (blockIdx.x & 7u) << 1 | (blockIdx.x >> 3 & 1u)), first = block * ATT_WAVES, worker = first + wave;
   find_starts<ATT_WAVES>(a, p, first, search, starts);
-  Walk w(a, p, starts[wave]);
+  Walk w(starts[wave]);
   __syncthreads();  // (the search's LDS is the values' from here on)
   T(*values)[PITCH] = sh.values[wave];
   Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
@@ -649,10 +652,10 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
   constexpr int PASS = ATT_THREADS / PER_ROW, PASSES = KEYS / PASS;
   const Plan& p = a.large;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int dim = a.c.dim, worker = worker_of(blockIdx.x, gridDim.x);
+  const int dim = a.c.dim, worker = blockIdx.x;
   find_starts<1>(a, p, worker, search, starts);
   if (tid < 3) spoiled[tid] = 0;
-  Walk w(a, p, starts[0]);
+  Walk w(starts[0]);
   __syncthreads();  // (the search's LDS is the tiles' from here on)
   Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
   const float c = a.s.scale * LOG2E;
@@ -888,7 +891,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void attention_kern
 // Blocks (w, 0 .. JOIN_BLOCKS - 1) for worker w, if its last piece begins an item: they
 // share its rows.  Groups of lanes take a row each, or, where an item has many pieces,
 // all of them one row, each every n-th piece.
-constexpr int JOIN_BLOCKS = 4;
+constexpr int JOIN_BLOCKS = 8;
 template <class T>
 __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int lanes) {
   __shared__ F4 sums[ATT_THREADS];
@@ -900,18 +903,18 @@ __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int 
   const Leaf* leaves = leaves_of(a);
   const Leaf leaf = leaves[worker];
   if (!leaf.last) return;
-  // the worker whose first piece ends the item
-  int last = worker + 1;
-  for (; last < p.workers; last += 64) {
-    const int i = last + (tid & 63);
-    const uint64_t votes = __ballot(i < p.workers && leaves[i].first == 2);
+  // up to the worker whose first piece ends the item
+  const int most = (p.workers - 1 - worker) / p.stride + 1;
+  int pieces = 1;
+  for (; pieces < most; pieces += 64) {
+    const int i = pieces + (tid & 63);
+    const uint64_t votes = __ballot(i < most && leaves[worker + i * p.stride].first == 2);
     if (votes) {
-      last += __builtin_ctzll(votes);
+      pieces += __builtin_ctzll(votes);
       break;
     }
   }
-  if (last >= p.workers) last = p.workers - 1;
-  const int pieces = last - worker + 1;
+  pieces = pieces < most ? pieces + 1 : most;
   const int groups = ATT_THREADS / lanes, group = tid / lanes, at = (tid - group * lanes) * 4;
   const int kv = leaf.head / p.groups, h0 = (leaf.head - kv * p.groups) * p.heads;
   const bool many = pieces > 2 * groups;
@@ -925,9 +928,9 @@ __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int 
     // (a piece that is all NaN has no maximum: its sums count as they are)
     auto weight = [](float x, float y, float top) { return x == NEG_INF ? (y != y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(x - top); };
     if (mine) {
-#pragma unroll 4
+#pragma unroll 8
       for (int i = many ? group : 0; i < pieces; i += many ? groups : 1) {
-        const float* piece = piece_of(a, p, worker + i, i ? 0 : 1);
+        const float* piece = piece_of(a, p, worker + i * p.stride, i ? 0 : 1);
         const float2 h = *reinterpret_cast<const float2*>(piece + (int64_t)p.rows * dim + 2 * row);
         const F4 x = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
         const float top = fmaxf(m, h.x), f = weight(m, sum, top), g = weight(h.x, h.y, top);
@@ -973,11 +976,14 @@ Plan plan_of(bool small, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   p.rows = small ? SMALL_ROWS : 128;
   p.keys = small ? 32 : 64;
   p.workers = BLOCKS / (dim > 128 ? 2 : 1) * (small ? ATT_WAVES : 1);
-  p.least = 4;
+  p.least = small ? 2 : 4;
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
   p.tokens = p.rows / p.heads;
   p.by_tokens = Quotient((uint32_t)p.tokens);
+  const int heads = kv_heads * p.groups;
+  p.stride = heads <= p.workers ? heads : 1;
+  p.parts = p.workers / p.stride;
   return p;
 }
 
