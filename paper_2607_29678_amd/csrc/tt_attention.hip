@@ -69,10 +69,8 @@ struct AttentionArgs {
 
 // What a worker leaves for the join.
 struct Leaf {
-  int32_t first;  // its first piece goes on an item that began before: 0 no, 1 and the item goes on, 2 and the item ends
-  int32_t last;   // its last piece begins an item that goes on behind it
+  int32_t pieces;              // of the item that its last piece begins and others go on; 0: none
   int32_t row0, tokens, head;  // that item's first row of queries, its tokens and its head unit
-  int32_t pad[3];
 };
 
 // The workspace: which path ran (256 bytes), a leaf for each worker, two pieces for each
@@ -129,6 +127,7 @@ struct Search {
 struct Start {
   int slot, request, head, unit, slots;
   int64_t count;  // units
+  int64_t size;   // units of every worker but the last ones
   Item item;
 };
 
@@ -245,7 +244,7 @@ __device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& 
       for (int e = 0; e < EACH; e++) {
         if (x >= 0 && x < units[e]) {
           const int64_t slot = slot0 + tid * each + e;
-          starts[w] = {(int)slot, requests[e], (int)head, (int)x, (int)slots, from + size < line ? size : line - from, item(slot, requests[e])};
+          starts[w] = {(int)slot, requests[e], (int)head, (int)x, (int)slots, from + size < line ? size : line - from, size, item(slot, requests[e])};
         }
         x -= units[e];
       }
@@ -256,11 +255,12 @@ __device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& 
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) { return ((int64_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x); }
 
 // A worker's walk through the items
 struct Walk {
   int slot, request, head, unit, slots;
-  int64_t left;
+  int64_t left, size;
   Item item;
   __device__ __forceinline__ void read(const AttentionArgs& a, const Plan& p) {
     const int raw1 = a.s.offsets[request + 1];
@@ -273,7 +273,7 @@ struct Walk {
   __device__ __forceinline__ explicit Walk(const Start& st)
       : slot(uniform(st.slot)), request(uniform(st.request)), head(uniform(st.head)), unit(uniform(st.unit)),
         slots(uniform(st.slots)),
-        left(((int64_t)uniform((int)(st.count >> 32)) << 32) | (uint32_t)uniform((int)st.count)) {
+        left(uniform(st.count)), size(uniform(st.size)) {
     take(st.item);
   }
   // to the next item that has units (there is one: left > 0; offsets that are not
@@ -428,7 +428,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
   Walk w(starts[wave]);
   __syncthreads();  // (the search's LDS is the values' from here on)
   T(*values)[PITCH] = sh.values[wave];
-  Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
+  Leaf leaf = {0, 0, 0, 0};
   const float c = a.s.scale * LOG2E;
   bool chunk[KK];
 #pragma unroll
@@ -616,10 +616,8 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
           }
         if (quad == 0) *reinterpret_cast<float2*>(piece + (int64_t)p.rows * dim + 2 * col) = float2{m, sum};
       }
-      if (began) {
-        leaf.first = ends ? 2 : 1;
-      } else {
-        leaf.last = 1;
+      if (!began) {
+        leaf.pieces = 1 + (int)divided(t.units - end + w.size - 1, w.size);
         leaf.row0 = t.row0;
         leaf.tokens = t.tokens;
         leaf.head = w.head;
@@ -657,7 +655,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
   if (tid < 3) spoiled[tid] = 0;
   Walk w(starts[0]);
   __syncthreads();  // (the search's LDS is the tiles' from here on)
-  Leaf leaf = {0, 0, 0, 0, 0, {0, 0, 0}};
+  Leaf leaf = {0, 0, 0, 0};
   const float c = a.s.scale * LOG2E;
   const int chunk = tid % PER_ROW, row_in = tid / PER_ROW;
   const bool loads = chunk * 8 < dim, stores = chunk * 8 < DP;
@@ -807,7 +805,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
             o[d] = product32(both<T>(transposed(from), transposed(from + 8 * V_PITCH)), weights[i], o[d]);
           }
         uint64_t bad = spoiled[third];
-        bad = ((uint64_t)uniform((int)(bad >> 32)) << 32) | (uint32_t)uniform((int)bad);
+        bad = (uint64_t)uniform((int64_t)bad);
         for (; bad; bad &= bad - 1) {
           const int key = k0 + __builtin_ctzll(bad);
           const int page = page_of(a, t, table, key);
@@ -856,10 +854,8 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
           }
         if (half == 0) *reinterpret_cast<float2*>(piece + (int64_t)p.rows * dim + 2 * row) = float2{m, sum};
       }
-      if (began) {
-        leaf.first = ends ? 2 : 1;
-      } else {
-        leaf.last = 1;
+      if (!began) {
+        leaf.pieces = 1 + (int)divided(t.units - end + w.size - 1, w.size);
         leaf.row0 = t.row0;
         leaf.tokens = t.tokens;
         leaf.head = w.head;
@@ -888,81 +884,105 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void attention_kern
 
 // ---- joins the pieces of items that several workers have ----------------------------
 
-// Blocks (w, 0 .. JOIN_BLOCKS - 1) for worker w, if its last piece begins an item: they
-// share its rows.  Groups of lanes take a row each, or, where an item has many pieces,
-// all of them one row, each every n-th piece.
-constexpr int JOIN_BLOCKS = 8;
+// A block looks after every 256th worker (neighbours begin items together); the blocks of one x share the rows of the
+// items that these begin and others go on.  Groups of lanes take a row each, or, where
+// an item has many pieces, all of them one row, each every n-th piece.
+constexpr int JOIN_X = 256, JOIN_Y = 8, JOIN_MOST = 2048 / JOIN_X;
 template <class T>
 __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int lanes) {
   __shared__ F4 sums[ATT_THREADS];
   __shared__ float2 heads[ATT_THREADS];
+  // (a dependent load takes a microsecond or two here: the leaves come with the word
+  // that says how many there are)
+  int32_t counts[JOIN_MOST];
+#pragma unroll
+  for (int i = 0; i < JOIN_MOST; i++) counts[i] = leaves_of(a)[min((int)blockIdx.x + i * JOIN_X, a.small.workers - 1)].pieces;
   const bool small = *reinterpret_cast<const int32_t*>(a.parts) != 0;
   const Plan& p = small ? a.small : a.large;
-  const int tid = threadIdx.x, worker = blockIdx.x, dim = a.c.dim;
-  if (worker >= p.workers) return;
-  const Leaf* leaves = leaves_of(a);
-  const Leaf leaf = leaves[worker];
-  if (!leaf.last) return;
-  // up to the worker whose first piece ends the item
-  const int most = (p.workers - 1 - worker) / p.stride + 1;
-  int pieces = 1;
-  for (; pieces < most; pieces += 64) {
-    const int i = pieces + (tid & 63);
-    const uint64_t votes = __ballot(i < most && leaves[worker + i * p.stride].first == 2);
-    if (votes) {
-      pieces += __builtin_ctzll(votes);
-      break;
-    }
-  }
-  pieces = pieces < most ? pieces + 1 : most;
+  const int tid = threadIdx.x, dim = a.c.dim, each = p.workers / JOIN_X;
   const int groups = ATT_THREADS / lanes, group = tid / lanes, at = (tid - group * lanes) * 4;
-  const int kv = leaf.head / p.groups, h0 = (leaf.head - kv * p.groups) * p.heads;
-  const bool many = pieces > 2 * groups;
-  const int rows = leaf.tokens * p.heads, share = many ? 1 : groups;  // rows at a time
-  for (int row0 = blockIdx.y * share; row0 < rows; row0 += JOIN_BLOCKS * share) {
-    const int row = many ? row0 : row0 + group;
-    const int token = row / p.heads, head = row - token * p.heads;
-    const bool mine = row < rows && head < a.per_kv - h0 && at < dim;
-    float m = NEG_INF, sum = 0.f;
-    F4 o = {0.f, 0.f, 0.f, 0.f};
-    // (a piece that is all NaN has no maximum: its sums count as they are)
-    auto weight = [](float x, float y, float top) { return x == NEG_INF ? (y != y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(x - top); };
-    if (mine) {
-#pragma unroll 8
-      for (int i = many ? group : 0; i < pieces; i += many ? groups : 1) {
-        const float* piece = piece_of(a, p, worker + i * p.stride, i ? 0 : 1);
-        const float2 h = *reinterpret_cast<const float2*>(piece + (int64_t)p.rows * dim + 2 * row);
-        const F4 x = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
-        const float top = fmaxf(m, h.x), f = weight(m, sum, top), g = weight(h.x, h.y, top);
-        sum = sum * f + h.y * g;
-        o = o * f + x * g;
+  int turn = 0;  // tasks before this item's
+  // (a piece that is all NaN has no maximum: its sums count as they are)
+  auto weight = [](float x, float y, float top) { return x == NEG_INF ? (y != y ? 1.f : 0.f) : __builtin_amdgcn_exp2f(x - top); };
+  for (int k = 0; k < each; k++) {
+    int pieces = counts[0];
+#pragma unroll
+    for (int i = 1; i < JOIN_MOST; i++) pieces = i == k ? counts[i] : pieces;
+    if (!pieces) continue;
+    const int worker = blockIdx.x + k * JOIN_X, most = (p.workers - 1 - worker) / p.stride + 1;
+    if (pieces > most) pieces = most;
+    const Leaf leaf = leaves_of(a)[worker];
+    const int kv = leaf.head / p.groups, h0 = (leaf.head - kv * p.groups) * p.heads;
+    const bool many = pieces > 2 * groups;
+    const int rows = leaf.tokens * p.heads, share = many ? 1 : groups;  // rows at a time
+    const int tasks = (rows + share - 1) / share;
+    for (int task = (int)((blockIdx.y + JOIN_Y - turn % JOIN_Y) % JOIN_Y); task < tasks; task += JOIN_Y) {
+      const int row = many ? task : task * share + group;
+      const int token = row / p.heads, head = row - token * p.heads;
+      const bool mine = row < rows && head < a.per_kv - h0 && at < dim;
+      float m = NEG_INF, sum = 0.f;
+      F4 o = {0.f, 0.f, 0.f, 0.f};
+      auto add = [&](auto ahead, int begin, int step) {
+        constexpr int AHEAD = decltype(ahead)::value;  // pieces under way at once
+        for (int i0 = begin; i0 < pieces; i0 += AHEAD * step) {
+          float2 h[AHEAD];
+          F4 x[AHEAD];
+#pragma unroll
+          for (int u = 0; u < AHEAD; u++) {
+            const int i = i0 + u * step;
+            h[u] = float2{NEG_INF, 0.f};
+            x[u] = F4{0.f, 0.f, 0.f, 0.f};
+            if (i < pieces) {
+              const float* piece = piece_of(a, p, worker + i * p.stride, i ? 0 : 1);
+              h[u] = *reinterpret_cast<const float2*>(piece + (int64_t)p.rows * dim + 2 * row);
+              x[u] = *reinterpret_cast<const F4*>(piece + (int64_t)row * dim + at);
+            }
+          }
+          float top = m;
+#pragma unroll
+          for (int u = 0; u < AHEAD; u++) top = fmaxf(top, h[u].x);
+          const float f = weight(m, sum, top);
+          sum *= f;
+          o *= f;
+#pragma unroll
+          for (int u = 0; u < AHEAD; u++) {
+            const float g = weight(h[u].x, h[u].y, top);
+            sum += h[u].y * g;
+            o += x[u] * g;
+          }
+          m = top;
+        }
+      };
+      if (mine) {
+        if (many) add(std::integral_constant<int, 16>{}, group, groups);
+        else add(std::integral_constant<int, 4>{}, 0, 1);
+      }
+      if (many) {
+        __syncthreads();
+        sums[tid] = o;
+        heads[tid] = float2{m, sum};
+        __syncthreads();
+        if (group != 0 || !mine) continue;
+        float top = m;
+        for (int g = 1; g < groups; g++) top = fmaxf(top, heads[g * lanes + tid].x);
+        o = F4{0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        for (int g = 0; g < groups; g++) {
+          const float2 h = heads[g * lanes + tid];
+          const float f = weight(h.x, h.y, top);
+          sum += h.y * f;
+          o += sums[g * lanes + tid] * f;
+        }
         m = top;
       }
+      if (!mine) continue;
+      const bool none = m == NEG_INF && sum == 0.f;
+      const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
+      const float x[4] = {o[0], o[1], o[2], o[3]};
+      store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);
+      if (a.s.logsums && at == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
     }
-    if (many) {
-      __syncthreads();
-      sums[tid] = o;
-      heads[tid] = float2{m, sum};
-      __syncthreads();
-      if (group != 0 || !mine) continue;
-      float top = m;
-      for (int g = 1; g < groups; g++) top = fmaxf(top, heads[g * lanes + tid].x);
-      o = F4{0.f, 0.f, 0.f, 0.f};
-      sum = 0.f;
-      for (int g = 0; g < groups; g++) {
-        const float2 h = heads[g * lanes + tid];
-        const float f = weight(h.x, h.y, top);
-        sum += h.y * f;
-        o += sums[g * lanes + tid] * f;
-      }
-      m = top;
-    }
-    if (!mine) continue;
-    const bool none = m == NEG_INF && sum == 0.f;
-    const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
-    const float x[4] = {o[0], o[1], o[2], o[3]};
-    store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);
-    if (a.s.logsums && at == 0) a.s.logsums[q_row * a.s.q_heads + q_head] = none ? NEG_INF : (m == NEG_INF ? 0.f : m) * LN2 + logf(sum);
+    turn += tasks;
   }
 }
 
@@ -996,7 +1016,7 @@ int run_attention(const AttentionArgs& a, hipStream_t st) {
   while (lanes * 4 < a.c.dim) lanes *= 2;
   auto* kernel = kk <= 2 ? attention_kernel<T, 64> : kk == 3 ? attention_kernel<T, 96> : kk == 4 ? attention_kernel<T, 128> : attention_kernel<T, 256>;
   if (launch(kernel, dim3(a.large.workers), dim3(ATT_THREADS), st, a) != hipSuccess) return TT_ERR_HIP;
-  return launch(join_kernel<T>, dim3(a.small.workers, JOIN_BLOCKS), dim3(ATT_THREADS), st, a, lanes) == hipSuccess ? TT_OK : TT_ERR_HIP;
+  return launch(join_kernel<T>, dim3(JOIN_X, JOIN_Y), dim3(ATT_THREADS), st, a, lanes) == hipSuccess ? TT_OK : TT_ERR_HIP;
 }
 
 }  // namespace
