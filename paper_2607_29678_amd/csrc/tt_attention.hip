@@ -62,6 +62,7 @@ struct AttentionArgs {
   int capacity;  // tokens that a request's table has room for (at most 2^31 - 65)
   Plan small, large;
   Quotient by_page;
+  uint32_t page_step, slot_step;  // strides in vectors of 8 elements
   int per_kv;      // query heads of a key head
   bool vectors;    // queries and out are aligned to 16 bytes
   uint8_t* parts;  // workspace
@@ -391,16 +392,21 @@ __device__ __forceinline__ bool needed(const Item& t, int key) { return key <= t
 __device__ __forceinline__ int first_key(const Item& t, int unit, int keys) {
   return (unit < t.front_units ? unit : t.begin_unit + unit - t.front_units) * keys;
 }
-// Page of a key's token: -1 where there is none, -2 where no token of the item sees it
-__device__ __forceinline__ int page_of(const AttentionArgs& a, const Item& t, const int32_t* table, int key) {
-  if (!needed(t, key)) return -2;
+// Where a key's token is: its page (-1: there is none, -2: no token of the item sees
+// it), and its place in the page
+struct Place {
+  int page, slot;
+};
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, const Item& t, const int32_t* table, int key) {
   const int entry = a.by_page.of(key);
-  const int page = entry < a.s.table_width ? table[entry] : -1;
-  return page >= 0 && page < a.c.pages ? page : -1;
+  Place x = {-2, key - entry * (int)a.by_page.d};
+  if (needed(t, key)) x.page = entry < a.s.table_width ? table[entry] : -1;
+  return x;
 }
-__device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, int page, int key, int64_t head) {
-  const int entry = a.by_page.of(key);
-  return page * a.c.page_stride + (key - entry * (int)a.by_page.d) * a.c.slot_stride + head;
+__device__ __forceinline__ bool is_page(const AttentionArgs& a, int page) { return (uint32_t)page < (uint32_t)a.c.pages; }
+// (strides in vectors of 8 elements: products of 32 bits by 32)
+__device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, const Place& x, int64_t head) {
+  return (int64_t)(((uint64_t)(uint32_t)x.page * a.page_step + (uint64_t)(uint32_t)x.slot * a.slot_step) * 8) + head;
 }
 
 // A running maximum goes up only where it has to by more than this (in powers of two)
@@ -455,24 +461,24 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
     const int64_t head = (int64_t)kv * a.c.head_stride + quad * 8;
     const T *K = static_cast<const T*>(a.c.keys), *V = static_cast<const T*>(a.c.values);
     Vec8<T> k[2][KK], v[2][KK];
-    int pages[2];
-    auto fetch_pages = [&](int unit) {
+    Place places[2];
+    auto fetch_places = [&](int unit) {
       const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
-      for (int i = 0; i < 2; i++) pages[i] = page_of(a, t, table, k0 + 16 * i + col);
+      for (int i = 0; i < 2; i++) places[i] = place_of(a, t, table, k0 + 16 * i + col);
     };
-    auto fetch = [&](int unit) {
-      const int k0 = first_key(t, unit, KEYS);
+    auto fetch = [&] {
 #pragma unroll
       for (int i = 0; i < 2; i++) {
-        const int64_t at = vector_at(a, pages[i], k0 + 16 * i + col, head);
+        const int64_t at = vector_at(a, places[i], head);
+        const bool there = is_page(a, places[i].page);
 #pragma unroll
         for (int kk = 0; kk < KK; kk++) {
-          if (pages[i] >= 0 && chunk[kk]) {
+          if (there && chunk[kk]) {
             k[i][kk] = *reinterpret_cast<const Vec8<T>*>(K + at + kk * 32);
             v[i][kk] = *reinterpret_cast<const Vec8<T>*>(V + at + kk * 32);
           } else {
-            k[i][kk] = pages[i] == -1 ? nan8<T>() : zero8<T>();
+            k[i][kk] = !there && places[i].page != -2 ? nan8<T>() : zero8<T>();
             v[i][kk] = zero8<T>();
           }
         }
@@ -483,9 +489,9 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
     for (int d = 0; d < DT; d++) o[d] = F4{0.f, 0.f, 0.f, 0.f};
     float m = NEG_INF, sum = 0.f;
     const int end = w.unit + take;
-    fetch_pages(w.unit);
-    fetch(w.unit);
-    if (w.unit + 1 < end) fetch_pages(w.unit + 1);
+    fetch_places(w.unit);
+    fetch();
+    if (w.unit + 1 < end) fetch_places(w.unit + 1);
     for (int unit = w.unit; unit < end; unit++) {
       const int k0 = first_key(t, unit, KEYS);
       const bool edge = !all_seen(a, t, k0, KEYS);
@@ -508,11 +514,6 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
           spoiled[i] = (votes | votes >> 16) & 0xFFFF;
         }
       }
-      int64_t at_now[2] = {0, 0};
-      if (spoiled[0] | spoiled[1]) {
-#pragma unroll
-        for (int i = 0; i < 2; i++) at_now[i] = page_of(a, t, table, k0 + 16 * i + col);
-      }
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int i = 0; i < 2; i++)
@@ -526,8 +527,8 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
         for (int kk = 0; kk < KK; kk++) s[i] = product16(k[i][kk], q[kk], s[i]);
       }
       if (unit + 1 < end) {
-        fetch(unit + 1);
-        if (unit + 2 < end) fetch_pages(unit + 2);
+        fetch();
+        if (unit + 2 < end) fetch_places(unit + 2);
       }
       if (edge) {
         const uint32_t seen = (uint32_t)seen_bits(a, position, k0, KEYS) >> (quad * 4);
@@ -574,10 +575,9 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
       if (spoiled[0] | spoiled[1]) {
         for (int j = 0; j < 32; j++) {
           if (!(spoiled[j >> 4] >> (j & 15) & 1)) continue;
-          const int page = __shfl((int)at_now[j >> 4], j & 15);
-          if (page < 0) continue;
-          const T* value = V + vector_at(a, page, k0 + j, (int64_t)kv * a.c.head_stride);
-          if (!sees(a, position, k0 + j)) continue;
+          const Place x = place_of(a, t, table, k0 + j);
+          if (!is_page(a, x.page) || !sees(a, position, k0 + j)) continue;
+          const T* value = V + vector_at(a, x, (int64_t)kv * a.c.head_stride);
 #pragma unroll
           for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -631,36 +631,57 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
 
 // ---- 128 rows a block: prompts ---------------------------------------------------
 
-// Four waves of 32 rows share tiles of 64 keys and values in LDS, two of each, so
-// that one barrier a unit is enough: the next unit's come from memory to registers
-// during a unit's products and are written where the last unit's were.
+// Four waves of 32 rows share tiles of 64 keys and values in LDS, two of each: the
+// next unit's come straight from memory during a unit's products, so that one barrier
+// a unit is enough and no registers wait for them.  A load writes 1 KB as it comes,
+// so rows stand without gaps, and the vectors of 16 bytes trade places in their row
+// instead (key_place, value_place): rows that are read at once lie in other banks.
 template <class T, int DP>  // DP: elements of a head, with zeros behind its own
 struct LargeShared {
-  static constexpr int KEYS = 64;
-  static constexpr int K_PITCH = DP + 8;                   // (16 rows 16 bytes apart in the banks)
-  static constexpr int V_PITCH = DP == 96 ? DP : DP + 32;  // (4 rows 64 bytes apart)
-  T keys[2][KEYS][K_PITCH];
-  T values[2][KEYS][V_PITCH];
+  static constexpr int KEYS = 64, PER_ROW = DP == 64 ? 8 : DP == 256 ? 32 : 16;  // vectors of a row
+  Vec8<T> keys[2][KEYS][PER_ROW];
+  Vec8<T> values[2][KEYS][PER_ROW];
+  // a read of keys takes one vector of 16 rows at a time, one of values four of 4 rows
+  static __device__ __forceinline__ int key_place(int row) { return PER_ROW == 8 ? row >> 1 & 7 : PER_ROW == 16 ? row & 15 : row & 7; }
+  static __device__ __forceinline__ int value_place(int row) { return PER_ROW == 8 ? (row >> 1 & 1) << 2 : (row & 3) << 2; }
 };
+// 16 bytes a lane from memory to LDS, at `to` + 16 lane.  Written as assembly, since
+// for the builtin the compiler makes every later read of LDS wait for the load; there
+// is no result register.  It takes a wait state from the write of m0 to its use.
+template <class T>
+__device__ __forceinline__ void load_to_lds(const T* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "m0", "memory");
+}
+// Waits for this wave's loads and LDS accesses, then for the block's other waves.
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 template <class T, int DP>
 __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& search, LargeShared<T, DP>& sh, Start* starts,
                                            unsigned long long* spoiled) {
-  constexpr int KEYS = 64, KK = DP / 16, DT = DP / 32, K_PITCH = LargeShared<T, DP>::K_PITCH, V_PITCH = LargeShared<T, DP>::V_PITCH;
-  constexpr int PER_ROW = DP == 64 ? 8 : DP == 256 ? 32 : 16;      // threads that fetch a row
+  using Shared = LargeShared<T, DP>;
+  constexpr int KEYS = 64, KK = DP / 16, DT = DP / 32, PER_ROW = Shared::PER_ROW;
   constexpr int PASS = ATT_THREADS / PER_ROW, PASSES = KEYS / PASS;
   const Plan& p = a.large;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
   const int dim = a.c.dim, worker = blockIdx.x;
   find_starts<1>(a, p, worker, search, starts);
-  if (tid < 3) spoiled[tid] = 0;
   Walk w(starts[0]);
   __syncthreads();  // (the search's LDS is the tiles' from here on)
+  // what lies behind a head's elements is not loaded: zeros, once
+  for (int i = tid; i < (int)(sizeof(sh.keys) / 16); i += ATT_THREADS) (&sh.keys[0][0][0])[i] = zero8<T>();
+  __syncthreads();
   Leaf leaf = {0, 0, 0, 0};
   const float c = a.s.scale * LOG2E;
-  const int chunk = tid % PER_ROW, row_in = tid / PER_ROW;
-  const bool loads = chunk * 8 < dim, stores = chunk * 8 < DP;
+  // the vector that this thread loads: its place in LDS, and which one of keys and values comes there
+  const int place = tid % PER_ROW, row_in = tid / PER_ROW;
+  const int k_vec = place ^ Shared::key_place(row_in), v_vec = place ^ Shared::value_place(row_in);
+  const bool k_loads = k_vec * 8 < dim, v_loads = v_vec * 8 < dim;
+  const uint32_t wave_at = uniform((int)((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&sh.keys[0][0][0])) + wave * 1024;
+  constexpr uint32_t STAGE = KEYS * PER_ROW * 16;  // bytes of a tile; the values' two follow the keys' two
+  // a lane's places in the tiles
+  const int k_in = half ^ Shared::key_place(col), v_row = 4 * half + ((lane & 15) >> 2);
+  const int v_in = ((lane >> 4 & 1) * 2 + ((lane & 3) >> 1)) ^ Shared::value_place(v_row);
   const T *K = static_cast<const T*>(a.c.keys), *V = static_cast<const T*>(a.c.values);
-  int turn = 0, third = 0;  // tiles, and word of spoiled keys, of the present unit
+  int turn = 0;  // tiles of the present unit
 
   while (w.left > 0) {
     const Item& t = w.item;
@@ -683,48 +704,24 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
         q[kk] = load8(static_cast<const T*>(a.s.queries) + q_row * a.s.query_stride + q_head * dim + kk * 16 + half * 8, a.vectors);
     }
     const int32_t* table = a.s.tables + w.request * a.s.table_stride;
-    const int64_t head = (int64_t)kv * a.c.head_stride + chunk * 8;
-    Vec8<T> k[PASSES], v[PASSES];
-    int pages[PASSES];
-    auto fetch_pages = [&](int unit) {
+    const int64_t head = (int64_t)kv * a.c.head_stride;
+    Place places[PASSES];
+    auto fetch_places = [&](int unit) {
       const int k0 = first_key(t, unit, KEYS);
 #pragma unroll
-      for (int i = 0; i < PASSES; i++) pages[i] = page_of(a, t, table, k0 + PASS * i + row_in);
+      for (int i = 0; i < PASSES; i++) places[i] = place_of(a, t, table, k0 + PASS * i + row_in);
     };
-    auto fetch = [&](int unit) {
-      const int k0 = first_key(t, unit, KEYS);
+    auto fetch = [&](int to) {
 #pragma unroll
       for (int i = 0; i < PASSES; i++) {
-        const int64_t at = vector_at(a, pages[i], k0 + PASS * i + row_in, head);
-        if (pages[i] >= 0 && loads) {
-          k[i] = *reinterpret_cast<const Vec8<T>*>(K + at);
-          v[i] = *reinterpret_cast<const Vec8<T>*>(V + at);
-        } else {
-          k[i] = pages[i] == -1 && loads ? nan8<T>() : zero8<T>();
-          v[i] = zero8<T>();
-        }
-      }
-    };
-    // registers to the tiles of `to`; values of keys that only some tokens see must
-    // not reach the others through 0 * NaN
-    auto put = [&](int unit, int to, int word) {
-      if (t.tokens > 1 && !all_seen(a, t, first_key(t, unit, KEYS), KEYS)) {
-#pragma unroll
-        for (int i = 0; i < PASSES; i++) {
-          const uint32_t bad = not_finite(v[i]);
-          if (bad) {
-            atomicOr(&spoiled[word], 1ull << (PASS * i + row_in));
-#pragma unroll
-            for (int e = 0; e < 8; e++)
-              if (bad >> e & 1) v[i][e] = (T)0.f;
-          }
-        }
-      }
-      if (stores) {
-#pragma unroll
-        for (int i = 0; i < PASSES; i++) {
-          *reinterpret_cast<Vec8<T>*>(&sh.keys[to][PASS * i + row_in][chunk * 8]) = k[i];
-          *reinterpret_cast<Vec8<T>*>(&sh.values[to][PASS * i + row_in][chunk * 8]) = v[i];
+        const int64_t at = vector_at(a, places[i], head);
+        const bool there = is_page(a, places[i].page);
+        const uint32_t lds = wave_at + to * STAGE + i * (PASS * PER_ROW * 16);
+        if (there && k_loads) load_to_lds(K + at + k_vec * 8, lds);
+        if (there && v_loads) load_to_lds(V + at + v_vec * 8, lds + 2 * STAGE);
+        if (!there) {
+          if (k_loads) sh.keys[to][PASS * i + row_in][place] = places[i].page != -2 ? nan8<T>() : zero8<T>();
+          if (v_loads) sh.values[to][PASS * i + row_in][place] = zero8<T>();
         }
       }
     };
@@ -735,33 +732,49 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
       for (int e = 0; e < 16; e++) o[d][e] = 0.f;
     float m = NEG_INF, sum = 0.f;
     const int end = w.unit + take;
-    fetch_pages(w.unit);
-    fetch(w.unit);
-    if (w.unit + 1 < end) fetch_pages(w.unit + 1);
-    put(w.unit, turn, third);
+    fetch_places(w.unit);
+    fetch(turn);
+    if (w.unit + 1 < end) fetch_places(w.unit + 1);
     for (int unit = w.unit; unit < end; unit++) {
-      const int after = third == 2 ? 0 : third + 1;
-      __syncthreads();
-      if (tid == 0) spoiled[after == 2 ? 0 : after + 1] = 0;  // (read in the last unit, written in the next one)
+      loads_done();
       if (unit + 1 < end) {
-        fetch(unit + 1);
-        if (unit + 2 < end) fetch_pages(unit + 2);
+        fetch(turn ^ 1);
+        if (unit + 2 < end) fetch_places(unit + 2);
       }
       const int k0 = first_key(t, unit, KEYS);
       const int64_t begin_low = a.s.window ? (int64_t)low - a.s.window + 1 : 0, begin_high = a.s.window ? (int64_t)high - a.s.window + 1 : 0;
+      // values of keys that only some tokens see must not reach the others through 0 * NaN:
+      // they are 0 in the product and added to those who see them
+      uint64_t bad = 0;
+      if (t.tokens > 1 && !all_seen(a, t, k0, KEYS)) {
+        if (tid == 0) *spoiled = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PASSES; i++) {
+          Vec8<T> v = sh.values[turn][PASS * i + row_in][place];
+          const uint32_t bits = v_loads ? not_finite(v) : 0;
+          if (bits) {
+            atomicOr(spoiled, 1ull << (PASS * i + row_in));
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              if (bits >> e & 1) v[e] = (T)0.f;
+            sh.values[turn][PASS * i + row_in][place] = v;
+          }
+        }
+        __syncthreads();
+        bad = (uint64_t)uniform((int64_t)*spoiled);
+      }
       const bool any = wave_rows > 0 && k0 <= high && (k0 + KEYS > begin_low || k0 < a.s.sinks || begin_low > a.capacity);
       if (any) {
-        const T(*keys)[K_PITCH] = sh.keys[turn];
-        const T(*values)[V_PITCH] = sh.values[turn];
         F16 s[2];
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
+        for (int i = 0; i < 2; i++)
 #pragma unroll
           for (int e = 0; e < 16; e++) s[i][e] = 0.f;
 #pragma unroll
-          for (int kk = 0; kk < KK; kk++)
-            s[i] = product32(*reinterpret_cast<const Vec8<T>*>(&keys[32 * i + col][kk * 16 + half * 8]), q[kk], s[i]);
-        }
+        for (int kk = 0; kk < KK; kk++)
+#pragma unroll
+          for (int i = 0; i < 2; i++) s[i] = product32(sh.keys[turn][32 * i + col][(2 * kk) ^ k_in], q[kk], s[i]);
         const bool whole = k0 + KEYS <= t.last + 1 && k0 + KEYS - 1 <= low && (k0 >= begin_high || k0 + KEYS <= a.s.sinks);
         if (!whole) {
           const uint64_t seen = seen_bits(a, position, k0, KEYS) >> (4 * half);
@@ -798,19 +811,17 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
             weights[i][e] = (T)x;
           }
 #pragma unroll
-        for (int d = 0; d < DT; d++)
+        for (int i = 0; i < 4; i++)
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const T* from = &values[16 * i + 4 * half + ((lane & 15) >> 2)][d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4];
-            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * V_PITCH)), weights[i], o[d]);
+          for (int d = 0; d < DT; d++) {
+            const T* from = reinterpret_cast<const T*>(&sh.values[turn][16 * i + v_row][(4 * d) ^ v_in]) + (lane & 1) * 4;
+            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * PER_ROW * 8)), weights[i], o[d]);
           }
-        uint64_t bad = spoiled[third];
-        bad = (uint64_t)uniform((int64_t)bad);
         for (; bad; bad &= bad - 1) {
           const int key = k0 + __builtin_ctzll(bad);
-          const int page = page_of(a, t, table, key);
-          if (page < 0 || !sees(a, position, key)) continue;
-          const T* value = V + vector_at(a, page, key, (int64_t)kv * a.c.head_stride) + 4 * half;
+          const Place x = place_of(a, t, table, key);
+          if (!is_page(a, x.page) || !sees(a, position, key)) continue;
+          const T* value = V + vector_at(a, x, head) + 4 * half;
 #pragma unroll
           for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -822,9 +833,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
             }
         }
       }
-      if (unit + 1 < end) put(unit + 1, turn ^ 1, after);
       turn ^= 1;
-      third = after;
     }
     sum += __shfl_xor(sum, 32);
     const bool began = w.unit > 0, ends = end == t.units;
@@ -875,11 +884,11 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void attention_kern
     LargeShared<T, DP> large;
   } sh;
   __shared__ Start starts[ATT_WAVES];
-  __shared__ unsigned long long spoiled[3];
+  __shared__ unsigned long long spoiled;
   const bool small = few_rows(a, sh.search);
   if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<int32_t*>(a.parts) = small;
   if (small) small_path<T, DP / 32>(a, sh.search, sh.small, starts);
-  else large_path<T, DP>(a, sh.search, sh.large, starts, spoiled);
+  else large_path<T, DP>(a, sh.search, sh.large, starts, &spoiled);
 }
 
 // ---- joins the pieces of items that several workers have ----------------------------
@@ -1050,7 +1059,8 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
   if (bad) return bad;
   if (!s.offsets || !s.lengths || (s.table_width > 0 && !s.tables) || !s.queries || !s.out || !workspace) return TT_ERR_NULL_ARG;
   // slots of items are numbered in 32 bits
-  if (s.tokens + s.n_requests > INT32_MAX) return TT_ERR_TOO_LARGE;
+  if (s.tokens + s.n_requests > INT32_MAX || cache->page_stride / 8 > UINT32_MAX || cache->slot_stride / 8 > UINT32_MAX)
+    return TT_ERR_TOO_LARGE;
   auto in_vectors = [](const void* p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; };
   const int64_t capacity = (int64_t)s.table_width * cache->page_size;
   const AttentionArgs a{*cache,
@@ -1059,6 +1069,8 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
                   plan_of(true, s.q_heads, cache->kv_heads, cache->dim),
                   plan_of(false, s.q_heads, cache->kv_heads, cache->dim),
                   Quotient((uint32_t)cache->page_size),
+                  (uint32_t)(cache->page_stride / 8),
+                  (uint32_t)(cache->slot_stride / 8),
                   s.q_heads / cache->kv_heads,
                   in_vectors(s.queries, s.query_stride) && in_vectors(s.out, s.out_stride),
                   static_cast<uint8_t*>(workspace)};
