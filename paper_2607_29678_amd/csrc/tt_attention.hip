@@ -345,6 +345,18 @@ __device__ __forceinline__ void store4(T* p, const float* x, float f, bool vecto
   }
 }
 
+// Adds what is not finite of four values to o[at], ... (the empty statement keeps the
+// loads of several calls apart: registers are for the products)
+template <class T, class F>
+__device__ __forceinline__ void add_not_finite(const T* value, bool there, F* o, int at) {
+  using T4 = T __attribute__((ext_vector_type(4)));
+  if (there) {
+    const T4 x = *reinterpret_cast<const T4*>(value);
+#pragma unroll
+    for (int i = 0; i < 4; i++) (*o)[at + i] += fabsf((float)x[i]) < __builtin_inff() ? 0.f : (float)x[i];
+  }
+  asm volatile("" ::: "memory");
+}
 using F4 = float __attribute__((ext_vector_type(4)));
 using F16 = float __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ F4 product16(Vec8<bf16_t> a, Vec8<bf16_t> b, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -579,14 +591,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
           if (!is_page(a, x.page) || !sees(a, position, k0 + j)) continue;
           const T* value = V + vector_at(a, x, (int64_t)kv * a.c.head_stride);
 #pragma unroll
-          for (int d = 0; d < DT; d++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              const int at = d * 16 + quad * 4 + e;
-              const float x = at < dim ? (float)value[at] : 0.f;
-              o[d][e] += fabsf(x) < __builtin_inff() ? 0.f : x;
-              if (e == 3) __builtin_amdgcn_sched_barrier(0);  // (few loads at a time: registers are for the products)
-            }
+          for (int d = 0; d < DT; d++) add_not_finite(value + d * 16 + quad * 4, d * 16 + quad * 4 < dim, &o[d], 0);
         }
       }
     }
@@ -771,10 +776,30 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
         for (int i = 0; i < 2; i++)
 #pragma unroll
           for (int e = 0; e < 16; e++) s[i][e] = 0.f;
+        // Reads stay a group of products ahead (of its own accord the compiler reads
+        // right before each product and waits): two steps of keys, then four tiles of values.
+        Vec8<T> k[2][4], v[2][DT];
+        auto read_keys = [&](int kk, Vec8<T>* to) {
 #pragma unroll
-        for (int kk = 0; kk < KK; kk++)
+          for (int i = 0; i < 4; i++) to[i] = sh.keys[turn][32 * (i & 1) + col][(2 * (kk + (i >> 1))) ^ k_in];
+        };
+        auto read_values = [&](int i, Vec8<T>* to) {
 #pragma unroll
-          for (int i = 0; i < 2; i++) s[i] = product32(sh.keys[turn][32 * i + col][(2 * kk) ^ k_in], q[kk], s[i]);
+          for (int d = 0; d < DT; d++) {
+            const T* from = reinterpret_cast<const T*>(&sh.values[turn][16 * i + v_row][(4 * d) ^ v_in]) + (lane & 1) * 4;
+            to[d] = both<T>(transposed(from), transposed(from + 8 * PER_ROW * 8));
+          }
+        };
+        read_keys(0, k[0]);
+#pragma unroll
+        for (int kk = 0; kk < KK; kk += 2) {
+          if (kk + 2 < KK) read_keys(kk + 2, k[(kk / 2 + 1) & 1]);
+          else read_values(0, v[0]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < 4; i++) s[i & 1] = product32(k[kk / 2 & 1][i], q[kk + (i >> 1)], s[i & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         const bool whole = k0 + KEYS <= t.last + 1 && k0 + KEYS - 1 <= low && (k0 >= begin_high || k0 + KEYS <= a.s.sinks);
         if (!whole) {
           const uint64_t seen = seen_bits(a, position, k0, KEYS) >> (4 * half);
@@ -811,12 +836,13 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
             weights[i][e] = (T)x;
           }
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int i = 0; i < 4; i++) {
+          if (i < 3) read_values(i + 1, v[(i + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int d = 0; d < DT; d++) {
-            const T* from = reinterpret_cast<const T*>(&sh.values[turn][16 * i + v_row][(4 * d) ^ v_in]) + (lane & 1) * 4;
-            o[d] = product32(both<T>(transposed(from), transposed(from + 8 * PER_ROW * 8)), weights[i], o[d]);
-          }
+          for (int d = 0; d < DT; d++) o[d] = product32(v[i & 1][d], weights[i], o[d]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         for (; bad; bad &= bad - 1) {
           const int key = k0 + __builtin_ctzll(bad);
           const Place x = place_of(a, t, table, key);
@@ -825,12 +851,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
 #pragma unroll
           for (int d = 0; d < DT; d++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-              const int at = d * 32 + 8 * (e / 4) + e % 4;
-              const float x = at + 4 * half < dim ? (float)value[at] : 0.f;
-              o[d][e] += fabsf(x) < __builtin_inff() ? 0.f : x;
-              if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (few loads at a time: registers are for the products)
-            }
+            for (int e = 0; e < 16; e += 4) add_not_finite(value + d * 32 + 2 * e, d * 32 + 2 * e + 4 * half < dim, &o[d], e);
         }
       }
       turn ^= 1;
