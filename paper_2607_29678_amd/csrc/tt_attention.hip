@@ -710,22 +710,18 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
     }
     const int32_t* table = a.s.tables + w.request * a.s.table_stride;
     const int64_t head = (int64_t)kv * a.c.head_stride;
-    Place places[PASSES];
-    auto fetch_places = [&](int unit) {
-      const int k0 = first_key(t, unit, KEYS);
-#pragma unroll
-      for (int i = 0; i < PASSES; i++) places[i] = place_of(a, t, table, k0 + PASS * i + row_in);
-    };
+    Place mine;  // of the key whose number in the unit is the lane's
+    auto fetch_places = [&](int unit) { mine = place_of(a, t, table, first_key(t, unit, KEYS) + lane); };
     auto fetch = [&](int to) {
+      const int64_t at_mine = is_page(a, mine.page) ? vector_at(a, mine, head) : mine.page == -2 ? -2 : -1;
 #pragma unroll
       for (int i = 0; i < PASSES; i++) {
-        const int64_t at = vector_at(a, places[i], head);
-        const bool there = is_page(a, places[i].page);
+        const int64_t at = __shfl((long long)at_mine, PASS * i + row_in);
         const uint32_t lds = wave_at + to * STAGE + i * (PASS * PER_ROW * 16);
-        if (there && k_loads) load_to_lds(K + at + k_vec * 8, lds);
-        if (there && v_loads) load_to_lds(V + at + v_vec * 8, lds + 2 * STAGE);
-        if (!there) {
-          if (k_loads) sh.keys[to][PASS * i + row_in][place] = places[i].page != -2 ? nan8<T>() : zero8<T>();
+        if (at >= 0 && k_loads) load_to_lds(K + at + k_vec * 8, lds);
+        if (at >= 0 && v_loads) load_to_lds(V + at + v_vec * 8, lds + 2 * STAGE);
+        if (at < 0) {
+          if (k_loads) sh.keys[to][PASS * i + row_in][place] = at == -1 ? nan8<T>() : zero8<T>();
           if (v_loads) sh.values[to][PASS * i + row_in][place] = zero8<T>();
         }
       }
@@ -826,21 +822,29 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
           for (int d = 0; d < DT; d++) o[d] *= f;
         }
         const float base = m == NEG_INF ? 0.f : m;
-        Vec8<T> weights[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++)
+        // (the exponentials of a step's weights are between the products of the last one)
+        Vec8<T> weights[2];
+        auto weigh = [&](int i) {
 #pragma unroll
           for (int e = 0; e < 8; e++) {
             const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], c, -base));
             sum += x;
-            weights[i][e] = (T)x;
+            weights[i & 1][e] = (T)x;
           }
+        };
+        weigh(0);
 #pragma unroll
         for (int i = 0; i < 4; i++) {
           if (i < 3) read_values(i + 1, v[(i + 1) & 1]);
           __builtin_amdgcn_sched_barrier(0);
+          if (i < 3) weigh(i + 1);
 #pragma unroll
-          for (int d = 0; d < DT; d++) o[d] = product32(v[i & 1][d], weights[i], o[d]);
+          for (int d = 0; d < DT; d++) o[d] = product32(v[i & 1][d], weights[i & 1], o[d]);
+#pragma unroll
+          for (int d = 0; d < DT; d++) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 28 / DT, 0);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
         for (; bad; bad &= bad - 1) {
