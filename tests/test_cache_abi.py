@@ -105,6 +105,8 @@ def test_attention_pointers_and_workspace():
     for name in ("tables", "offsets", "lengths", "queries", "out"):
         assert _attention(**{name: None}) == NULL, name
     assert _attention(cache(values=None)) == NULL
+    assert _attention(cache(page_stride=1 << 36)) == LARGE and _attention(cache(slot_stride=1 << 36)) == LARGE
+    assert _attention(tokens=(1 << 31) - 1, n_requests=3) == LARGE
     assert _attention(tokens=0, queries=None, out=None) == OK
     assert _attention(n_requests=0, offsets=None) == OK
     need = tt.cache_attention_workspace(7, 3, 4, 2, 64)
