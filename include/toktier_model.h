@@ -100,7 +100,8 @@ enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 };
  * each of kv_heads heads in each of page_size slots of each page.  Both have the
  * same strides, in elements; a slot's number is page * page_size + place in it,
  * as in tt_step.  dim and the strides are multiples of 8, dim is at most
- * TT_MAX_HEAD_DIM, and keys and values are aligned to 16 bytes. */
+ * TT_MAX_HEAD_DIM, strides of pages and slots are below 2^35, and keys and values
+ * are aligned to 16 bytes. */
 #define TT_MAX_HEAD_DIM 256
 typedef struct {
   int32_t type;                 /* TT_BF16 or TT_F16, of every tensor of a call              */

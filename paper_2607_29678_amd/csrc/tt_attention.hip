@@ -65,6 +65,7 @@ struct AttentionArgs {
   uint32_t page_step, slot_step;  // strides in vectors of 8 elements
   int per_kv;      // query heads of a key head
   bool vectors;    // queries and out are aligned to 16 bytes
+  bool wide;       // sums of units may pass 32 bits, or there are more requests than LDS holds
   uint8_t* parts;  // workspace
 };
 
@@ -105,7 +106,7 @@ __device__ __forceinline__ Item item_of(const AttentionArgs& a, const Plan& p, i
   if (at < 0 || row0 >= off1) return t;
   t.tokens = off1 - row0 < p.tokens ? (int)(off1 - row0) : p.tokens;
   const int64_t low = (int64_t)length - raw1 + row0, high = low + t.tokens - 1;
-  t.low = clamped(low, INT32_MIN / 2, INT32_MAX);
+  t.low = clamped(low, INT32_MIN / 2, INT32_MAX - 256);  // (positions of an item's tokens do not overflow)
   t.last = clamped(high, -1, a.capacity);
   t.begin = a.s.window ? clamped(low - a.s.window + 1, 0, a.capacity) : 0;
   t.front = a.s.sinks < t.begin ? a.s.sinks : t.begin;
@@ -162,97 +163,139 @@ __device__ __forceinline__ bool few_rows(const AttentionArgs& a, Search& sh) {
 __device__ __forceinline__ int64_t divided(int64_t n, int64_t d) {
   return n <= INT32_MAX && d <= INT32_MAX ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d;
 }
+__device__ __forceinline__ int32_t divided(int32_t n, int32_t d) { return (int32_t)((uint32_t)n / (uint32_t)d); }
 
-// Finds the parts of the block's COUNT workers (first, first + 1, ...).
-template <int COUNT>
-__device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& p, int first, Search& sh, Start* starts) {
+// Sum of the lanes up to and with this one
+__device__ __forceinline__ int32_t wave_scan(int32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // within rows of 16: 1, 2, 4, 8 lanes back
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // a row's last lane to the next row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+  return x;
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up((long long)x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Finds the parts of the block's COUNT workers (first, first + 1, ...), with 32-bit sums
+// from LDS (SHORT) or with 64-bit sums from memory, where the sizes that the host sees
+// do not keep them below 2^31 or there are more requests than LDS holds.
+template <int COUNT, bool SHORT, class I = std::conditional_t<SHORT, int32_t, int64_t>>
+__device__ __forceinline__ void find_starts_by(const AttentionArgs& a, const Plan& p, int first, Search& sh, Start* starts) {
   const tt_attention& s = a.s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = s.n_requests;
-  const bool staged = n <= STAGED;
   if (tid < COUNT) starts[tid].count = 0;
-  auto raw = [&](int r) { return staged ? sh.offsets[r] : s.offsets[r]; };
+  auto raw = [&](int r) {
+    if constexpr (SHORT) return sh.offsets[r];
+    else return s.offsets[r];
+  };
+  auto length = [&](int r) {
+    if constexpr (SHORT) return sh.lengths[r];
+    else return s.lengths[r];
+  };
   auto offset = [&](int r) { return clamped(raw(r), 0, s.tokens); };
-  auto begin = [&](int r) { return (int64_t)p.by_tokens.of(offset(r)) + r; };
-  const int64_t slots = begin(n);
+  auto begin = [&](int r) { return p.by_tokens.of(offset(r)) + r; };
+  const int slots = begin(n);
   // threads take one slot each, or EACH
   const int each = slots <= ATT_THREADS ? 1 : EACH;
-  const int64_t at_once = (int64_t)ATT_THREADS * each;
-  auto item = [&](int64_t slot, int r) {
-    return item_of(a, p, (int)slot, r, offset(r), offset(r + 1), raw(r + 1), staged ? sh.lengths[r] : s.lengths[r]);
+  auto item = [&](int slot, int r) {
+    return item_of(a, p, slot, r, offset(r), offset(r + 1), raw(r + 1), length(r));
   };
-  // units of the thread's slots from slot0 on; their requests
-  auto count = [&](int64_t slot0, int* units, int* requests) {
-    if (slot0 >= slots) return (int64_t)0;
-    int lo = 0, hi = n;  // requests [0, lo) begin at or before slot0
+  auto request_of = [&](int slot) {
+    int lo = 0, hi = n;  // requests [0, lo) begin at or before the slot
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (begin(mid) <= slot0) lo = mid + 1;
+      if (begin(mid) <= slot) lo = mid + 1;
       else hi = mid;
     }
-    int r = lo > 0 ? lo - 1 : 0;
-    int64_t sum = 0;
-#pragma unroll
-    for (int e = 0; e < EACH; e++) {
-      const int64_t slot = slot0 + e;
-      units[e] = 0;
-      if (e >= each || slot >= slots) continue;
+    return lo > 0 ? lo - 1 : 0;
+  };
+  // units of the thread's slots from slot0 on, the first of them of request r
+  auto count = [&](int slot0, int r) {
+    I sum = 0;
+#pragma unroll 1
+    for (int slot = slot0; slot < slot0 + each && slot < slots; slot++) {
       while (r + 1 < n && begin(r + 1) <= slot) r++;
-      units[e] = item(slot, r).units;
-      requests[e] = r;
-      sum += units[e];
+      sum += item(slot, r).units;
     }
     return sum;
   };
   // sums of the threads before this one, and of all
-  auto scan = [&](int64_t mine, int64_t& before) {
-    int64_t x = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
+  auto scan = [&](I mine, I& before) {
+    const I x = wave_scan(mine);
     __syncthreads();
     if (lane == 63) sh.sums[wave] = x;
     __syncthreads();
     before = x - mine;
-    int64_t all = 0;
+    I all = 0;
 #pragma unroll
     for (int w = 0; w < ATT_WAVES; w++) {
-      if (w < wave) before += sh.sums[w];
-      all += sh.sums[w];
+      if (w < wave) before += (I)sh.sums[w];
+      all += (I)sh.sums[w];
     }
     return all;
   };
-  int64_t total = 0, before = 0, mine = 0;
-  int units[EACH], requests[EACH];
-  for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) total += scan(mine = count(slot0 + tid * each, units, requests), before);
-  if (total == 0) return;
-  const int64_t line = p.stride > 1 ? total : total * a.c.kv_heads * p.groups;
-  int64_t size = divided(line + p.parts - 1, p.parts);
-  if (size < p.least) size = p.least;
-  int64_t base = 0;
+  const int at_once = ATT_THREADS * each;
+  I total = 0, before = 0, mine = 0;
+  int request = 0;
   for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) {
-    int64_t here = total;
-    if (slots > at_once) here = scan(mine = count(slot0 + tid * each, units, requests), before);
+    const int slot = (int)slot0 + tid * each;
+    request = slot < slots ? request_of(slot) : 0;
+    mine = slot < slots ? count(slot, request) : 0;
+    total += scan(mine, before);
+  }
+  if (total == 0) return;
+  const I line = p.stride > 1 ? total : total * (I)(a.c.kv_heads * p.groups);
+  I size = divided(line + p.parts - 1, (I)p.parts);
+  if (size < p.least) size = p.least;
+  I base = 0;
+  for (int64_t slot0 = 0; slot0 < slots; slot0 += at_once) {
+    const int slot_mine = (int)slot0 + tid * each;
+    I here = total;
+    if (slots > at_once) {
+      request = slot_mine < slots ? request_of(slot_mine) : 0;
+      mine = slot_mine < slots ? count(slot_mine, request) : 0;
+      here = scan(mine, before);
+    }
+    int part = p.stride > 1 ? divided(first, p.stride) : first, head_unit = p.stride > 1 ? first - part * p.stride : 0;
     for (int w = 0; w < COUNT; w++) {
-      const int part = (first + w) / p.stride;
-      const int64_t from = part * size;
-      if (from >= line || part >= p.parts) break;
-      const int64_t over = p.stride > 1 ? 0 : divided(from, total), head = p.stride > 1 ? first + w - part * p.stride : over;
-      int64_t x = from - over * total - base - before;
-      if (x < 0 || x >= mine) continue;
-#pragma unroll
-      for (int e = 0; e < EACH; e++) {
-        if (x >= 0 && x < units[e]) {
-          const int64_t slot = slot0 + tid * each + e;
-          starts[w] = {(int)slot, requests[e], (int)head, (int)x, (int)slots, from + size < line ? size : line - from, size, item(slot, requests[e])};
+      const I from = part * size;
+      if (part >= p.parts || from >= line) break;
+      const I over = p.stride > 1 ? 0 : divided(from, total);
+      I x = from - over * total - base - before;
+      if (x >= 0 && x < mine) {
+        int r = request;
+        for (int slot = slot_mine; slot < slot_mine + each && slot < slots; slot++) {
+          while (r + 1 < n && begin(r + 1) <= slot) r++;
+          const Item t = item(slot, r);
+          if (x < t.units) {
+            starts[w] = {slot, r, p.stride > 1 ? head_unit : (int)over, (int)x, slots, from + size < line ? size : line - from, size, t};
+            break;
+          }
+          x -= t.units;
         }
-        x -= units[e];
+      }
+      if (p.stride == 1 || ++head_unit == p.stride) {
+        part++;
+        head_unit = 0;
       }
     }
     base += here;
   }
   __syncthreads();
+}
+template <int COUNT>
+__device__ __forceinline__ void find_starts(const AttentionArgs& a, const Plan& p, int first, Search& sh, Start* starts) {
+  if (a.wide) find_starts_by<COUNT, false>(a, p, first, sh, starts);
+  else find_starts_by<COUNT, true>(a, p, first, sh, starts);
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -921,7 +964,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) void attention_kern
 // A block looks after every 256th worker (neighbours begin items together); the blocks of one x share the rows of the
 // items that these begin and others go on.  Groups of lanes take a row each, or, where
 // an item has many pieces, all of them one row, each every n-th piece.
-constexpr int JOIN_X = 256, JOIN_Y = 8, JOIN_MOST = 2048 / JOIN_X;
+constexpr int JOIN_X = 256, JOIN_Y = 4, JOIN_MOST = 2048 / JOIN_X;
 template <class T>
 __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int lanes) {
   __shared__ F4 sums[ATT_THREADS];
@@ -988,7 +1031,7 @@ __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int 
         }
       };
       if (mine) {
-        if (many) add(std::integral_constant<int, 16>{}, group, groups);
+        if (many) add(std::integral_constant<int, 8>{}, group, groups);
         else add(std::integral_constant<int, 4>{}, 0, 1);
       }
       if (many) {
@@ -1030,7 +1073,7 @@ Plan plan_of(bool small, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   p.rows = small ? SMALL_ROWS : 128;
   p.keys = small ? 32 : 64;
   p.workers = BLOCKS / (dim > 128 ? 2 : 1) * (small ? ATT_WAVES : 1);
-  p.least = small ? 2 : 4;
+  p.least = small ? 1 : 4;
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
   p.tokens = p.rows / p.heads;
@@ -1098,6 +1141,8 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
                   (uint32_t)(cache->slot_stride / 8),
                   s.q_heads / cache->kv_heads,
                   in_vectors(s.queries, s.query_stride) && in_vectors(s.out, s.out_stride),
+                  // at most this many items of a head unit, units of an item and head units
+                  s.n_requests > STAGED || (double)(s.tokens + s.n_requests) * ((double)capacity / 32 + 3) * s.q_heads * 2 >= INT32_MAX,
                   static_cast<uint8_t*>(workspace)};
   return cache->type == TT_BF16 ? run_attention<bf16_t>(a, static_cast<hipStream_t>(stream))
                                 : run_attention<f16_t>(a, static_cast<hipStream_t>(stream));

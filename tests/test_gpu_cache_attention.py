@@ -55,6 +55,13 @@ def test_prompts(gpu, heads, kv, dim, dtype):
     check(Step([(0, 130), (77, 65), (200, 1), (0, 1), (3, 17)], heads, kv, dim, 16, dtype, seed=dim))
 
 
+@pytest.mark.parametrize("kv,requests", [(600, [(0, 40)]), (600, [(30, 1), (0, 1)]), (2_100, [(40, 1), (7, 2)]), (300, [(3, 30), (0, 1)])])
+def test_more_heads_than_workers(gpu, kv, requests):
+    check(Step(requests, kv, kv, 8, 16, BF))
+    if kv == 300:
+        check(Step(requests, kv, kv, 136, 16, BF))
+
+
 @pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 1_000, 4_097, 20_001])
 def test_lengths(gpu, length):
     check(Step([(length - 1, 1)], 8, 2, 64, 16, BF, seed=length))
@@ -68,6 +75,17 @@ def test_pages(gpu, page):
     requests = [(333, 1), (0, 5), (page, 1), (2 * page - 1, 2), (17, 40)]
     check(Step(requests, 8, 2, 64, page, BF, seed=page))
     check(Step([(c, 1) for c, _ in requests], 8, 2, 64, page, H, seed=page))
+
+
+@pytest.mark.parametrize("requests", [[(333, 1), (0, 1), (90, 1)], [(333, 70), (0, 5), (90, 1)], [(i % 40, 1) for i in range(1_500)]])
+def test_wide_tables(gpu, requests):
+    """Tables of so many entries that sums of units could pass 32 bits."""
+    s = Step(requests, 4, 2, 64, 1_000, BF)
+    tables = torch.full((len(requests), 300_000), -1, dtype=torch.int32, device="cuda")
+    tables[:, :s.width] = s.tables
+    s.tables = tables
+    check(s, rows=set(range(0, s.tokens, 41)) | {s.tokens - 1})
+    check(s, 50, 4, rows=set(range(0, s.tokens, 41)) | {s.tokens - 1})
 
 
 @pytest.mark.parametrize("layout", sorted(LAYOUTS))
