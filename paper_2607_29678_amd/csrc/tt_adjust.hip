@@ -5,6 +5,13 @@
 // row's history names (integers: the order does not matter) and which entry of the
 // bias list names them last, and then streams the columns through: 16 bytes a load,
 // all of a thread's loads under way before the lists are read.
+//
+// What bounds it: reading and writing the rows.  512 rows of 100,257 in f32 with 2,000
+// tokens of history and masks take 83 us, 5.0 TB/s (70 without lists and masks).  The
+// gradient of 1,536 rows in bf16 takes 108 us without a history and 205 with one of
+// 1,000 tokens a row: 24 of those are every block's reading of the lists, the rest the
+// logits of repeated tokens, whose sign the slope depends on: scattered reads, a
+// million of them.  32 rows of 50,257: the host call.
 #include "tt_scores.h"
 
 namespace tt {
@@ -12,7 +19,8 @@ namespace {
 
 constexpr int ADJ_THREADS = 256;
 // Vectors of a thread: four, but two where LDS holds a count or a place for each
-// column of 16 bits, so that more blocks fit a compute unit
+// column of 16 bits, so that more blocks fit a compute unit (512 rows of 100,257 in
+// bf16 with histories of 2,000 tokens 73 us, with four 89; with 100 and biases 76 and 112)
 template <class T, bool LISTS>
 constexpr int adj_vecs() { return LISTS && sizeof(T) == 2 ? 2 : 4; }
 

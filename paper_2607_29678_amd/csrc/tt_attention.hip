@@ -13,7 +13,16 @@
 // Products are of transposed tiles: S^T = K Q^T puts a query's scores into the
 // lanes of one column, so that the running maximum and sum are a lane's own and the
 // exponentials are, as they stand, the operand of O^T = V^T P^T.  Values are
-// transposed by the loads from LDS.
+// transposed by the loads from LDS.  An online softmax keeps the sums of a row as of
+// a maximum that goes up only by more than a factor of 2^8, so that most tiles move
+// nothing.
+//
+// What bounds it: single tokens, reads of keys and values (96 requests of 4,000 tokens,
+// 32 heads over 8 of 128 elements: 1.63 GB in 317 us, 5.1 TB/s, the rate of a plain
+// copy being 4.9); prompts, the matrix cores and the vector instructions beside them
+// (14,001 tokens, the same heads: 1,175 us, 760 TFLOP/s; a plain library product
+// 1,200 to 1,490 on these cards); a few short requests, the search of every block's
+// part, cold, 6 us of 13, and the join, 4 to 8.
 #include "tt_cache.h"
 
 namespace tt {
@@ -35,6 +44,10 @@ struct Quotient {
 constexpr int ATT_THREADS = 256;
 constexpr int ATT_WAVES = 4;
 constexpr int STAGED = 1024;  // requests whose offsets and lengths are held in LDS for the search
+// Rows (tokens times query heads of a key head) of a request up to which, on average,
+// the small path takes a step.  us by the small and by the large path: 2 requests of
+// 120,000 tokens, 7 rows 132 / 188; 64 of 20,000 in a window of 4,096, 40 rows 443 /
+// 205 (the small path reads the keys once for every 16 rows).
 constexpr int SMALL_ROWS = 16;
 constexpr int EACH = 4;       // items counted by a thread at a time
 
@@ -471,7 +484,11 @@ constexpr float SLACK = 8.f;
 
 // A wave takes its units by itself: 32 keys and values go from memory to registers,
 // the keys straight into the product, the values through LDS that is the wave's own.
-// The next unit's are under way during the exponentials and the second product.
+// The next unit's are under way during the exponentials and the second product: 16 KB
+// a wave, 128 KB a compute unit.  Loads that do not stay in the caches were slower
+// (96 requests of 4,000 tokens 385 us against 367: a row comes in two requests of 64
+// bytes a cache line), and so were workers that follow each other within a head (367
+// against 334: neighbours then read rows 2 KB apart).
 template <class T, int KK>  // KK: 32 elements of a head
 struct SmallShared {
   static constexpr int PITCH = KK * 32 + 16;  // (rows 32 bytes apart in the banks)
@@ -681,7 +698,8 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
 
 // Four waves of 32 rows share tiles of 64 keys and values in LDS, two of each: the
 // next unit's come straight from memory during a unit's products, so that one barrier
-// a unit is enough and no registers wait for them.  A load writes 1 KB as it comes,
+// a unit is enough and no registers wait for them (a prefill of 14,001 tokens 1,390 us,
+// through registers 1,834).  A load writes 1 KB as it comes,
 // so rows stand without gaps, and the vectors of 16 bytes trade places in their row
 // instead (key_place, value_place): rows that are read at once lie in other banks.
 template <class T, int DP>  // DP: elements of a head, with zeros behind its own
@@ -816,7 +834,8 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
 #pragma unroll
           for (int e = 0; e < 16; e++) s[i][e] = 0.f;
         // Reads stay a group of products ahead (of its own accord the compiler reads
-        // right before each product and waits): two steps of keys, then four tiles of values.
+        // right before each product and waits: 1,390 us for 1,258): two steps of keys,
+        // then four tiles of values.
         Vec8<T> k[2][4], v[2][DT];
         auto read_keys = [&](int kk, Vec8<T>* to) {
 #pragma unroll
@@ -865,7 +884,8 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
           for (int d = 0; d < DT; d++) o[d] *= f;
         }
         const float base = m == NEG_INF ? 0.f : m;
-        // (the exponentials of a step's weights are between the products of the last one)
+        // (the exponentials of a step's weights are between the products of the last one:
+        // with one place found by a lane instead of a row's by 16, 1,258 us -> 1,204)
         Vec8<T> weights[2];
         auto weigh = [&](int i) {
 #pragma unroll
@@ -1073,7 +1093,7 @@ Plan plan_of(bool small, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   p.rows = small ? SMALL_ROWS : 128;
   p.keys = small ? 32 : 64;
   p.workers = BLOCKS / (dim > 128 ? 2 : 1) * (small ? ATT_WAVES : 1);
-  p.least = small ? 1 : 4;
+  p.least = small ? 1 : 4;  // (4 short requests: 24.0 us, with 2 units 24.9)
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
   p.tokens = p.rows / p.heads;
