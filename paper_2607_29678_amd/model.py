@@ -155,39 +155,54 @@ def _heads(t, name, device, dtype, tokens=None, heads=None, dim=None):
         raise ValueError("%s must be a %s tensor of [tokens%s, heads%s, dim%s] on device %d with the others, not %s %s on %s"
                          % (name, dtype, "" if tokens is None else " = %d" % tokens, "" if heads is None else " = %d" % heads,
                             "" if dim is None else " = %d" % dim, device, t.dtype, tuple(shape), t.device))
-    n, h, d = shape
-    row, head, step = t.stride()
+    row = _row_stride(shape, t.stride())
+    if row < 0:
+        raise ValueError("the rows of %s %s" % (name, "must be contiguous" if row == -1 else "overlap"))
+    return t.data_ptr(), row
+
+
+@functools.lru_cache(maxsize=256)
+def _row_stride(shape, strides):
+    """Distance of the rows [heads, dim] of a tensor of this shape and these strides: a function of them alone.
+    -1: the rows are not contiguous; -2: they overlap."""
+    (n, h, d), (row, head, step) = shape, strides
     if (d > 1 and step != 1) or (h > 1 and head != d):
-        raise ValueError("the rows of %s must be contiguous" % name)
+        return -1
     if n <= 1:
         row = max(row, h * d)
-    if row < h * d:
-        raise ValueError("the rows of %s overlap" % name)
-    return t.data_ptr(), row
+    return row if row >= h * d else -2
+
+
+@functools.lru_cache(maxsize=64)
+def _cache_layout(shape, strides):
+    """The sizes and strides of tt_cache for tensors of this shape and these strides: a function of them alone."""
+    pages, page_size, heads, dim = shape
+    if dim > 1 and strides[3] != 1:
+        raise ValueError("the vectors of a cache must be contiguous")
+    if page_size > 0x7FFFFFFF or heads > 0x7FFFFFFF or dim > 0x7FFFFFFF:
+        raise ValueError("a cache of shape %s is too large" % (tuple(shape),))
+    # no two vectors of a cache share elements: from the narrowest stride up, each is at least what lies below it
+    below = dim
+    for stride, size in sorted(zip(strides[:3], shape[:3])):
+        if size > 1:
+            if stride < below:
+                raise ValueError("vectors of the cache overlap")
+            below = stride * (size - 1) + below
+    stride = [0 if n <= 1 else s for s, n in zip(strides, shape)]  # (one page, slot or head: its stride means nothing)
+    return page_size, heads, dim, pages, stride[0], stride[1], stride[2]
 
 
 def _cache(keys, values):
     """tt_cache of two tensors [pages, page_size, heads, dim] of the same strides; (packed, device)."""
     d = _device(keys, "key_cache")
     kind = _type_of(keys, "key_cache", (1, 2))
-    if keys.dim() != 4 or values.shape != keys.shape or values.dtype != keys.dtype or values.get_device() != d:
+    shape, strides = keys.shape, keys.stride()
+    if len(shape) != 4 or values.shape != shape or values.dtype != keys.dtype or values.get_device() != d:
         raise ValueError("key_cache and value_cache must be two tensors of [pages, page_size, heads, dim], not %s %s and %s %s on %s"
-                         % (keys.dtype, tuple(keys.shape), values.dtype, tuple(values.shape), values.device))
-    pages, page_size, heads, dim = keys.shape
-    strides = keys.stride()
-    if values.stride() != strides or (dim > 1 and strides[3] != 1):
-        raise ValueError("key_cache and value_cache must have the same strides, and contiguous vectors")
-    if page_size > 0x7FFFFFFF or heads > 0x7FFFFFFF or dim > 0x7FFFFFFF:
-        raise ValueError("a cache of shape %s is too large" % (tuple(keys.shape),))
-    # no two vectors of a cache share elements: from the narrowest stride up, each is at least what lies below it
-    below = dim
-    for stride, size in sorted(zip(strides[:3], keys.shape[:3])):
-        if size > 1:
-            if stride < below:
-                raise ValueError("vectors of the cache overlap")
-            below = stride * (size - 1) + below
-    stride = [0 if n <= 1 else s for s, n in zip(strides, keys.shape)]  # (one page, slot or head: its stride means nothing)
-    return _CACHE.pack(kind, page_size, heads, dim, pages, stride[0], stride[1], stride[2], keys.data_ptr(), values.data_ptr()), d
+                         % (keys.dtype, tuple(shape), values.dtype, tuple(values.shape), values.device))
+    if values.stride() != strides:
+        raise ValueError("key_cache and value_cache must have the same strides")
+    return _CACHE.pack(kind, *_cache_layout(shape, strides), keys.data_ptr(), values.data_ptr()), d
 
 
 def cache_append(keys, values, key_cache, value_cache, slots, positions=None, frequencies=None, interleaved=False, queries=None,
