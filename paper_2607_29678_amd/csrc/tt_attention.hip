@@ -3,9 +3,9 @@
 //
 // Work is cut into items: a tile of a request's tokens with the query heads that
 // share a key head (their products share the loads of keys and values), and every
-// item into units, tiles of keys that some of its tokens see.  All units of a step
-// stand in one line, and workers take equal parts of it: a step of long and short
-// requests, of single tokens and prompts, is even by construction, and a
+// item into units, tiles of keys that some of its tokens see.  The units of a key head
+// stand in one line, and the head's workers take equal parts of it: a step of long and
+// short requests, of single tokens and prompts, is even by construction, and a
 // graph's launches need no lengths on the host.  Every block finds its part by
 // summing the items' units for itself.  Where an item's units fall to several
 // workers, each leaves its sums in the workspace, and a second launch joins them.
