@@ -883,14 +883,26 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
 #pragma unroll
           for (int d = 0; d < DT; d++) o[d] *= f;
         }
-        const float base = m == NEG_INF ? 0.f : m;
+        float base = m == NEG_INF ? 0.f : m, by = c;
+        // One multiply-add gives an exponent, by the exact product of score and scale.  m is
+        // rounded, and where half its last place is a power of two or more, far maxima would
+        // overflow by that: their exponents are the difference of rounded products.
+        if (fabsf(base) >= PLAIN_MOST) {
+#pragma clang fp contract(off)
+#pragma unroll
+          for (int i = 0; i < 2; i++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) s[i][e] = s[i][e] * c - base;
+          base = 0.f;
+          by = 1.f;
+        }
         // (the exponentials of a step's weights are between the products of the last one:
         // with one place found by a lane instead of a row's by 16, 1,258 us -> 1,204)
         Vec8<T> weights[2];
         auto weigh = [&](int i) {
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], c, -base));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], by, -base));
             sum += x;
             weights[i & 1][e] = (T)x;
           }
