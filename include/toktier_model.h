@@ -147,8 +147,9 @@ int tt_cache_append(const tt_cache* cache, int64_t tokens, const int64_t* slots,
  * How the sums of a step are shared out, and with it their rounding, depends on
  * the offsets and lengths of the whole step.
  * Products and sums are held in 32 bits; exp(x_j - max), at most 1 up to a factor
- * of 2^8, is rounded to the type before it is multiplied by the values, and the
- * result is rounded once. */
+ * of 2^8 (of 2^15 in TT_F16, whose weights below 2^-14 have fewer places), is
+ * rounded to the type before it is multiplied by the values, and the result is
+ * rounded once. */
 typedef struct {
   int32_t n_requests;
   int32_t table_width;

@@ -477,8 +477,21 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, const Place
   return (int64_t)(((uint64_t)(uint32_t)x.page * a.page_step + (uint64_t)(uint32_t)x.slot * a.slot_step) * 8) + head;
 }
 
-// A running maximum goes up only where it has to by more than this (in powers of two)
+// The weights 2^(score - m) are rounded to the type for the second product, their sum is
+// of 32 bits.  (One rounding a weight, half a place: the matrix cores take operands of the
+// type, and the result is rounded by as much again.)  m goes up only where a score is more
+// than SLACK powers of two above the largest it is of.
+// A weight of f16 has full places from 2^-14 on and none below 2^-25, while the sum holds
+// them all: many small ones would be missing above and there below, 16% of a result with
+// one key 17.4 above 20,000 others.  So m lies HEAD below that largest score: weights go up
+// to 2^15, and n keys lose at most n 2^-32 of their largest value.
 constexpr float SLACK = 8.f;
+template <class T>
+constexpr float HEAD = std::is_same<T, f16_t>::value ? 7.f : 0.f;
+// m after a tile whose largest score is top (differences: near the ends of the range, and
+// without one, sums would round to either side)
+template <class T>
+__device__ __forceinline__ float raised(float m, float top) { return top - m > SLACK + HEAD<T> ? top - HEAD<T> : m; }
 
 // ---- 16 rows a wave: single tokens -----------------------------------------------
 
@@ -617,10 +630,10 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
           s[i][e] *= c;
           top = fmaxf(top, s[i][e]);
         }
-      if (__ballot(top > m + SLACK)) {
+      if (__ballot(raised<T>(m, top) != m)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        top = top > m + SLACK ? top : m;  // (a row's own choice: its result does not depend on its neighbours)
+        top = raised<T>(m, top);  // (a row's own choice: its result does not depend on its neighbours)
         const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
         m = top;
         sum *= f;
@@ -874,9 +887,9 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
 #pragma unroll
           for (int e = 0; e < 16; e++) top = fmaxf(top, s[i][e]);
         top *= c;
-        if (__ballot(top > m + SLACK)) {
+        if (__ballot(raised<T>(m, top) != m)) {
           top = fmaxf(top, __shfl_xor(top, 32));
-          top = top > m + SLACK ? top : m;  // (a row's own choice: its result does not depend on its neighbours)
+          top = raised<T>(m, top);  // (a row's own choice: its result does not depend on its neighbours)
           const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
           m = top;
           sum *= f;
@@ -885,8 +898,8 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
         }
         float base = m == NEG_INF ? 0.f : m, by = c;
         // One multiply-add gives an exponent, by the exact product of score and scale.  m is
-        // rounded, and where half its last place is a power of two or more, far maxima would
-        // overflow by that: their exponents are the difference of rounded products.
+        // rounded, and half its last place is what the largest weight would be off by, to
+        // overflow: far maxima's exponents are the difference of rounded products.
         if (fabsf(base) >= PLAIN_MOST) {
 #pragma clang fp contract(off)
 #pragma unroll

@@ -68,3 +68,69 @@ def test_scores_far_from_zero(gpu, requests, dim, dtype, scale):
             assert torch.equal(out[t, h], v[best, h // 2]), (t, p, h)
             want = float(level[best, h // 2]) * scale
             assert abs(float(sums[t, h]) - want) <= 7 * 2.0 ** -24 * (abs(want) + 5)
+
+
+def reference(s, q, k, v, scale, rows):
+    """(out, logsums, tolerances of both) in float64 of these rows.  A score: sums of dim products and three roundings of the
+    exponent; an exponential 2 units, sums of n terms; the weights are rounded to the type once, and so is the result.  A
+    weight is at least 2^7 for a largest score, so that half the smallest step of f16 that it may be off by is 2^-32 of it."""
+    u, least, u32 = (2.0 ** -11, 2.0 ** -25, 2.0 ** -24) if s.dtype == H else (2.0 ** -8, 0.0, 2.0 ** -24)
+    group, at, result = s.heads // s.kv, positions(s), []
+    k, v = k.double().cuda().transpose(0, 1).contiguous(), v.double().cuda().transpose(0, 1).contiguous()
+    for t in rows:
+        n = at[t] + 1
+        qt = q[t].double().cuda().view(s.kv, group, 1, s.dim)
+        x = (qt * k[:, None, :n]).sum(3) * scale
+        terms = (qt.abs() * k[:, None, :n].abs()).sum(3).amax(2) * scale
+        top = x.amax(2, keepdim=True)
+        e = (x - top).exp()
+        total = e.sum(2, keepdim=True)
+        y, size = (torch.matmul(e / total, w[:, :n]) for w in (v, v.abs()))
+        deep = (top - x.amin(2, keepdim=True))[..., 0].clamp(max=90)
+        e_x = u32 * ((s.dim + 4) * terms + 4 * (deep + top[..., 0].abs()))
+        off = size * (u + 2 * e_x + u32 * (n + 16))[..., None] + n * least / 128 * v.abs().amax() / total
+        ls = (top + total.log())[..., 0]
+        result.append([x.flatten(0, 1).cpu() for x in (y, ls, off + u * (y.abs() + off) + least, e_x + u32 * (n + 16 + 4 * ls.abs()))])
+    return [torch.stack(x) for x in zip(*result)]
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("cached,requests,heads,kv", [
+    (20_000, [(20_000, 1)] * 512, 8, 8), (100_000, [(100_000, 1)] * 40, 16, 16), (20_001, [(20_001, 3)] * 300, 8, 4),
+    (20_000, [(20_000, 512)] * 8, 16, 16), (100_000, [(99_000, 1_000)], 8, 4)])
+def test_a_first_key_above_all_others(gpu, cached, requests, heads, kv, dtype):
+    """The first token draws nearly all of the weight and has no value: what the result is made of are many small weights,
+    that a worker has along with the first one's."""
+    dim, n, scale = 64, max(c + f for c, f in requests), 0.125
+    g = torch.Generator().manual_seed(cached + len(requests))
+    k = 0.3 * torch.randn(n, kv, dim, generator=g)
+    v = 1 + 0.5 * torch.randn(n, kv, dim, generator=g)
+    k[0], v[0] = 17.4 / scale / dim, 0.0
+    q = (1 + 0.1 * torch.randn(sum(f for _, f in requests), heads, dim, generator=g)).to(dtype)
+    k, v = k.to(dtype), v.to(dtype)
+    s = step(requests, heads, k, v)
+    out, sums = run(s, q, scale)
+    rows = sorted({0, 1, s.tokens // 3, s.tokens // 2, s.tokens - 1})
+    want, want_sums, tol, sums_tol = reference(s, q, k, v, scale, rows)
+    off = ((out[rows].double() - want).abs() / tol).max()
+    assert float(off) <= 1, float(off)
+    assert bool(((sums[rows].double() - want_sums).abs() <= sums_tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("above", [5.4, 5.6, 9.9, 10.3, 10.5])
+@pytest.mark.parametrize("requests", [[(200, 1)] * 3, [(100, 300), (7, 90)]])
+def test_a_late_key_near_the_step_of_the_maximum(gpu, requests, above, dtype):
+    """The largest weight that a tile may have before the running maximum goes up, times values of the type's largest size."""
+    heads, kv, dim, scale, n = 4, 2, 64, 0.125, 400
+    g = torch.Generator().manual_seed(int(above * 10))
+    k, v = 0.01 * torch.randn(n, kv, dim, generator=g), 3e4 * torch.randn(n, kv, dim, generator=g).clamp(-2, 2)
+    k[150::64] = above / scale / dim
+    q = torch.ones(sum(f for _, f in requests), heads, dim, dtype=dtype)
+    k, v = k.to(dtype), v.to(dtype)
+    s = step(requests, heads, k, v)
+    out, sums = run(s, q, scale)
+    rows = sorted({0, s.tokens // 3, s.tokens // 2, s.tokens - 1})
+    want, want_sums, tol, sums_tol = reference(s, q, k, v, scale, rows)
+    assert bool(((out[rows].double() - want).abs() <= tol).all())
+    assert bool(((sums[rows].double() - want_sums).abs() <= sums_tol).all())
