@@ -86,6 +86,7 @@ struct AttentionArgs {
 struct Leaf {
   int32_t pieces;              // of the item that its last piece begins and others go on; 0: none
   int32_t row0, tokens, head;  // that item's first row of queries, its tokens and its head unit
+  int32_t low;                 // position of its first token
 };
 
 // The workspace: which path ran (256 bytes), a leaf for each worker, two pieces for each
@@ -519,7 +520,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
   Walk w(starts[wave]);
   __syncthreads();  // (the search's LDS is the values' from here on)
   T(*values)[PITCH] = sh.values[wave];
-  Leaf leaf = {0, 0, 0, 0};
+  Leaf leaf = {0, 0, 0, 0, 0};
   const float c = a.s.scale * LOG2E;
   bool chunk[KK];
 #pragma unroll
@@ -672,7 +673,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
     sum += __shfl_xor(sum, 32);
     const bool began = w.unit > 0, ends = end == t.units;
     if (!began && ends) {
-      const bool none = m == NEG_INF && sum == 0.f;
+      const bool none = position < 0;
       if (live) {
         const float f = none ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + quad * 4;
@@ -699,6 +700,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
         leaf.row0 = t.row0;
         leaf.tokens = t.tokens;
         leaf.head = w.head;
+        leaf.low = t.low;
       }
     }
     w.left -= take;
@@ -748,7 +750,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
   // what lies behind a head's elements is not loaded: zeros, once
   for (int i = tid; i < (int)(sizeof(sh.keys) / 16); i += ATT_THREADS) (&sh.keys[0][0][0])[i] = zero8<T>();
   __syncthreads();
-  Leaf leaf = {0, 0, 0, 0};
+  Leaf leaf = {0, 0, 0, 0, 0};
   const float c = a.s.scale * LOG2E;
   // the vector that this thread loads: its place in LDS, and which one of keys and values comes there
   const int place = tid % PER_ROW, row_in = tid / PER_ROW;
@@ -951,7 +953,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
     sum += __shfl_xor(sum, 32);
     const bool began = w.unit > 0, ends = end == t.units;
     if (!began && ends) {
-      const bool none = m == NEG_INF && sum == 0.f;
+      const bool none = position < 0;
       if (live) {
         const float f = none ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + half * 4;
@@ -981,6 +983,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
         leaf.row0 = t.row0;
         leaf.tokens = t.tokens;
         leaf.head = w.head;
+        leaf.low = t.low;
       }
     }
     w.left -= take;
@@ -1098,7 +1101,7 @@ __global__ __launch_bounds__(ATT_THREADS) void join_kernel(AttentionArgs a, int 
         m = top;
       }
       if (!mine) continue;
-      const bool none = m == NEG_INF && sum == 0.f;
+      const bool none = leaf.low + token < 0;
       const int64_t q_row = leaf.row0 + token, q_head = (int64_t)kv * a.per_kv + h0 + head;
       const float x[4] = {o[0], o[1], o[2], o[3]};
       store4(static_cast<T*>(a.s.out) + q_row * a.s.out_stride + q_head * dim + at, x, none ? 0.f : 1.f / sum, a.vectors);

@@ -134,3 +134,26 @@ def test_a_late_key_near_the_step_of_the_maximum(gpu, requests, above, dtype):
     want, want_sums, tol, sums_tol = reference(s, q, k, v, scale, rows)
     assert bool(((out[rows].double() - want).abs() <= tol).all())
     assert bool(((sums[rows].double() - want_sums).abs() <= sums_tol).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("requests", [[(40, 1), (300, 1), (0, 1)], [(0, 60), (35, 30), (200, 100)], [(300, 1)] * 300])
+def test_scores_of_minus_infinity(gpu, requests, dtype):
+    """A token whose scores are all -inf sees its keys: the sums of exponentials are 0, their logarithm -inf, and the result
+    0 / 0.  With one finite score among them, its value is the result."""
+    heads, kv, dim, n = 4, 2, 64, 301
+    g = torch.Generator().manual_seed(5)
+    v = torch.randn(n, kv, dim, generator=g).to(dtype)
+    k = torch.zeros(n, kv, dim, dtype=dtype)
+    k[:, :, 9] = -math.inf
+    k[50, 1, 9] = 0.5
+    q = torch.ones(sum(f for _, f in requests), heads, dim, dtype=dtype)
+    s = step(requests, heads, k, v)
+    out, sums = run(s, q, 0.5)
+    for t, p in enumerate(positions(s)):
+        assert bool(torch.isnan(out[t, :2]).all()) and bool((sums[t, :2] == -math.inf).all()), (t, p)
+        if p < 50:
+            assert bool(torch.isnan(out[t, 2:]).all()) and bool((sums[t, 2:] == -math.inf).all()), (t, p)
+        else:
+            assert torch.equal(out[t, 2:], v[50, 1].expand(2, dim)), (t, p)
+            assert bool(((sums[t, 2:] - 0.25).abs() <= 7 * 2.0 ** -24 * 5.25).all()), (t, p)  # (roundings as above)
