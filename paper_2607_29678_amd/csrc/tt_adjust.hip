@@ -213,7 +213,7 @@ __global__ __launch_bounds__(ADJ_THREADS) void adjust_kernel(AdjustArgs<T> g) {
     out[j] = (T)(words && !(words[j >> 5] >> (j & 31) & 1) ? banned : no_mask ? nan : y);
   };
   if (chunk == 0 && tid < head) edge(tid);
-  if (last && tail + tid < a.vocab) edge(tail + tid);
+  if (last && tid < (int)(a.vocab - tail)) edge((int64_t)tail + tid);  // (tail + tid may pass 32 bits)
 }
 
 template <class T, bool GRAD>
