@@ -126,7 +126,9 @@ typedef struct {
  * rotated the same way into rotated, which may be queries (same stride); rows of
  * tokens without a slot stay as they are.  Each result is computed in 32 bits and
  * rounded once.  The slots of one call are different ones: where a slot stands
- * twice, it holds elements of either token. */
+ * twice, it holds elements of either token.
+ * TT_ERR_TOO_LARGE: (q_heads + 2 * kv_heads) * dim is above 65,535, or there are
+ * more tokens than the launch has blocks for (2^24 - 1 fit in any case). */
 int tt_cache_append(const tt_cache* cache, int64_t tokens, const int64_t* slots, const int32_t* positions,
                     const float* frequencies, int32_t pairs, int32_t interleaved, const void* keys, int64_t key_stride,
                     const void* values, int64_t value_stride, int32_t q_heads, const void* queries,
@@ -145,7 +147,10 @@ int tt_cache_append(const tt_cache* cache, int64_t tokens, const int64_t* slots,
  * table's entries, gets NaN.  What a token does not see does not matter, be it
  * NaN or infinite.  Rows behind offsets[n_requests] stay as they are.
  * How the sums of a step are shared out, and with it their rounding, depends on
- * the offsets and lengths of the whole step.
+ * the offsets and lengths of the whole step.  The workspace is of a size that fits
+ * any lengths: it depends on the heads and their elements alone (34 MB for 64
+ * elements, 68 MB for 128) and may be shared by calls that are ordered.
+ * TT_ERR_TOO_LARGE: tokens + n_requests is 2^31 or more.
  * Products and sums are held in 32 bits; exp(x_j - max), at most 1 up to a factor
  * of 2^8 (of 2^15 in TT_F16, whose weights below 2^-14 have fewer places), is
  * rounded to the type before it is multiplied by the values, and the result is
@@ -185,7 +190,12 @@ int tt_cache_attention(const tt_cache* cache, const tt_attention* step, void* wo
  * bit j % 32 of word j / 32 is 1 where j is allowed; mask_rows[r] is the mask of
  * row r, negative for none, and a number that is no mask makes the row NaN.  IDs
  * outside the vocabulary are passed over, and offsets are held within their lists.
- * Rounded once, to the type of the logits. */
+ * Rounded once, to the type of the logits.  All penalties of a call look at one
+ * history: where repetition is to count a prompt and an answer but presence and
+ * frequency the answer alone, that takes a call for each (in place: one more pass,
+ * and one more rounding), repetition first, biases and masks with the second.
+ * TT_ERR_TOO_LARGE: rows of more than 2^24 - 1 runs of columns together (a run has
+ * 4,096 or more), or lists of 2^32 - 1 entries and more. */
 typedef struct {
   int32_t type;                 /* TT_F32, TT_BF16 or TT_F16                                 */
   int32_t n_masks;
