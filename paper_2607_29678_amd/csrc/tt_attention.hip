@@ -388,12 +388,20 @@ __device__ __forceinline__ Vec8<T> load8(const T* p, bool vectors) {
   for (int i = 0; i < 8; i++) z[i] = p[i];
   return z;
 }
+// A result lies between its values, but the weights' roundings may carry it past the
+// largest one that f16 has (65,504; infinite from 65,520 on).  What is not finite stays.
+template <class T>
+__device__ __forceinline__ T result(float x) {
+  constexpr float MOST = 65504.f;
+  if (std::is_same<T, f16_t>::value && fabsf(x) < __builtin_inff()) x = __builtin_amdgcn_fmed3f(x, -MOST, MOST);
+  return (T)x;
+}
 template <class T>
 __device__ __forceinline__ void store4(T* p, const float* x, float f, bool vectors) {
   using T4 = T __attribute__((ext_vector_type(4)));
   T4 z;
 #pragma unroll
-  for (int i = 0; i < 4; i++) z[i] = (T)(x[i] * f);
+  for (int i = 0; i < 4; i++) z[i] = result<T>(x[i] * f);
   if (vectors) {
     *reinterpret_cast<T4*>(p) = z;
   } else {

@@ -157,3 +157,22 @@ def test_scores_of_minus_infinity(gpu, requests, dtype):
         else:
             assert torch.equal(out[t, 2:], v[50, 1].expand(2, dim)), (t, p)
             assert bool(((sums[t, 2:] - 0.25).abs() <= 7 * 2.0 ** -24 * 5.25).all()), (t, p)  # (roundings as above)
+
+
+@pytest.mark.parametrize("requests", [[(i, 1) for i in range(300)], [(0, 300), (100, 150)], [(300, 1)] * 400])
+def test_values_of_the_largest_size(gpu, requests):
+    """Weighted means of 65,504 alone, of -65,504, and of one infinite value: the weights' roundings (half a place each, 2^-11,
+    and the result's) leave the first two finite."""
+    heads, kv, dim, n = 8, 2, 64, 301
+    g = torch.Generator().manual_seed(11)
+    k = torch.randn(n, kv, dim, generator=g).half()
+    v = torch.full((n, kv, dim), 65504.0, dtype=H)
+    v[:, :, 1::2] *= -1
+    v[0, 1, 6] = math.inf
+    q = (2 * torch.randn(sum(f for _, f in requests), heads, dim, generator=g)).half()
+    out, _ = run(step(requests, heads, k, v), q, 0.125)
+    assert bool((out[:, 4:, 6] == math.inf).all())
+    out[:, 4:, 6] = 65504.0
+    assert bool(torch.isfinite(out).all())
+    assert float((out[..., 0::2].double() - 65504).abs().max()) <= 65504 * 2.0 ** -10
+    assert float((out[..., 1::2].double() + 65504).abs().max()) <= 65504 * 2.0 ** -10
