@@ -75,6 +75,14 @@ def _matrix(t, name, device, dtype=None, shape=None):
     return t.data_ptr(), stride
 
 
+def _entries(t, name):
+    """Entries of a tensor of one dimension."""
+    shape = t.shape
+    if len(shape) != 1:
+        raise ValueError("%s must have one dimension, not shape %s" % (name, tuple(shape)))
+    return shape[0]
+
+
 def _type_of(t, name, allowed):
     code = _code(t.dtype)
     if code not in allowed:
@@ -218,8 +226,9 @@ def cache_append(keys, values, key_cache, value_cache, slots, positions=None, fr
     """
     cache, d = _cache(key_cache, value_cache)
     _, _, heads, dim = key_cache.shape
-    n, dtype = keys.shape[0], key_cache.dtype
-    k, k_stride = _heads(keys, "keys", d, dtype, n, heads, dim)
+    dtype = key_cache.dtype
+    k, k_stride = _heads(keys, "keys", d, dtype, None, heads, dim)
+    n = keys.shape[0]
     v, v_stride = _heads(values, "values", d, dtype, n, heads, dim)
     if (queries is None) != (rotated is None):
         raise ValueError("queries and rotated come together")
@@ -233,9 +242,7 @@ def cache_append(keys, values, key_cache, value_cache, slots, positions=None, fr
     if frequencies is not None:
         if positions is None:
             raise ValueError("frequencies need positions")
-        if frequencies.dim() != 1:
-            raise ValueError("frequencies must have one dimension")
-        pairs = frequencies.shape[0]
+        pairs = _entries(frequencies, "frequencies")
     _lib.check(_lib.load().tt_cache_append(
         cache, n, _flat(slots, "slots", _I64, (n,), d), _flat(positions, "positions", _I32, (n,), d),
         _flat(frequencies, "frequencies", _F32, (pairs,), d), pairs, 1 if interleaved else 0, k, k_stride, v, v_stride,
@@ -258,7 +265,7 @@ def cache_attention(queries, key_cache, value_cache, tables, offsets, lengths, o
     """
     cache, d = _cache(key_cache, value_cache)
     _, _, heads, dim = key_cache.shape
-    dtype, n = key_cache.dtype, lengths.shape[0]
+    dtype, n = key_cache.dtype, _entries(lengths, "lengths")
     q, q_stride = _heads(queries, "queries", d, dtype, None, None, dim)
     tokens, q_heads, _ = queries.shape
     o, o_stride = _heads(out, "out", d, dtype, tokens, q_heads, dim)
@@ -294,9 +301,9 @@ def _adjustment(logits, device, history, history_offsets, repetition, presence, 
         raise ValueError("penalties need a history")
     n_history = n_biases = n_masks = mask = mask_stride = 0
     if history is not None:
-        n_history = history.shape[0]
+        n_history = _entries(history, "history")
     if bias_ids is not None:
-        n_biases = bias_ids.shape[0]
+        n_biases = _entries(bias_ids, "bias_ids")
     if masks is not None:
         mask, mask_stride = _matrix(masks, "masks", device)
         n_masks, words = masks.shape
