@@ -497,10 +497,9 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, const Place
 constexpr float SLACK = 8.f;
 template <class T>
 constexpr float HEAD = std::is_same<T, f16_t>::value ? 7.f : 0.f;
-// m after a tile whose largest score is top (differences: near the ends of the range, and
-// without one, sums would round to either side)
+// Whether m goes up to top - HEAD (the difference: far from zero a sum rounds to either side)
 template <class T>
-__device__ __forceinline__ float raised(float m, float top) { return top - m > SLACK + HEAD<T> ? top - HEAD<T> : m; }
+__device__ __forceinline__ bool rises(float m, float top) { return top - m > SLACK + HEAD<T>; }
 
 // ---- 16 rows a wave: single tokens -----------------------------------------------
 
@@ -639,10 +638,10 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
           s[i][e] *= c;
           top = fmaxf(top, s[i][e]);
         }
-      if (__ballot(raised<T>(m, top) != m)) {
+      if (__ballot(rises<T>(m, top))) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        top = raised<T>(m, top);  // (a row's own choice: its result does not depend on its neighbours)
+        top = rises<T>(m, top) ? top - HEAD<T> : m;  // (a row's own choice: its result does not depend on its neighbours)
         const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
         m = top;
         sum *= f;
@@ -897,27 +896,29 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
 #pragma unroll
           for (int e = 0; e < 16; e++) top = fmaxf(top, s[i][e]);
         top *= c;
-        if (__ballot(raised<T>(m, top) != m)) {
+        float base = m == NEG_INF ? 0.f : m;
+        if (__ballot(rises<T>(m, top) || fabsf(m) >= PLAIN_MOST)) {
           top = fmaxf(top, __shfl_xor(top, 32));
-          top = raised<T>(m, top);  // (a row's own choice: its result does not depend on its neighbours)
+          top = rises<T>(m, top) ? top - HEAD<T> : m;  // (a row's own choice: its result does not depend on its neighbours)
           const float f = top == m ? 1.f : __builtin_amdgcn_exp2f(m - top);
           m = top;
           sum *= f;
 #pragma unroll
           for (int d = 0; d < DT; d++) o[d] *= f;
-        }
-        float base = m == NEG_INF ? 0.f : m, by = c;
-        // One multiply-add gives an exponent, by the exact product of score and scale.  m is
-        // rounded, and half its last place is what the largest weight would be off by, to
-        // overflow: far maxima's exponents are the difference of rounded products.
-        if (fabsf(base) >= PLAIN_MOST) {
+          base = m == NEG_INF ? 0.f : m;
+          // One multiply-add gives an exponent, by the exact product of score and scale.  m is
+          // rounded, and half its last place is what the largest weight would be off by, to
+          // overflow: far maxima's exponents are the difference of rounded products, brought
+          // to the form that the multiply-add takes.
+          if (fabsf(base) >= PLAIN_MOST) {
 #pragma clang fp contract(off)
+            const float back = 1.f / c;
 #pragma unroll
-          for (int i = 0; i < 2; i++)
+            for (int i = 0; i < 2; i++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) s[i][e] = s[i][e] * c - base;
-          base = 0.f;
-          by = 1.f;
+              for (int e = 0; e < 16; e++) s[i][e] = (s[i][e] * c - base) * back;
+            base = 0.f;
+          }
         }
         // (the exponentials of a step's weights are between the products of the last one:
         // with one place found by a lane instead of a row's by 16, 1,258 us -> 1,204)
@@ -925,7 +926,7 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
         auto weigh = [&](int i) {
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], by, -base));
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 2][i % 2 * 8 + e], c, -base));
             sum += x;
             weights[i & 1][e] = (T)x;
           }
