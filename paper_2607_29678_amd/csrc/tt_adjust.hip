@@ -7,11 +7,14 @@
 // all of a thread's loads under way before the lists are read.
 //
 // What bounds it: reading and writing the rows.  512 rows of 100,257 in f32 with 2,000
-// tokens of history and masks take 83 us, 5.0 TB/s (70 without lists and masks).  The
-// gradient of 1,536 rows in bf16 takes 108 us without a history and 205 with one of
-// 1,000 tokens a row: 24 of those are every block's reading of the lists, the rest the
-// logits of repeated tokens, whose sign the slope depends on: scattered reads, a
-// million of them.  32 rows of 50,257: the host call.
+// tokens of history and masks take 83 us, 5.0 TB/s (70 without lists and masks); in bf16
+// 72, where the rows alone take 42: every block of 4,096 columns reads the row's whole
+// history, and its stores wait for that.  The gradient of 1,536 rows in bf16 takes 108 us
+// without a history and 206 with one of 1,000 tokens a row.  Its traffic, with scattered
+// reads of the logits of repeated tokens, whose sign the slope depends on, is 745 MB, 150 us
+// at a copy's rate.  The rest is the order of a block's work: lists, barrier, vectors and
+// logits, stores, with nothing of the next columns under way.  32 rows of 50,257: the host
+// call.
 #include "tt_scores.h"
 
 namespace tt {
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(ADJ_THREADS) void adjust_kernel(AdjustArgs<T> g) {
   const int vecs = (int)((a.vocab - head) / N), tail = head + vecs * N, v0 = (int)chunk * ADJ_THREADS * VECS;
   const int64_t base = head + (int64_t)v0 * N;
   const bool last = chunk + 1 == (uint32_t)g.chunks;
-  // the block's columns (the last block may have none but the tail, which begins up to N - 1 before its base)
+  // the block's columns (the last block may have none but the tail, which begins up to N before its base)
   const int64_t lo = !chunk ? 0 : last && tail < base ? tail : base, hi = last ? a.vocab : base + COLS;
   // What does not depend on the lists is asked for first; but the gradient asks for
   // its vectors when it knows which logits it needs, so that both come at once.
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(ADJ_THREADS) void adjust_kernel(AdjustArgs<T> g) {
         hit[k] |= ((n.x ? 1u : 0u) | (n.y ? 2u : 0u) | (n.z ? 4u : 0u) | (n.w ? 8u : 0u)) << i;
       }
     }
-    if (GRAD) hit[k] &= allowed[k];  (void)0;
+    if (GRAD) hit[k] &= allowed[k];
     if (GRAD && hit[k]) z[k] = load_once(logits + base + (int64_t)v * N);
   }
 #pragma unroll

@@ -45,9 +45,14 @@ constexpr int ATT_THREADS = 256;
 constexpr int ATT_WAVES = 4;
 constexpr int STAGED = 1024;  // requests whose offsets and lengths are held in LDS for the search
 // Rows (tokens times query heads of a key head) of a request up to which, on average,
-// the small path takes a step.  us by the small and by the large path: 2 requests of
-// 120,000 tokens, 7 rows 132 / 188; 64 of 20,000 in a window of 4,096, 40 rows 443 /
-// 205 (the small path reads the keys once for every 16 rows).
+// the small path takes a step.  us by the small and by the large path, heads of 128 but
+// where 64 is said: 300 requests of 2,000 tokens, 1 row of 64 471 / 524; 4 of 700, 4 rows
+// 21.8 / 24.8; 64 of 4,000, 4 rows 213 / 204, 16 rows 227 / 204, 20 rows 337 / 205, 40 rows
+// 611 / 210 (the small path reads the keys once for every 16 rows); 2 of 120,000, 7 rows
+// 126 / 114; 64 of 20,000 in a window of 4,096, 16 rows of 64 128 / 122, 40 rows 328 / 127.
+// (So long requests of 4 to 16 rows would be 5 to 10% faster by the large path.)  The mean
+// speaks for all of a step: 256 single tokens behind 4,000 and a prompt of 700 840 / 845, of
+// 900 834 / 954; 32 single tokens with 8 rows each and 60 more of one request 184 / 138.
 constexpr int SMALL_ROWS = 16;
 constexpr int EACH = 4;       // items counted by a thread at a time
 
@@ -497,6 +502,12 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, const Place
 constexpr float SLACK = 8.f;
 template <class T>
 constexpr float HEAD = std::is_same<T, f16_t>::value ? 7.f : 0.f;
+// A product that no addition may be joined to: differences of such from a maximum of such
+// are not above 0, however large they are
+__device__ __forceinline__ float rounded(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
 // Whether m goes up to top - HEAD (the difference: far from zero a sum rounds to either side)
 template <class T>
 __device__ __forceinline__ bool rises(float m, float top) { return top - m > SLACK + HEAD<T>; }
@@ -635,7 +646,7 @@ __device__ __forceinline__ void small_path(const AttentionArgs& a, Search& searc
       for (int i = 0; i < 2; i++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          s[i][e] *= c;
+          s[i][e] = rounded(s[i][e], c);
           top = fmaxf(top, s[i][e]);
         }
       if (__ballot(rises<T>(m, top))) {
@@ -911,17 +922,18 @@ __device__ __forceinline__ void large_path(const AttentionArgs& a, Search& searc
           // overflow: far maxima's exponents are the difference of rounded products, brought
           // to the form that the multiply-add takes.
           if (fabsf(base) >= PLAIN_MOST) {
-#pragma clang fp contract(off)
             const float back = 1.f / c;
 #pragma unroll
             for (int i = 0; i < 2; i++)
 #pragma unroll
-              for (int e = 0; e < 16; e++) s[i][e] = (s[i][e] * c - base) * back;
+              for (int e = 0; e < 16; e++) s[i][e] = (rounded(s[i][e], c) - base) * back;
             base = 0.f;
           }
         }
         // (the exponentials of a step's weights are between the products of the last one:
-        // with one place found by a lane instead of a row's by 16, 1,258 us -> 1,204)
+        // with one place found by a lane instead of a row's by 16, 1,258 us -> 1,204.  The
+        // additions to the row's sum are not: the compiler puts a tile's 32 behind its last
+        // product, in one chain)
         Vec8<T> weights[2];
         auto weigh = [&](int i) {
 #pragma unroll
@@ -1130,7 +1142,7 @@ Plan plan_of(bool small, int32_t q_heads, int32_t kv_heads, int32_t dim) {
   p.rows = small ? SMALL_ROWS : 128;
   p.keys = small ? 32 : 64;
   p.workers = BLOCKS / (dim > 128 ? 2 : 1) * (small ? ATT_WAVES : 1);
-  p.least = small ? 1 : 4;  // (4 short requests: 24.0 us, with 2 units 24.9)
+  p.least = small ? 1 : 4;  // (a prompt of 700 tokens 46 us, with 1 unit 53; 4 requests of 700, 5 tokens each 24.4 and 21.8)
   p.heads = per_kv < p.rows ? per_kv : p.rows;
   p.groups = (per_kv + p.heads - 1) / p.heads;
   p.tokens = p.rows / p.heads;
