@@ -20,9 +20,9 @@
 // What bounds it: single tokens, reads of keys and values (96 requests of 4,000 tokens,
 // 32 heads over 8 of 128 elements: 1.63 GB in 317 us, 5.1 TB/s, the rate of a plain
 // copy being 4.9); prompts, the matrix cores and the vector instructions beside them
-// (14,001 tokens, the same heads: 1,175 us, 760 TFLOP/s; a plain library product
-// 1,200 to 1,490 on these cards); a few short requests, the search of every block's
-// part, cold, 6 us of 13, and the join, 4 to 8.
+// (14,001 tokens, the same heads: 1,150 to 1,240 us on several cards, 720 to 780
+// TFLOP/s; a plain library product 1,160 to 1,490); a few short requests, the search of
+// every block's part, cold, 6 us of 13, and the join, 4 to 9.
 #include "tt_cache.h"
 
 namespace tt {
@@ -493,8 +493,11 @@ __device__ __forceinline__ int64_t vector_at(const AttentionArgs& a, const Place
 
 // The weights 2^(score - m) are rounded to the type for the second product, their sum is
 // of 32 bits.  (One rounding a weight, half a place: the matrix cores take operands of the
-// type, and the result is rounded by as much again.)  m goes up only where a score is more
-// than SLACK powers of two above the largest it is of.
+// type, and the result is rounded by as much again; errors come to 1.4 times those of
+// weights of 32 bits.  A second product, of what the rounding leaves, takes no time on the
+// small path up to 128 elements, but what it leaves of a weight may be 0 or negative, and an
+// infinite value would come out as NaN.)  m goes up only where a score is more than SLACK
+// powers of two above the largest it is of.
 // A weight of f16 has full places from 2^-14 on and none below 2^-25, while the sum holds
 // them all: many small ones would be missing above and there below, 16% of a result with
 // one key 17.4 above 20,000 others.  So m lies HEAD below that largest score: weights go up
@@ -1210,7 +1213,8 @@ extern "C" int tt_cache_attention(const tt_cache* cache, const tt_attention* ste
                   (uint32_t)(cache->slot_stride / 8),
                   s.q_heads / cache->kv_heads,
                   in_vectors(s.queries, s.query_stride) && in_vectors(s.out, s.out_stride),
-                  // at most this many items of a head unit, units of an item and head units
+                  // at most this many items of a head unit, units of an item and head units (8,192 tokens
+                  // of 1,000 requests, tables of 131,072: 160 us, found with short sums 153; of 4 prompts 303 both)
                   s.n_requests > STAGED || (double)(s.tokens + s.n_requests) * ((double)capacity / 32 + 3) * s.q_heads * 2 >= INT32_MAX,
                   static_cast<uint8_t*>(workspace)};
   return cache->type == TT_BF16 ? run_attention<bf16_t>(a, static_cast<hipStream_t>(stream))
